@@ -37,3 +37,17 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .tied import (  # noqa: F401
+    DST_FP8_ROW,
+    DST_FP8_SQUARE,
+    Fp8Matrix,
+    TiedProjection,
+    dst_dropout,
+    dst_embed,
+    dst_linear_fp8,
+    dst_linear_fp8_workspace_bytes,
+    dst_matmul_fp8,
+    dst_matmul_fp8_workspace_bytes,
+    dst_quantize_fp8,
+    dst_sample,
+)

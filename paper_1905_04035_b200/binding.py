@@ -69,6 +69,17 @@ class _AccumPlan(ctypes.Structure):
                 ("n_slice_rows", ctypes.c_int64), ("converts", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class _Dropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("offset_device", ctypes.c_void_p), ("row_offset", ctypes.c_int64)]
+
+
+class _Fp8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ld_scale", ctypes.c_int64), ("block", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 RESULT_BYTES = ctypes.sizeof(_Result)
 DST_GRAD_DENSE, DST_GRAD_SLICES = 0, 1
 DST_ACC_STOCK, DST_ACC_PROPOSED, DST_ACC_SPARSE_AS_DENSE = 0, 1, 2
@@ -106,6 +117,17 @@ SYMBOLS = {
                                            ctypes.POINTER(_AccumPlan)]),
     "dst_accumulate": (ctypes.c_int, [ctypes.POINTER(_Grad), _i32, _i64, _i64, _i32, _vp, _vp, _vp, _i64, _vp,
                                       ctypes.POINTER(_Opts), _vp, _sz, _vp, ctypes.POINTER(_AccumPlan)]),
+    # include/dst_tied.h
+    "dst_dropout": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i64, _vp, _i64, _i32, _i64, _i64, ctypes.c_float,
+                                   ctypes.POINTER(_Dropout), _vp]),
+    "dst_embed": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i64, _i64, _i32, _vp, _i64, _vp, _i32, ctypes.c_float,
+                                 ctypes.POINTER(_Dropout), _vp, _vp]),
+    "dst_quantize_fp8": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, ctypes.POINTER(_Fp8), ctypes.POINTER(_Fp8), _vp]),
+    "dst_matmul_fp8_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "dst_matmul_fp8": (ctypes.c_int, [ctypes.POINTER(_Fp8), ctypes.POINTER(_Fp8), _vp, _i64, _i32, _vp, _sz, _vp]),
+    "dst_linear_fp8_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "dst_linear_fp8": (ctypes.c_int, [_vp, _i64, _i32, _i64, ctypes.POINTER(_Fp8), _vp, _i64, _i32, _vp, _sz, _vp]),
+    "dst_sample": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
 }
 
 

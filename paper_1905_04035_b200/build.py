@@ -11,8 +11,9 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libdst_b200.so")
 SOURCES = ["dst_api.cu", "dst_index_kernels.cu", "dst_front_cluster.cu", "dst_reduce_kernels.cu",
-           "dst_accumulate_kernels.cu"]
-HEADERS = [os.path.join(CSRC, "dst_common.cuh"), os.path.join(INCLUDE, "dst.h")]
+           "dst_accumulate_kernels.cu", "dst_dropout.cu", "dst_fp8.cu", "dst_sample.cu", "dst_tied_api.cu"]
+HEADERS = [os.path.join(CSRC, "dst_common.cuh"), os.path.join(CSRC, "dst_tied.cuh"), os.path.join(INCLUDE, "dst.h"),
+           os.path.join(INCLUDE, "dst_tied.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", INCLUDE]
 

@@ -47,6 +47,9 @@ static int sm_count() {
     return n;
 }
 
+int device_sm_count() { return sm_count(); }
+void count_launches(int n) { g_launches += n; }
+
 // `dense`: the n_dense dense partners (n_dense <= kMaxDensePartners, no null among them), added after the value
 // rows in the order given.
 static int densify_impl(const dst_slice_t* slices, int32_t R, int64_t d, int64_t vocab, const void* const* dense,

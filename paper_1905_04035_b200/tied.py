@@ -1,0 +1,300 @@
+"""ctypes marshalling for the operators around the tied weight (see ``include/dst_tied.h`` for the contract).
+
+The functions carry the names of the C entry points; ``Fp8Matrix`` and ``TiedProjection`` own caller-side buffers.
+Matrices are 2-D CUDA tensors with contiguous rows (any distance between rows); outputs are allocated by the caller.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from typing import Optional
+
+import torch
+
+from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _Fp8, load_library
+
+DST_FP8_ROW, DST_FP8_SQUARE = 0, 1
+_TYPES = {torch.float32: DST_F32, torch.bfloat16: DST_BF16}
+_INDEX = {torch.int32: DST_I32, torch.int64: DST_I64}
+_nothing = contextlib.nullcontext()
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, name: str):
+    """(pointer, leading dimension, type) of a [rows, cols] matrix with contiguous rows."""
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
+    ld, step = t.stride()
+    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return t.data_ptr(), max(ld, cols) if rows > 1 else max(cols, 1), kind
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, device, name: str):
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be contiguous [%d]" % (name, n))
+    if t.device != device:
+        raise ValueError("all tensors must live on the same device")
+    return t.data_ptr()
+
+
+def _same_device(device, *tensors) -> None:
+    if device.type != "cuda":
+        raise ValueError("tensors must be CUDA tensors")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors must live on the same device")
+
+
+def _on(device):
+    """The context in which work for `device` is enqueued (nothing to do where it is current already)."""
+    return _nothing if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream(stream, device) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def _drop(p, seed, offset, offset_tensor, row_offset, device) -> _Dropout:
+    if offset_tensor is not None:
+        if offset_tensor.dtype != torch.int64 or offset_tensor.numel() != 1:
+            raise TypeError("offset_tensor must hold one int64")
+        _same_device(device, offset_tensor)
+    return _Dropout(p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF,
+                    None if offset_tensor is None else offset_tensor.data_ptr(), row_offset)
+
+
+def dst_dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, offset: int = 0, *,
+                residual: Optional[torch.Tensor] = None, scale: float = 1.0, row_offset: int = 0,
+                offset_tensor: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue ``dst_dropout``: out = residual + scale * dropout(x).  The same call on the output's gradient, without
+    the residual, is the gradient of ``x``.  ``out`` may be ``x`` or ``residual``."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, d]")
+    rows, d = x.shape
+    device = out.device
+    _same_device(device, x, residual)
+    px, ldx, tx = _matrix(x, rows, d, "x")
+    po, ldo, to = _matrix(out, rows, d, "out")
+    pr, ldr = None, 0
+    if residual is not None:
+        pr, ldr, tr = _matrix(residual, rows, d, "residual")
+        if tr != to:
+            raise TypeError("residual and out must share a dtype")
+    drop = _drop(p, seed, offset, offset_tensor, row_offset, device)
+    with _on(device):
+        rc = load_library().dst_dropout(px, ldx, tx, pr, ldr, po, ldo, to, rows, d, scale, drop, _stream(stream, device))
+    if rc != 0:
+        raise DstError(rc, "dst_dropout")
+    return out
+
+
+def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *, scale: float = 1.0,
+              position: Optional[torch.Tensor] = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+              row_offset: int = 0, offset_tensor: Optional[torch.Tensor] = None, result: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """Enqueue ``dst_embed``: out = dropout(scale * weight[indices] + position rows).  Its gradient's value rows are
+    ``dst_dropout(grad, values, p, seed, offset, scale=scale)``, which ``dst_densify`` takes with ``indices``.
+
+    ``result``: an int32/uint8 CUDA tensor of at least 24 bytes that receives ``dst_result_t``."""
+    index_type = _INDEX.get(indices.dtype)
+    if index_type is None:
+        raise TypeError("indices must be int32 or int64, got %s" % indices.dtype)
+    if indices.dim() != 1 or not indices.is_contiguous() or weight.dim() != 2:
+        raise ValueError("indices must be 1-D contiguous and weight [vocab, d]")
+    n, (vocab, d) = indices.shape[0], weight.shape
+    device = out.device
+    _same_device(device, indices, weight, position, result)
+    pw, _, tw = _matrix(weight, vocab, d, "weight")
+    po, _, to = _matrix(out, n, d, "out")
+    if not weight.is_contiguous() or not out.is_contiguous():
+        raise ValueError("weight and out must be contiguous")
+    n_pos, pp = 0, None
+    if position is not None:
+        if position.dtype != torch.float32:
+            raise TypeError("position must be float32, got %s" % position.dtype)
+        if position.dim() != 2 or position.shape[1] != d or not position.is_contiguous():
+            raise ValueError("position must be contiguous [n_positions, d]")
+        n_pos, pp = position.shape[0], position.data_ptr()
+    if result is not None and (not result.is_contiguous() or result.numel() * result.element_size() < 24):
+        raise ValueError("result must be contiguous and hold 24 bytes")
+    drop = _drop(p, seed, offset, offset_tensor, row_offset, device)
+    with _on(device):
+        rc = load_library().dst_embed(indices.data_ptr(), n, index_type, pw, vocab, d, tw, pp, n_pos, po, to, scale, drop,
+                                      None if result is None else result.data_ptr(), _stream(stream, device))
+    if rc != 0:
+        raise DstError(rc, "dst_embed")
+    return out
+
+
+class Fp8Matrix:
+    """Owns a matrix [rows, cols] in 8-bit floating point (``dst_fp8_t``): ``q`` [rows, cols padded to 16] and one
+    scale for each block: 128 columns of a row (``DST_FP8_ROW``; ``scale`` [column blocks, rows padded]) or 128 x 128
+    (``DST_FP8_SQUARE``; ``scale`` [column blocks, row blocks])."""
+
+    def __init__(self, rows: int, cols: int, block: int = DST_FP8_ROW, *, device="cuda"):
+        if block not in (DST_FP8_ROW, DST_FP8_SQUARE):
+            raise ValueError("block must be DST_FP8_ROW or DST_FP8_SQUARE")
+        if rows < 0 or cols < 0:
+            raise ValueError("rows and cols must not be negative")
+        self.rows, self.cols, self.block = rows, cols, block
+        across = -(-rows // 128) if block == DST_FP8_SQUARE else rows
+        self.q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)
+        self.scale = torch.empty(-(-cols // 128), -(-across // 4) * 4, dtype=torch.float32, device=device)
+        self.device = self.q.device
+        self._c = _Fp8(self.q.data_ptr(), self.scale.data_ptr(), rows, cols, self.q.shape[1], self.scale.shape[1], block, 0)
+
+    def part(self, rows: int, cols: int) -> "Fp8Matrix":
+        """The same buffers seen as a smaller matrix (leading dimensions stay)."""
+        if not (0 <= rows <= self.rows and 0 <= cols <= self.cols):
+            raise ValueError("a part is at most [%d, %d]" % (self.rows, self.cols))
+        m = object.__new__(Fp8Matrix)
+        m.rows, m.cols, m.block, m.q, m.scale, m.device = rows, cols, self.block, self.q[:rows], self.scale, self.device
+        m._c = _Fp8(self._c.q, self._c.scale, rows, cols, self._c.ld, self._c.ld_scale, self.block, 0)
+        return m
+
+    def dequantize(self) -> torch.Tensor:
+        """The fp32 matrix that the 8-bit one stands for."""
+        across = self.scale.T.repeat_interleave(128, 0) if self.block == DST_FP8_SQUARE else self.scale.T
+        return self.q[:, :self.cols].float() * across[:self.rows, :-(-self.cols // 128)].repeat_interleave(128, 1)[:, :self.cols]
+
+
+def dst_quantize_fp8(x: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, *, stream=None) -> None:
+    """Enqueue ``dst_quantize_fp8``: x into ``q`` and its transpose into ``qt`` (either may be None)."""
+    some = q if q is not None else qt
+    if some is None:
+        raise ValueError("q or qt must be given")
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    _same_device(some.device, x, None if q is None else q.q, None if qt is None else qt.q)
+    px, ldx, tx = _matrix(x, rows, cols, "x")
+    with _on(some.device):
+        rc = load_library().dst_quantize_fp8(px, ldx, tx, rows, cols, None if q is None else q._c,
+                                             None if qt is None else qt._c, _stream(stream, some.device))
+    if rc != 0:
+        raise DstError(rc, "dst_quantize_fp8")
+
+
+def dst_matmul_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load_library().dst_matmul_fp8_workspace_bytes(M, N, K))
+
+
+def dst_linear_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load_library().dst_linear_fp8_workspace_bytes(M, N, K))
+
+
+def _workspace(t: Optional[torch.Tensor]):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def dst_matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
+                   stream=None) -> torch.Tensor:
+    """Enqueue ``dst_matmul_fp8``: out [a.rows, b.rows] = a b^T."""
+    device = out.device
+    _same_device(device, a.q, b.q, workspace)
+    po, ldo, to = _matrix(out, a.rows, b.rows, "out")
+    ws, ws_bytes = _workspace(workspace)
+    with _on(device):
+        rc = load_library().dst_matmul_fp8(a._c, b._c, po, ldo, to, ws, ws_bytes, _stream(stream, device))
+    if rc != 0:
+        raise DstError(rc, "dst_matmul_fp8")
+    return out
+
+
+def dst_linear_fp8(x: torch.Tensor, w: Fp8Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
+                   stream=None) -> torch.Tensor:
+    """Enqueue ``dst_linear_fp8``: out [x.rows, w.rows] = quantised(x) w^T."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    device, m = out.device, x.shape[0]
+    _same_device(device, x, w.q, workspace)
+    px, ldx, tx = _matrix(x, m, w.cols, "x")
+    po, ldo, to = _matrix(out, m, w.rows, "out")
+    ws, ws_bytes = _workspace(workspace)
+    with _on(device):
+        rc = load_library().dst_linear_fp8(px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes, _stream(stream, device))
+    if rc != 0:
+        raise DstError(rc, "dst_linear_fp8")
+    return out
+
+
+def dst_sample(logits: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, *,
+               temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+               top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+               prob: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue ``dst_sample``: a token per row of ``logits`` from the row's uniform number and filters."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    rows, vocab = logits.shape
+    device = logits.device
+    token_type = _INDEX.get(tokens.dtype)
+    if token_type is None:
+        raise TypeError("tokens must be int32 or int64, got %s" % tokens.dtype)
+    _same_device(device)
+    pl, ld, tl = _matrix(logits, rows, vocab, "logits")
+    f32, lib = torch.float32, load_library()
+    args = (_vector(uniform, rows, f32, device, "uniform"), _vector(temperature, rows, f32, device, "temperature"),
+            _vector(top_k, rows, torch.int32, device, "top_k"), _vector(top_p, rows, f32, device, "top_p"),
+            _vector(min_p, rows, f32, device, "min_p"), _vector(tokens, rows, tokens.dtype, device, "tokens"))
+    if args[0] is None:
+        raise ValueError("uniform must be given")
+    with _on(device):
+        rc = lib.dst_sample(pl, ld, tl, rows, vocab, *args, token_type, _vector(prob, rows, f32, device, "prob"),
+                            _stream(stream, device))
+    if rc != 0:
+        raise DstError(rc, "dst_sample")
+    return tokens
+
+
+class TiedProjection:
+    """The pre-softmax projection through the tied weight [vocab, d] in 8-bit floating point, for up to ``max_tokens``
+    rows a call: owns the quantised weight and the workspaces, the arithmetic stays in the library.
+
+    ``update(weight)`` quantises the weight (after every optimizer step), ``logits(x, out)`` is x W^T, and with
+    ``training`` ``backward(dlogits, x, dx, dweight)`` gives both gradients; ``dweight`` is the dense partner that
+    ``dst_densify`` adds to the embedding's gradient."""
+
+    def __init__(self, vocab: int, d: int, max_tokens: int, *, training: bool = True, device="cuda"):
+        self.vocab, self.d, self.max_tokens, self.training = vocab, d, max_tokens, training
+        self.weight = Fp8Matrix(vocab, d, DST_FP8_SQUARE, device=device)
+        self.device = self.weight.device
+        need = dst_linear_fp8_workspace_bytes(max_tokens, vocab, d)
+        if training:
+            # everything backward needs is there from the start: nothing is allocated, or freed, under a caller's stream
+            self.weight_t = Fp8Matrix(d, vocab, DST_FP8_SQUARE, device=device)
+            self.grad = Fp8Matrix(max_tokens, vocab, device=device)
+            self.grad_t = Fp8Matrix(vocab, max_tokens, device=device)
+            self.x_t = Fp8Matrix(d, max_tokens, device=device)
+            need = max(need, dst_matmul_fp8_workspace_bytes(max_tokens, d, vocab),
+                       dst_matmul_fp8_workspace_bytes(vocab, d, max_tokens))
+        self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+
+    def update(self, weight: torch.Tensor, stream=None) -> None:
+        dst_quantize_fp8(weight, self.weight, self.weight_t if self.training else None, stream=stream)
+
+    def _check(self, tokens: int) -> None:
+        if tokens > self.max_tokens:
+            raise ValueError("at most %d tokens a call, got %d" % (self.max_tokens, tokens))
+
+    def logits(self, x: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
+        self._check(x.shape[0])
+        return dst_linear_fp8(x, self.weight, out, self.workspace, stream=stream)
+
+    def backward(self, dlogits: torch.Tensor, x: torch.Tensor, dx: torch.Tensor, dweight: torch.Tensor, stream=None) -> None:
+        """dx [tokens, d] = dlogits W and dweight [vocab, d] = dlogits^T x."""
+        if not self.training:
+            raise ValueError("the projection was made without training=True")
+        m = x.shape[0]
+        self._check(m)
+        g, gt, xt = self.grad.part(m, self.vocab), self.grad_t.part(self.vocab, m), self.x_t.part(self.d, m)
+        dst_quantize_fp8(dlogits, g, gt, stream=stream)
+        dst_quantize_fp8(x, None, xt, stream=stream)
+        dst_matmul_fp8(g, self.weight_t, dx, self.workspace, stream=stream)
+        dst_matmul_fp8(gt, xt, dweight, self.workspace, stream=stream)

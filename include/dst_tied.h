@@ -91,7 +91,8 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
  * out[m, n] = sum over column blocks b of a.scale[b, m] * b.scale[b, n] * sum_{k in b} a.q[m, k] * b.q[n, k]
  * a [M, K], b [N, K], out [M, N] in out_type (fp32 or bf16, rounded once).  Sums over a block and over the blocks are
  * fp32 in an order fixed by the shapes.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes
- * (may be 0), 256-byte aligned.
+ * (may be 0), 256-byte aligned; as much is enough for every smaller M, N and K too.  A device-side wait that gives up
+ * leaves NaN in the part of `out` that was still to be written.
  */
 size_t dst_matmul_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,

@@ -56,7 +56,8 @@ struct QuantParams {
     Fp8View q, qt;                          // q.q / qt.q null: not wanted
 };
 cudaError_t launch_quantize(const QuantParams& p, int x_type, int sms, cudaStream_t stream);
-size_t matmul_fp8_workspace(long long M, long long N, long long K);
+size_t matmul_fp8_workspace(long long M, long long N, long long K);        // of this product
+size_t matmul_fp8_workspace_bound(long long M, long long N, long long K);  // of this one and every smaller one
 cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace,
                               int sms, cudaStream_t stream);
 

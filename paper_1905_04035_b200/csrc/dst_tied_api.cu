@@ -74,7 +74,7 @@ static LinearLayout linear_layout(int64_t M, int64_t N, int64_t K) {
     L.ld_scale = (M + 3) / 4 * 4;
     L.off_scale = align_up(size_t(M) * size_t(L.ld), 256);
     L.off_matmul = L.off_scale + align_up(size_t((K + 127) / 128) * size_t(L.ld_scale) * 4, 256);
-    L.total = L.off_matmul + matmul_fp8_workspace(M, N, K);
+    L.total = L.off_matmul + matmul_fp8_workspace_bound(M, N, K);
     return L;
 }
 
@@ -141,7 +141,7 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
 
 size_t dst_matmul_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || N <= 0 || K <= 0 || M > kMaxCols || N > kMaxCols || K > kMaxCols) return 0;
-    return matmul_fp8_workspace(M, N, K);
+    return matmul_fp8_workspace_bound(M, N, K);
 }
 
 int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,
@@ -167,13 +167,14 @@ int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const 
     dst_fp8_t a{nullptr, nullptr, M, w->cols, L.ld, L.ld_scale, DST_FP8_ROW, 0};
     if (w->cols > 0) {
         if (!workspace || misaligned(workspace, 256)) return DST_ERR_INVALID_ARG;
-        if (workspace_bytes < L.total) return DST_ERR_WORKSPACE_TOO_SMALL;
+        if (workspace_bytes < L.off_matmul + matmul_fp8_workspace(M, w->rows, w->cols)) return DST_ERR_WORKSPACE_TOO_SMALL;
         a.q = workspace;
         a.scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.off_scale);
         const int rq = dst_quantize_fp8(x, ldx, x_type, M, w->cols, &a, nullptr, stream);
         if (rq != DST_OK) return rq;
     }
-    return matmul_impl(&a, w, out, ldo, out_type, static_cast<char*>(workspace) + L.off_matmul, L.total - L.off_matmul, stream);
+    return matmul_impl(&a, w, out, ldo, out_type, workspace ? static_cast<char*>(workspace) + L.off_matmul : nullptr,
+                       w->cols > 0 ? workspace_bytes - L.off_matmul : 0, stream);
 }
 
 int dst_sample(const void* logits, int64_t ld, int32_t type, int64_t rows, int64_t vocab, const float* uniform,

@@ -91,7 +91,9 @@ def test_matmul_refusals(lib):
     big = need(512, 512, 1 << 17)
     if big:
         many = dict(a=fp8(512, 1 << 17), b=fp8(512, 1 << 17), ldo=512)
-        assert call(**many, ws_bytes=big - 1) == 3 and call(**many, ws=None, ws_bytes=big) == 1 and call(**many, ws=FAKE + 8, ws_bytes=big) == 1
+        assert call(**many, ws_bytes=4) == 3 and call(**many, ws=None, ws_bytes=big) == 1 and call(**many, ws=FAKE + 8, ws_bytes=big) == 1
+    for M, N, K in ((30, 40, 200), (512, 512, 1 << 17), (8000, 512, 33708), (8000, 33708, 512)):
+        assert all(need(m, n, k) <= need(M, N, K) for m in (1, M // 3, M - 1) for n in (1, N // 2, N) for k in (1, K // 2, K))
     assert need(0, 5, 5) == 0 and need(-1, 5, 5) == 0 and need(1 << 31, 5, 5) == 0
 
 
@@ -102,7 +104,7 @@ def test_linear_refusals(lib):
         return lib.dst_linear_fp8(x, ldx, xt, m, fp8(40, 200, block=1) if w == "" else w, out, ldo, ot, ws, ws_bytes, None)
     assert call(xt=3) == 2 and call(ot=3) == 2
     assert call(x=None) == 1 and call(ldx=199) == 1 and call(m=-1) == 1 and call(w=None) == 1 and call(out=None) == 1 and call(ldo=39) == 1
-    assert call(ws=None) == 1 and call(ws=FAKE + 8) == 1 and call(ws_bytes=need - 1) == 3
+    assert call(ws=None) == 1 and call(ws=FAKE + 8) == 1 and call(ws_bytes=100) == 3
     assert call(m=0, x=None, out=None) == 0
 
 

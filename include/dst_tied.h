@@ -63,15 +63,19 @@ int dst_embed(const void* indices, int64_t n_rows, int32_t index_type, const voi
               const dst_dropout_t* drop, dst_result_t* result, dst_stream_t stream);
 
 /*
- * A matrix [rows, cols] in 8-bit floating point (4 exponent bits, 3 mantissa bits, largest value 448) with one fp32
- * scale for each block: DST_FP8_ROW blocks are 128 consecutive columns of one row, DST_FP8_SQUARE blocks are 128 rows
- * by 128 columns (the last ones smaller).  The element stands for q * scale.  q: 16-byte aligned, ld a multiple of 16.
- * scale[b * ld_scale + i] belongs to column block b and to row i (ROW) or row block i (SQUARE).
+ * A matrix [rows, cols] in 8-bit floating point (4 exponent bits, 3 mantissa bits, largest value 448) with one scale, a
+ * power of two, for each block: DST_FP8_ROW blocks are 128 consecutive columns of one row, DST_FP8_SQUARE blocks are
+ * 128 rows by 128 columns (the last ones smaller).  The element stands for q * scale.
+ *   q      [rows, ld], 16-byte aligned, ld a multiple of 16
+ *   scale  one byte for each row and column block, the exponent plus 127 (255: NaN), whatever the kind of block, in the
+ *          order in which the tensor cores take them: tiles of 512 bytes for 128 rows by 4 column blocks; the byte of
+ *          row r and column block b is at (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4 of tile (r / 128) * ld_scale + b / 4.
+ *          ld_scale (tiles for 128 rows) is at least the number of column blocks / 4, rounded up; 16-byte aligned.
  */
 typedef enum { DST_FP8_ROW = 0, DST_FP8_SQUARE = 1 } dst_fp8_block_t;
 typedef struct {
     void* q;
-    float* scale;
+    void* scale;
     int64_t rows, cols, ld, ld_scale;
     int32_t block; /* dst_fp8_block_t */
     int32_t reserved;
@@ -88,11 +92,11 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
                      const dst_fp8_t* qt, dst_stream_t stream);
 
 /*
- * out[m, n] = sum over column blocks b of a.scale[b, m] * b.scale[b, n] * sum_{k in b} a.q[m, k] * b.q[n, k]
- * a [M, K], b [N, K], out [M, N] in out_type (fp32 or bf16, rounded once).  Sums over a block and over the blocks are
- * fp32 in an order fixed by the shapes.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes
- * (may be 0), 256-byte aligned; as much is enough for every smaller M, N and K too.  A device-side wait that gives up
- * leaves NaN in the part of `out` that was still to be written.
+ * out[m, n] = sum over column blocks b of a.scale(m, b) * b.scale(n, b) * sum_{k in b} a.q[m, k] * b.q[n, k]
+ * a [M, K], b [N, K], out [M, N] in out_type (fp32 or bf16, rounded once).  All sums are fp32 in an order fixed by the
+ * shapes.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes (may be 0), 256-byte aligned;
+ * as much is enough for every smaller M, N and K too.  A device-side wait that gives up leaves NaN in the part of `out`
+ * that was still to be written.
  */
 size_t dst_matmul_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,

@@ -7,20 +7,19 @@
 namespace dst {
 
 // ---- quantisation -----------------------------------------------------------------
-// The scale of a block whose largest magnitude has the bits `amax`: the smallest power of two 2^e with
-// amax <= 448 * 2^e.  448 = 1.75 * 2^8, so e is amax's exponent less 8, one more where its mantissa is above 1.75.
-// NaN where the block holds an infinity or a NaN (their bits are the largest).
-__device__ __forceinline__ float block_scale(unsigned amax) {
-    if (amax >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    const unsigned low = 0x0D800000u;                       // 2^-100
-    if (amax < low) amax = low;
-    const unsigned e = (amax >> 23) - 8u + ((amax & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
-    return __uint_as_float(e << 23);
+// The scale of a block whose largest magnitude has the bits `amax`, as an exponent plus 127: the smallest power of two
+// 2^e with amax <= 448 * 2^e.  448 = 1.75 * 2^8, so e is amax's exponent less 8, one more where its mantissa is above
+// 1.75.  255 (NaN) where the block holds an infinity or a NaN (their bits are the largest).
+__device__ __forceinline__ unsigned block_exponent(unsigned amax) {
+    if (amax >= 0x7F800000u) return 255u;
+    amax = max(amax, 0x0D800000u);                          // 2^-100
+    return (amax >> 23) - 8u + ((amax & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
 }
-// its reciprocal: exact, a power of two
-__device__ __forceinline__ float block_unscale(float scale) { return __uint_as_float(0x7F000000u - __float_as_uint(scale)); }
-__device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
+// 2^-e: exact (what a block with the scale NaN is multiplied by does not matter)
+__device__ __forceinline__ float block_unscale(unsigned exponent) { return __uint_as_float((254u - min(exponent, 253u)) << 23); }
+__device__ __forceinline__ uint8_t* scale_byte(const Fp8View& m, long long row, long long block) {
+    return m.scale + ((row >> 7) * m.ld_scale + (block >> 2)) * kScaleTile + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
 // four floats to four e4m3 bytes, round to nearest even
 __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d) {
     const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -28,98 +27,162 @@ __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d
     return lo | hi << 16;
 }
 
-constexpr int kQuantThreads = 256;
+// four neighbouring elements as they are stored
+template <typename T> struct Four;
+template <> struct Four<float> {
+    float4 v;
+    __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void set(int j, float x) { (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) = x; }
+    __device__ __forceinline__ float get(int j) const { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+    __device__ __forceinline__ unsigned amax() const {
+        const unsigned m = 0x7FFFFFFFu;
+        return max(max(__float_as_uint(v.x) & m, __float_as_uint(v.y) & m), max(__float_as_uint(v.z) & m, __float_as_uint(v.w) & m));
+    }
+};
+template <> struct Four<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void clear() { v = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
+        unsigned& w = j < 2 ? v.x : v.y;
+        const unsigned b = __bfloat16_as_ushort(x);
+        w = j & 1 ? (w & 0xFFFFu) | b << 16 : (w & 0xFFFF0000u) | b;
+    }
+    __device__ __forceinline__ float get(int j) const {
+        const unsigned w = j < 2 ? v.x : v.y;
+        return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    __device__ __forceinline__ unsigned amax() const {
+        const unsigned m = __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu);
+        return max(m << 16, m & 0xFFFF0000u);
+    }
+};
 
-// A CTA takes 128 x 128 elements: each is read once, into shared memory, and rounded for the matrix and for its
-// transpose from there.  Rows of the tile are 129 floats apart, so that lanes on neighbouring columns and lanes on
-// neighbouring rows both find 32 different banks.
-template <typename T, bool SQUARE>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize_tile(const __grid_constant__ QuantParams p) {
-    extern __shared__ float tile[];                          // [128][129]
-    __shared__ unsigned warp_max[kQuantThreads / 32];
+constexpr int kQuantThreads = 256, kQuantWarps = kQuantThreads / 32, kQuantRows = 128 / kQuantWarps;
+constexpr int kQuantPitch = 132;                           // elements between rows of the staged tile
+
+// A CTA takes 128 x 128 elements, read once: a warp holds 16 whole rows of the tile, four neighbouring columns a lane,
+// so a row's largest magnitude is one reduction over the warp and its 128 bytes go out in one store.  For the transpose
+// the tile passes through shared memory: row r is kept in place (r % 4) * 32 + r / 4, so that a lane that wants rows
+// 4 l .. 4 l + 3 (the four bytes of a transposed row it writes) reads, with the whole warp, neighbouring places.
+// VEC: rows are aligned to four elements.
+template <typename T, bool SQUARE, bool VEC>
+__global__ void __launch_bounds__(kQuantThreads) k_quantize(const __grid_constant__ QuantParams p) {
+    extern __shared__ __align__(16) unsigned char dyn[];
+    __shared__ unsigned warp_max[kQuantWarps];
+    T* const tile = reinterpret_cast<T*>(dyn);
     pdl_trigger();
     pdl_wait();
-    const long long r0 = (long long)blockIdx.y * 128, c0 = (long long)blockIdx.x * 128;
-    const int nr = (int)(p.rows - r0 < 128 ? p.rows - r0 : 128), nc = (int)(p.cols - c0 < 128 ? p.cols - c0 : 128);
+    const int col_tiles = (int)((p.cols + 127) >> 7);
+    const long long rb = blockIdx.x / col_tiles, cb = blockIdx.x - rb * col_tiles, r0 = rb * 128, c0 = cb * 128;
+    const int nr = (int)min(p.rows - r0, 128ll), nc = (int)min(p.cols - c0, 128ll);
     const int lane = lane_id(), warp = warp_id();
-    constexpr int kWarps = kQuantThreads / 32;
-    const T* x = static_cast<const T*>(p.x);
-    unsigned top = 0;
-    for (int r = warp; r < 128; r += kWarps)
+    const T* const x = static_cast<const T*>(p.x) + r0 * p.ldx + c0 + lane * 4;
+    Four<T> v[kQuantRows];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = j * 32 + lane;
-            const float v = r < nr && c < nc ? to_float(x[(r0 + r) * p.ldx + c0 + c]) : 0.f;
-            tile[r * 129 + c] = v;
-            top = max(top, abs_bits(v));
+    for (int i = 0; i < kQuantRows; ++i) {
+        const int r = i * kQuantWarps + warp;
+        v[i].clear();
+        if (r < nr) {
+            if (VEC && lane * 4 + 4 <= nc) v[i].v = __ldcs(reinterpret_cast<const decltype(v[i].v)*>(x + r * p.ldx));
+            else
+                for (int j = 0; j < 4; ++j) if (lane * 4 + j < nc) v[i].set(j, x[r * p.ldx + j]);
         }
-    float square = 0.f;
+    }
+    unsigned square = 0;
     if (SQUARE) {
+        unsigned top = 0;
+#pragma unroll
+        for (int i = 0; i < kQuantRows; ++i) top = max(top, v[i].amax());
         top = __reduce_max_sync(0xFFFFFFFFu, top);
         if (lane == 0) warp_max[warp] = top;
     }
-    __syncthreads();
-    if (SQUARE) {
-        for (int w = 0; w < kWarps; ++w) top = max(top, warp_max[w]);
-        square = block_scale(top);
-        if (threadIdx.x == 0) {
-            if (p.q.q) p.q.scale[(long long)blockIdx.x * p.q.ld_scale + blockIdx.y] = square;
-            if (p.qt.q) p.qt.scale[(long long)blockIdx.y * p.qt.ld_scale + blockIdx.x] = square;
+    if (p.qt.q) {
+#pragma unroll
+        for (int i = 0; i < kQuantRows; ++i) {
+            const int r = i * kQuantWarps + warp;
+            *reinterpret_cast<decltype(v[i].v)*>(tile + ((r & 3) * 32 + (r >> 2)) * kQuantPitch + lane * 4) = v[i].v;
         }
     }
-    if (p.q.q)
-        for (int r = warp; r < nr; r += kWarps) {
-            float v[4];
-            unsigned m = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { v[j] = tile[r * 129 + lane * 4 + j]; m = max(m, abs_bits(v[j])); }
-            float s = square;
-            if (!SQUARE) {
-                s = block_scale(__reduce_max_sync(0xFFFFFFFFu, m));
-                if (lane == 0) p.q.scale[(long long)blockIdx.x * p.q.ld_scale + r0 + r] = s;
-            }
-            const float u = block_unscale(s);
-            if (lane * 4 < nc)
-                *reinterpret_cast<unsigned*>(p.q.q + (r0 + r) * p.q.ld + c0 + lane * 4) = to_e4m3x4(v[0] * u, v[1] * u, v[2] * u, v[3] * u);
+    if (SQUARE || p.qt.q) __syncthreads();
+    if (SQUARE) {
+        unsigned top = 0;
+        for (int w = 0; w < kQuantWarps; ++w) top = max(top, warp_max[w]);
+        square = block_exponent(top);
+        if (threadIdx.x < 128) {                            // every row's byte, as the product wants it
+            if (p.q.q) *scale_byte(p.q, r0 + threadIdx.x, cb) = (uint8_t)square;
+            if (p.qt.q) *scale_byte(p.qt, c0 + threadIdx.x, rb) = (uint8_t)square;
         }
-    if (p.qt.q)
-        for (int c = warp; c < nc; c += kWarps) {
-            float v[4];
-            unsigned m = 0;
+    }
+    if (p.q.q) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { v[j] = tile[(lane * 4 + j) * 129 + c]; m = max(m, abs_bits(v[j])); }
-            float s = square;
+        for (int i = 0; i < kQuantRows; ++i) {
+            const int r = i * kQuantWarps + warp;
+            if (r >= nr) break;
+            unsigned e = square;
             if (!SQUARE) {
-                s = block_scale(__reduce_max_sync(0xFFFFFFFFu, m));
-                if (lane == 0) p.qt.scale[(long long)blockIdx.y * p.qt.ld_scale + c0 + c] = s;
+                e = block_exponent(__reduce_max_sync(0xFFFFFFFFu, v[i].amax()));
+                if (lane == 0) *scale_byte(p.q, r0 + r, cb) = (uint8_t)e;
             }
-            const float u = block_unscale(s);
-            if (lane * 4 < nr)
-                *reinterpret_cast<unsigned*>(p.qt.q + (c0 + c) * p.qt.ld + r0 + lane * 4) = to_e4m3x4(v[0] * u, v[1] * u, v[2] * u, v[3] * u);
+            const float u = block_unscale(e);
+            if (lane * 4 < nc)                              // (up to three bytes of a row's padding are written too)
+                *reinterpret_cast<unsigned*>(p.q.q + (r0 + r) * p.q.ld + c0 + lane * 4) =
+                    to_e4m3x4(v[i].get(0) * u, v[i].get(1) * u, v[i].get(2) * u, v[i].get(3) * u);
         }
+    }
+    if (p.qt.q) {
+#pragma unroll
+        for (int k = 0; k < 32 / kQuantWarps; ++k) {
+            const int c = (k * kQuantWarps + warp) * 4;      // four columns, rows 4 lane .. 4 lane + 3
+            if (c >= nc) break;
+            Four<T> w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j].v = *reinterpret_cast<const decltype(w[j].v)*>(tile + (j * 32 + lane) * kQuantPitch + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (c + i >= nc) break;
+                const float a0 = w[0].get(i), a1 = w[1].get(i), a2 = w[2].get(i), a3 = w[3].get(i);
+                unsigned e = square;
+                if (!SQUARE) {
+                    const unsigned m = 0x7FFFFFFFu;
+                    const unsigned top = max(max(__float_as_uint(a0) & m, __float_as_uint(a1) & m), max(__float_as_uint(a2) & m, __float_as_uint(a3) & m));
+                    e = block_exponent(__reduce_max_sync(0xFFFFFFFFu, top));
+                    if (lane == 0) *scale_byte(p.qt, c0 + c + i, rb) = (uint8_t)e;
+                }
+                const float u = block_unscale(e);
+                if (lane * 4 < nr)
+                    *reinterpret_cast<unsigned*>(p.qt.q + (c0 + c + i) * p.qt.ld + r0 + lane * 4) = to_e4m3x4(a0 * u, a1 * u, a2 * u, a3 * u);
+            }
+        }
+    }
 }
 
-template <typename T, bool SQUARE>
-static cudaError_t quantize_t(const QuantParams& p, cudaStream_t stream) {
+template <typename T, bool SQUARE, bool VEC>
+static cudaError_t quantize_v(const QuantParams& p, cudaStream_t stream) {
     static SmemOptIn opt;
-    const size_t smem = 128 * 129 * sizeof(float);
-    const cudaError_t e = ensure_dynamic_smem(k_quantize_tile<T, SQUARE>, smem, opt);
+    const size_t smem = p.qt.q ? 128 * kQuantPitch * sizeof(T) : 0;
+    const cudaError_t e = ensure_dynamic_smem(k_quantize<T, SQUARE, VEC>, smem, opt);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)((p.cols + 127) / 128), (unsigned)((p.rows + 127) / 128));
-    return launch_pdl(k_quantize_tile<T, SQUARE>, grid, dim3(kQuantThreads), smem, stream, p);
+    const long long tiles = ((p.cols + 127) / 128) * ((p.rows + 127) / 128);
+    return launch_pdl(k_quantize<T, SQUARE, VEC>, dim3((unsigned)tiles), dim3(kQuantThreads), smem, stream, p);
 }
-
-cudaError_t launch_quantize(const QuantParams& p, int x_type, int, cudaStream_t stream) {
-    const bool square = (p.q.q ? p.q.shift : p.qt.shift) != 0;
-    if (x_type == DST_F32) return square ? quantize_t<float, true>(p, stream) : quantize_t<float, false>(p, stream);
-    return square ? quantize_t<__nv_bfloat16, true>(p, stream) : quantize_t<__nv_bfloat16, false>(p, stream);
+template <typename T>
+static cudaError_t quantize_t(const QuantParams& p, cudaStream_t stream) {
+    const bool square = p.q.q ? p.q.square : p.qt.square;
+    const bool vec = (reinterpret_cast<uintptr_t>(p.x) & (4 * sizeof(T) - 1)) == 0 && p.ldx % 4 == 0;
+    if (square) return vec ? quantize_v<T, true, true>(p, stream) : quantize_v<T, true, false>(p, stream);
+    return vec ? quantize_v<T, false, true>(p, stream) : quantize_v<T, false, false>(p, stream);
+}
+cudaError_t launch_quantize(const QuantParams& p, int x_type, cudaStream_t stream) {
+    return x_type == DST_F32 ? quantize_t<float>(p, stream) : quantize_t<__nv_bfloat16>(p, stream);
 }
 
 // ---- product ----------------------------------------------------------------------
-// D[p, q] = sum over blocks b of sp[b, p] sq[b, q] (P_b Q_b^T): a block's 128 products are summed by the tensor cores
-// into tensor memory, then epilogue warps take the partial tile out, scale it and add it to fp32 sums in registers,
-// while the tensor cores fill the other of two tensor-memory buffers with the next block.  P is the operand whose rows
-// are the 128 lanes of tensor memory, Q the one whose rows are its columns.
+// D[p, q] = sum over blocks b of sp[b, p] sq[b, q] (P_b Q_b^T).  The scales are powers of two in the form the tensor
+// cores multiply by themselves (one scale for 32 elements of the inner dimension; the four steps of a block use the same
+// byte), so the whole sum stays in tensor memory and the epilogue sees a finished tile (fp32 sums:
+// 1.3e-7 relative for random signs over 33,708 terms, 5e-7 where all terms are positive).  P is the operand whose rows are
+// the 128 lanes of tensor memory, Q the one whose rows are its columns.
 //
 // Both sides large: two CTAs share a 256 x 256 tile (each holds 128 rows of P, half of Q's rows, and 128 x 256 of
 // the result), which halves what an SM has to fetch for a block against a tile of its own: 32 KB where the tensor
@@ -140,19 +203,21 @@ struct TileShape {
     static constexpr int kCols = NT > 128 ? 128 : NT;     // columns of the result an epilogue warp holds
     static constexpr int kThreads = (kEpiWarps + 2) * 32;
     static constexpr int kStageBytes = (kTileP + kQRows) * kBlockK;
+    static constexpr int kQScaleTiles = (NT + 127) / 128;
+    static constexpr int kScaleBytes = (1 + kQScaleTiles) * kScaleTile;   // of four blocks
     static constexpr int kOutBytes = kEpiWarps * 4096;    // 32 x 32 words a warp, for turning rows into runs
-    static constexpr int kHeaderBytes = 3072;
-    static constexpr int kFit = (kSmemMost - kOutBytes - kHeaderBytes) / kStageBytes;
+    static constexpr int kHeaderBytes = 1024;
+    static constexpr int kFit = (kSmemMost - kOutBytes - kHeaderBytes) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kFit < 8 ? kFit : 8;
-    static constexpr int kSmem = kStages * kStageBytes + kOutBytes + kHeaderBytes;
-    static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+    static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kOutBytes + kHeaderBytes;
+    // tensor memory: one or two results, then a ring of scales (P's four columns, then Q's; four groups of four blocks)
+    static constexpr int kBufs = NT > 128 ? 1 : 2;
+    static constexpr int kScaleCols = 4 * (1 + kQScaleTiles), kScaleRing = 4;
+    static constexpr int kUsedCols = kBufs * NT + kScaleRing * kScaleCols;
+    static constexpr int kTmemCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
 };
 
 struct MatmulParams {
-    const float* sp;
-    const float* sq;
-    long long ld_sp, ld_sq;                               // scales of a block
-    int shift_p, shift_q;                                 // 7: a scale for 128 rows
     int rows_p, rows_q;
     int blocks, splits;                                   // blocks of the inner dimension, parts it is cut into
     int tiles_p, tiles_q;
@@ -166,7 +231,7 @@ __device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
 // (what is handed over here is tensor memory, ordered by the tcgen05 fences around it; a release at cluster scope would
-// wait for all of the thread's memory traffic: 935 -> ... )
+// wait for all of the thread's memory traffic)
 __device__ __forceinline__ void bar_arrive_cluster(unsigned bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
     unsigned done;
@@ -196,13 +261,28 @@ __device__ __forceinline__ void copy_tile(unsigned dst, const CUtensorMap* map, 
                      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 template <int CG>
-__device__ __forceinline__ void mma_fp8(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate) {
+__device__ __forceinline__ void copy_scales(unsigned dst, const CUtensorMap* map, int group, int tile, unsigned bar) {
     if (CG == 2)
-        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p; }"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(0), "r"(group), "r"(tile), "r"(bar) : "memory");
     else
-        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p; }"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(0), "r"(group), "r"(tile), "r"(bar) : "memory");
+}
+// 32 rows of 16 bytes from shared memory to four columns of tensor memory, the same in all four quarters of its lanes
+template <int CG>
+__device__ __forceinline__ void tmem_copy_scales(unsigned d, uint64_t desc) {
+    if (CG == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(d), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d), "l"(desc) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma_fp8(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned scale_a, unsigned scale_b, unsigned accumulate) {
+    if (CG == 2)
+        asm volatile("{ .reg .pred p; setp.ne.b32 p, %6, 0; tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p; }"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
+    else
+        asm volatile("{ .reg .pred p; setp.ne.b32 p, %6, 0; tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p; }"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
 }
 // arrives at `bar` (CG == 2: at that place in both CTAs) once the matrix instructions issued so far are done
 template <int CG>
@@ -228,15 +308,13 @@ __device__ __forceinline__ void tmem_wait(float (&v)[16]) {
                    "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
                  :: "memory");
 }
-// two sums at once: the packed form has the same roundings and half the instructions
-__device__ __forceinline__ void fma2(float& a0, float& a1, float x0, float x1, float s0, float s1) {
-    asm("{ .reg .b64 a, x, s; mov.b64 a, {%0, %1}; mov.b64 x, {%2, %3}; mov.b64 s, {%4, %5}; fma.rn.f32x2 a, x, s, a; mov.b64 {%0, %1}, a; }"
-        : "+f"(a0), "+f"(a1) : "f"(x0), "f"(x1), "f"(s0), "f"(s1));
-}
-
 // Shared-memory operand: rows of 128 bytes, 128-byte swizzle in groups of eight rows (1024 bytes apart)
 __device__ __forceinline__ uint64_t operand_desc(unsigned addr) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// scales: 32 rows of 16 bytes, one after another
+__device__ __forceinline__ uint64_t scale_desc(unsigned addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
 // The columns [c0, c0 + kCols) of a warp's 32 rows, from one row a lane to runs of consecutive columns.
@@ -284,16 +362,18 @@ __device__ __forceinline__ void store_swapped(const MatmulParams& p, OT* out, co
         if (col0 + c < p.rows_q) out[(long long)(col0 + c) * p.ldo + row] = from_float<OT>(acc[c]);
 }
 
-template <int CG, int NT, bool QVEC, typename OT>
+template <int CG, int NT, typename OT>
 __global__ void __launch_bounds__(TileShape<CG, NT>::kThreads, 1)
-k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ MatmulParams p) {
+k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
+             const __grid_constant__ CUtensorMap map_sq, const __grid_constant__ MatmulParams p) {
     using S = TileShape<CG, NT>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    unsigned char* const header = smem + S::kStages * S::kStageBytes + S::kOutBytes;
-    float* const scales = reinterpret_cast<float*>(header);                       // QVEC: [warps / 4][2][128]
-    unsigned* const tmem_slot = reinterpret_cast<unsigned*>(header + 2048);
-    const unsigned bars = smem_addr(header + 2064);
-    const unsigned full = bars, empty = bars + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 16;
+    unsigned char* const scale_ring = smem + S::kStages * S::kStageBytes;
+    unsigned char* const out_words = scale_ring + S::kStages * S::kScaleBytes;
+    unsigned char* const header = out_words + S::kOutBytes;
+    unsigned* const tmem_slot = reinterpret_cast<unsigned*>(header);
+    const unsigned bars = smem_addr(header + 16);
+    const unsigned full = bars, empty = bars + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 8 * S::kBufs;
     const int warp = warp_id(), lane = lane_id();
     const unsigned rank = CG == 2 ? (unsigned)(blockIdx.x & 1) : 0u;               // of the pair; 0 issues for both
     const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
@@ -301,7 +381,7 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) { bar_init(full + 8 * i, 1); bar_init(empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(tmem_full + 8 * i, 1); bar_init(tmem_empty + 8 * i, CG * S::kEpiWarps); }
+        for (int i = 0; i < S::kBufs; ++i) { bar_init(tmem_full + 8 * i, 1); bar_init(tmem_empty + 8 * i, CG * S::kEpiWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -320,123 +400,119 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     const unsigned tmem = *tmem_slot;
     pdl_wait();
 
-    const int tiles = p.tiles_p * p.tiles_q, items = tiles * p.splits;
-    // an item's tile and part; the side with fewer tiles moves fastest, so that CTAs at work together share the other's rows
+    const int tiles = p.tiles_p * p.tiles_q, items = tiles * p.splits, groups = (p.blocks + 3) >> 2;
+    // an item's tile and part (whole groups of four blocks); the side with fewer tiles moves fastest, so that CTAs at work
+    // together share the other's rows
     auto item_of = [&](int item, int& tp, int& tq, int& k0, int& k1) {
         const int part = item / tiles, tile = item - part * tiles;
         if (p.tiles_p <= p.tiles_q) { tq = tile / p.tiles_p; tp = tile - tq * p.tiles_p; }
         else { tp = tile / p.tiles_q; tq = tile - tp * p.tiles_q; }
-        k0 = (int)((long long)p.blocks * part / p.splits);
-        k1 = (int)((long long)p.blocks * (part + 1) / p.splits);
+        k0 = (int)((long long)groups * part / p.splits) * 4;
+        k1 = min((int)((long long)groups * (part + 1) / p.splits) * 4, p.blocks);
         return part;
     };
     bool ok = true;
 
     if (warp == S::kEpiWarps) {                                                    // ---- copies ----
         if (lane == 0) {
-            const unsigned stages = smem_addr(smem);
-            int n = 0;
+            const unsigned stages = smem_addr(smem), ring = smem_addr(scale_ring);
+            const unsigned first_full = CG == 2 ? in_cta(full, 0) : full;          // the issuing CTA waits for both CTAs' copies
+            int s = 0, used = 0;
+            unsigned phase = 1;                                                    // every stage is free at first
             for (int item = worker; item < items && ok; item += workers) {
                 int tp, tq, k0, k1;
                 item_of(item, tp, tq, k0, k1);
-                for (int b = k0; b < k1; ++b, ++n) {
-                    const int s = n % S::kStages;
-                    ok = bar_wait(empty + 8 * s, ((n / S::kStages) & 1) ^ 1);
+                for (int b = k0; b < k1; ++b) {
+                    ok = bar_wait(empty + 8 * s, phase);
                     if (!ok) break;
-                    const unsigned bar = CG == 2 ? in_cta(full + 8 * s, 0) : full + 8 * s;
-                    if (rank == 0) bar_expect(full + 8 * s, CG * S::kStageBytes);
-                    const unsigned at = stages + s * S::kStageBytes;
+                    const unsigned bar = first_full + 8 * s;
+                    const bool scales = (b & 3) == 0;
+                    if (rank == 0) bar_expect(full + 8 * s, CG * (S::kStageBytes + (scales ? S::kScaleBytes : 0)));
+                    const unsigned at = stages + s * S::kStageBytes, sc = ring + s * S::kScaleBytes;
                     copy_tile<CG>(at, &map_p, b * kBlockK, (tp * CG + (int)rank) * kTileP, bar);
                     copy_tile<CG>(at + kTileP * kBlockK, &map_q, b * kBlockK, tq * NT + (int)rank * S::kQRows, bar);
+                    if (scales) {                                                  // all of Q's for both CTAs: each has every column
+                        copy_scales<CG>(sc, &map_sp, b >> 2, tp * CG + (int)rank, bar);
+                        for (int i = 0; i < S::kQScaleTiles; ++i) copy_scales<CG>(sc + (1 + i) * kScaleTile, &map_sq, b >> 2, tq * S::kQScaleTiles + i, bar);
+                    }
+                    used = min(used + 1, S::kStages);
+                    if (++s == S::kStages) { s = 0; phase ^= 1; }
                 }
             }
-            // the last arrivals at this CTA's barriers come before it ends
-            for (int i = n > S::kStages ? n - S::kStages : 0; i < n && ok; ++i) ok = bar_wait(empty + 8 * (i % S::kStages), (i / S::kStages) & 1);
+            // the last arrivals at this CTA's barriers come before it ends: each stage in use becomes free once more
+            for (int i = 0; i < used && ok; ++i) {
+                ok = bar_wait(empty + 8 * (used < S::kStages ? i : s), used < S::kStages ? 0u : phase);
+                if (used == S::kStages && ++s == S::kStages) { s = 0; phase ^= 1; }
+            }
         }
     } else if (warp == S::kEpiWarps + 1) {                                         // ---- matrix instructions ----
         if (lane == 0 && rank == 0) {
-            // fp32 results, both operands e4m3 with the inner dimension contiguous, N and M of the instruction
-            constexpr unsigned idesc = 1u << 4 | (unsigned)(NT >> 3) << 17 | (unsigned)((kTileP * CG) >> 4) << 24;
-            const unsigned stages = smem_addr(smem);
-            int n = 0;
+            // both operands e4m3 with the inner dimension contiguous, N and M of the instruction, scales as exponents
+            constexpr unsigned idesc = (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)((kTileP * CG) >> 4) << 24;
+            // The instruction queue is shallow: whatever this thread does between two blocks beyond two instructions' time
+            // leaves the tensor cores idle, so the loop counts and never divides.
+            const uint64_t operands = operand_desc(smem_addr(smem)), scales = scale_desc(smem_addr(scale_ring));
+            int s = 0, buf = 0, slot = 0;
+            unsigned phase = 0, buf_phase = 1;
             for (int item = worker; item < items && ok; item += workers) {
                 int tp, tq, k0, k1;
                 item_of(item, tp, tq, k0, k1);
-                for (int b = k0; b < k1; ++b, ++n) {
-                    const int s = n % S::kStages, buf = n & 1;
-                    ok = bar_wait(tmem_empty + 8 * buf, ((n >> 1) & 1) ^ 1) && bar_wait(full + 8 * s, (n / S::kStages) & 1);
+                ok = bar_wait(tmem_empty + 8 * buf, buf_phase);
+                const unsigned d = tmem + buf * NT;
+                unsigned sc = 0;
+                for (int b = k0; b < k1 && ok; ++b) {
+                    ok = bar_wait(full + 8 * s, phase);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_desc(stages + s * S::kStageBytes), q = operand_desc(stages + s * S::kStageBytes + kTileP * kBlockK);
+                    if ((b & 3) == 0) {
+                        sc = tmem + S::kBufs * NT + slot * S::kScaleCols;
+                        slot = (slot + 1) & (S::kScaleRing - 1);
+#pragma unroll
+                        for (int i = 0; i < 1 + S::kQScaleTiles; ++i) tmem_copy_scales<CG>(sc + 4 * i, scales + ((s * S::kScaleBytes + i * kScaleTile) >> 4));
+                    }
+                    const uint64_t a = operands + ((s * S::kStageBytes) >> 4), q = a + ((kTileP * kBlockK) >> 4);
+                    const unsigned id = idesc | (unsigned)(b & 3) << 4 | (unsigned)(b & 3) << 29;   // which of the four bytes
 #pragma unroll
                     for (int k = 0; k < kBlockK / 32; ++k)                          // 32 bytes of the inner dimension each
-                        mma_fp8<CG>(tmem + buf * NT, a + 2 * k, q + 2 * k, idesc, k > 0);
+                        mma_fp8<CG>(d, a + 2 * k, q + 2 * k, id, sc, sc + 4, b > k0 || k > 0);
                     mma_commit<CG>(empty + 8 * s);
-                    mma_commit<CG>(tmem_full + 8 * buf);
+                    if (++s == S::kStages) { s = 0; phase ^= 1; }
                 }
+                if (ok) mma_commit<CG>(tmem_full + 8 * buf);
+                if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
             }
         }
     } else {                                                                       // ---- epilogue ----
         const int group = warp >> 2, quarter = warp & 3;                           // a warp reaches the 32 lanes of its quarter
         const unsigned mine = tmem + ((unsigned)(quarter * 32) << 16) + group * 128;
-        unsigned* const words = reinterpret_cast<unsigned*>(smem + S::kStages * S::kStageBytes + warp * 4096);
+        unsigned* const words = reinterpret_cast<unsigned*>(out_words + warp * 4096);
         const unsigned free_bar = in_cta(tmem_empty, 0);
-        int n = 0;
+        int buf = 0;
+        unsigned buf_phase = 0;
         for (int item = worker; item < items; item += workers) {
             int tp, tq, k0, k1;
             const int part = item_of(item, tp, tq, k0, k1);
-            const int row0 = (tp * CG + (int)rank) * kTileP + quarter * 32, row = row0 + lane, col0 = tq * NT + group * 128;
-            const float* sp = p.sp + (min(row, p.rows_p - 1) >> p.shift_p);
-            const int my_col = QVEC ? min(col0 + (int)(threadIdx.x & 127), p.rows_q - 1) : min(col0, p.rows_q - 1);
-            const float* sq = p.sq + (my_col >> p.shift_q);
-            float next_p = sp[k0 * p.ld_sp], next_q = sq[k0 * p.ld_sq];
+            const int row0 = (tp * CG + (int)rank) * kTileP + quarter * 32, col0 = tq * NT + group * 128;
             float acc[S::kCols];
+            if (ok) ok = bar_wait(tmem_full + 8 * buf, buf_phase);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (ok) {
 #pragma unroll
-            for (int i = 0; i < S::kCols; ++i) acc[i] = 0.f;
-            for (int b = k0; b < k1; ++b, ++n) {
-                const int buf = n & 1;
-                const float scale = QVEC ? next_p : next_p * next_q;
-                float* const vec = scales + (group * 2 + buf) * 128;
-                if (QVEC) {
-                    vec[threadIdx.x & 127] = next_q;
-                    asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory");
-                }
-                if (b + 1 < k1) { next_p = sp[(b + 1) * p.ld_sp]; next_q = sq[(b + 1) * p.ld_sq]; }
-                if (ok) ok = bar_wait(tmem_full + 8 * buf, (n >> 1) & 1);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) continue;                                                 // (bar.sync above stays matched)
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                float v[2][16];
-                tmem_load16(mine + buf * NT, v[0]);
+                for (int c = 0; c < S::kCols; c += 16) tmem_load16(mine + buf * NT + c, *reinterpret_cast<float (*)[16]>(acc + c));
 #pragma unroll
-                for (int c = 0; c < S::kCols; c += 16) {
-                    float (&x)[16] = v[(c >> 4) & 1];
-                    tmem_wait(x);
-                    if (c + 16 < S::kCols) tmem_load16(mine + buf * NT + c + 16, v[((c >> 4) & 1) ^ 1]);
-                    else {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) bar_arrive_cluster(free_bar + 8 * buf);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        if (QVEC) {
-                            const float4 q = *reinterpret_cast<const float4*>(vec + c + i);
-                            fma2(acc[c + i], acc[c + i + 1], x[i], x[i + 1], scale * q.x, scale * q.y);
-                            fma2(acc[c + i + 2], acc[c + i + 3], x[i + 2], x[i + 3], scale * q.z, scale * q.w);
-                        } else {
-                            fma2(acc[c + i], acc[c + i + 1], x[i], x[i + 1], scale, scale);
-                            fma2(acc[c + i + 2], acc[c + i + 3], x[i + 2], x[i + 3], scale, scale);
-                        }
-                    }
-                }
+                for (int c = 0; c < S::kCols; c += 16) tmem_wait(*reinterpret_cast<float (*)[16]>(acc + c));
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(free_bar + 8 * buf);              // the next tile's sums may start
             }
+            if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
             if (!ok) {
 #pragma unroll
                 for (int i = 0; i < S::kCols; ++i) acc[i] = __uint_as_float(0x7FC00000u);
             }
             OT* const out = static_cast<OT*>(p.out) + part * p.split_stride;
-            if (p.swap) store_swapped<OT, S::kCols>(p, out, acc, row, col0);
+            if (p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
             else if (row0 < p.rows_p) store_rows<OT, S::kCols>(p, out, acc, words, row0, col0);
         }
     }
@@ -470,6 +546,7 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ pa
 
 // How a product is cut: which side is Q, its tile, and the parts of the inner dimension.
 constexpr int kMaxParts = 32;
+
 struct MatmulPlan { int cg, nt, swap; long long rows_p, rows_q, tiles_p, tiles_q, blocks; int splits; };
 static MatmulPlan plan_matmul(long long M, long long N, long long K) {
     MatmulPlan L{};
@@ -481,14 +558,15 @@ static MatmulPlan plan_matmul(long long M, long long N, long long K) {
     L.tiles_p = (L.rows_p + kTileP * L.cg - 1) / (kTileP * L.cg);
     L.tiles_q = (L.rows_q + L.nt - 1) / L.nt;
     L.blocks = (K + kBlockK - 1) / kBlockK;
-    // Parts: the fewest microseconds by a model of 0.3 a block, 1 a tile, and for more than one part their results written
+    const long long groups = (L.blocks + 3) / 4;
+    // Parts, of whole groups of four blocks: the fewest microseconds by a model of 0.3 a block, 1 a tile, and for more than one part their results written
     // and read again at 4 TB/s and another launch.  SMs of a B200, not the device's, so that the order of the sums
     // follows from the sizes.
     const long long tiles = L.tiles_p * L.tiles_q, workers = kSmCount / L.cg;
     double best = 0;
-    for (int s = 1; s <= kMaxParts && s <= L.blocks; ++s) {
+    for (int s = 1; s <= kMaxParts && s <= groups; ++s) {
         if (s > 1 && tiles * s > 2 * workers) break;
-        const long long rounds = (tiles * s + workers - 1) / workers, len = (L.blocks + s - 1) / s;
+        const long long rounds = (tiles * s + workers - 1) / workers, len = (groups + s - 1) / s * 4;
         const double us = rounds * (len * 0.3 + 1.0) + (s > 1 ? 3.0 + double(s) * M * N * 8 / 4e6 : 0.0);
         if (s == 1 || us < best) { best = us; L.splits = s; }
     }
@@ -501,9 +579,9 @@ size_t matmul_fp8_workspace(long long M, long long N, long long K) {
 }
 // What no product up to these sizes exceeds: parts x tiles stay within two for each SM (or pair of them).
 size_t matmul_fp8_workspace_bound(long long M, long long N, long long K) {
-    const long long blocks = (K + kBlockK - 1) / kBlockK;
-    if (blocks < 2) return 0;
-    const size_t every = size_t(blocks < kMaxParts ? blocks : kMaxParts) * size_t(M) * size_t(N) * 4;
+    const long long groups = (K + 4 * kBlockK - 1) / (4 * kBlockK);
+    if (groups < 2) return 0;
+    const size_t every = size_t(groups < kMaxParts ? groups : kMaxParts) * size_t(M) * size_t(N) * 4;
     const size_t pairs = size_t(kSmCount) * 256 * 256 * 4;
     return every < pairs ? every : pairs;
 }
@@ -530,11 +608,23 @@ static bool operand_map(CUtensorMap& map, const Fp8View& m, int rows) {
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, int NT, bool QVEC, typename OT>
-static cudaError_t matmul_launch(const CUtensorMap& mp, const CUtensorMap& mq, const MatmulParams& p, int sms, cudaStream_t stream) {
+// The scales as [128 rows' tiles][groups of four blocks][128 words], a tile a copy.
+static bool scale_map(CUtensorMap& map, const Fp8View& m) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {kScaleTile / 4, (cuuint64_t)((m.cols + 511) / 512), (cuuint64_t)((m.rows + 127) / 128)};
+    const cuuint64_t strides[2] = {kScaleTile, (cuuint64_t)m.ld_scale * kScaleTile};
+    const cuuint32_t box[3] = {kScaleTile / 4, 1, 1}, step[3] = {1, 1, 1};
+    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, m.scale, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct MatmulMaps { CUtensorMap p, q, sp, sq; };
+template <int CG, int NT, typename OT>
+static cudaError_t matmul_launch(const MatmulMaps& m, const MatmulParams& p, int sms, cudaStream_t stream) {
     using S = TileShape<CG, NT>;
     static SmemOptIn opt;
-    const cudaError_t e = ensure_dynamic_smem(k_matmul_fp8<CG, NT, QVEC, OT>, S::kSmem, opt);
+    const cudaError_t e = ensure_dynamic_smem(k_matmul_fp8<CG, NT, OT>, S::kSmem, opt);
     if (e != cudaSuccess) return e;
     const long long items = (long long)p.tiles_p * p.tiles_q * p.splits, workers = sms / CG;
     cudaLaunchConfig_t cfg = {};
@@ -546,31 +636,28 @@ static cudaError_t matmul_launch(const CUtensorMap& mp, const CUtensorMap& mq, c
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_matmul_fp8<CG, NT, QVEC, OT>, mp, mq, p);
+    return cudaLaunchKernelEx(&cfg, k_matmul_fp8<CG, NT, OT>, m.p, m.q, m.sp, m.sq, p);
 }
 template <int CG, int NT>
-static cudaError_t matmul_nt(const CUtensorMap& mp, const CUtensorMap& mq, const MatmulParams& p, int out_type, int sms, cudaStream_t stream) {
-    if (p.shift_q == 0)
-        return out_type == DST_F32 ? matmul_launch<CG, NT, true, float>(mp, mq, p, sms, stream) : matmul_launch<CG, NT, true, __nv_bfloat16>(mp, mq, p, sms, stream);
-    return out_type == DST_F32 ? matmul_launch<CG, NT, false, float>(mp, mq, p, sms, stream) : matmul_launch<CG, NT, false, __nv_bfloat16>(mp, mq, p, sms, stream);
+static cudaError_t matmul_nt(const MatmulMaps& m, const MatmulParams& p, int out_type, int sms, cudaStream_t stream) {
+    return out_type == DST_F32 ? matmul_launch<CG, NT, float>(m, p, sms, stream) : matmul_launch<CG, NT, __nv_bfloat16>(m, p, sms, stream);
 }
 
 cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace, int sms, cudaStream_t stream) {
     const MatmulPlan L = plan_matmul(a.rows, b.rows, a.cols);
     const Fp8View &vp = L.swap ? b : a, &vq = L.swap ? a : b;
-    CUtensorMap mp, mq;
-    if (!operand_map(mp, vp, kTileP) || !operand_map(mq, vq, L.nt / L.cg)) return cudaErrorInvalidValue;
-    MatmulParams p{vp.scale, vq.scale, vp.ld_scale, vq.ld_scale, vp.shift, vq.shift, (int)vp.rows, (int)vq.rows, (int)L.blocks, L.splits,
-                   (int)L.tiles_p, (int)L.tiles_q, L.swap, out, ldo, 0};
+    MatmulMaps m;
+    if (!operand_map(m.p, vp, kTileP) || !operand_map(m.q, vq, L.nt / L.cg) || !scale_map(m.sp, vp) || !scale_map(m.sq, vq)) return cudaErrorInvalidValue;
+    MatmulParams p{(int)vp.rows, (int)vq.rows, (int)L.blocks, L.splits, (int)L.tiles_p, (int)L.tiles_q, L.swap, out, ldo, 0};
     int type = out_type;
     if (L.splits > 1) { p.out = workspace; p.ldo = b.rows; p.split_stride = a.rows * b.rows; type = DST_F32; }
     cudaError_t e;
     switch (L.nt) {
-        case 16: e = matmul_nt<1, 16>(mp, mq, p, type, sms, stream); break;
-        case 32: e = matmul_nt<1, 32>(mp, mq, p, type, sms, stream); break;
-        case 64: e = matmul_nt<1, 64>(mp, mq, p, type, sms, stream); break;
-        case 128: e = matmul_nt<1, 128>(mp, mq, p, type, sms, stream); break;
-        default: e = matmul_nt<2, 256>(mp, mq, p, type, sms, stream); break;
+        case 16: e = matmul_nt<1, 16>(m, p, type, sms, stream); break;
+        case 32: e = matmul_nt<1, 32>(m, p, type, sms, stream); break;
+        case 64: e = matmul_nt<1, 64>(m, p, type, sms, stream); break;
+        case 128: e = matmul_nt<1, 128>(m, p, type, sms, stream); break;
+        default: e = matmul_nt<2, 256>(m, p, type, sms, stream); break;
     }
     if (e != cudaSuccess || L.splits == 1) return e;
     const long long total = a.rows * b.rows, blocks = (total + 255) / 256, cap = (long long)sms * 8;

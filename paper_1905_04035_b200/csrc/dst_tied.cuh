@@ -44,18 +44,19 @@ cudaError_t launch_dropout(const DropoutParams& p, int x_type, int out_type, int
 cudaError_t launch_embed(const EmbedParams& p, int index_type, int weight_type, int out_type, int sms, cudaStream_t stream);
 
 // ---- 8-bit floating point (dst_fp8.cu) --------------------------------------------
-struct Fp8View {                            // dst_fp8_t with the block shift of its rows: 0 (ROW) or 7 (SQUARE)
+struct Fp8View {                            // dst_fp8_t
     uint8_t* q;
-    float* scale;
+    uint8_t* scale;
     long long rows, cols, ld, ld_scale;
-    int shift;
+    int square;
 };
+constexpr int kScaleTile = 512;             // bytes of scales for 128 rows by 4 column blocks
 struct QuantParams {
     const void* x;
     long long ldx, rows, cols;
     Fp8View q, qt;                          // q.q / qt.q null: not wanted
 };
-cudaError_t launch_quantize(const QuantParams& p, int x_type, int sms, cudaStream_t stream);
+cudaError_t launch_quantize(const QuantParams& p, int x_type, cudaStream_t stream);
 size_t matmul_fp8_workspace(long long M, long long N, long long K);        // of this product
 size_t matmul_fp8_workspace_bound(long long M, long long N, long long K);  // of this one and every smaller one
 cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace,

@@ -37,10 +37,10 @@ static int fp8_view(const dst_fp8_t* m, Fp8View& v) {
     if (!m || m->rows < 0 || m->cols < 0 || m->ld < m->cols) return DST_ERR_INVALID_ARG;
     if (m->block != DST_FP8_ROW && m->block != DST_FP8_SQUARE) return DST_ERR_INVALID_ARG;
     if (m->rows > kMaxCols || m->cols > kMaxCols) return DST_ERR_UNSUPPORTED;
-    const int shift = m->block == DST_FP8_SQUARE ? 7 : 0;
-    if (m->ld % 16 != 0 || m->ld_scale < (shift ? (m->rows + 127) / 128 : m->rows)) return DST_ERR_INVALID_ARG;
-    if (m->rows > 0 && m->cols > 0 && (!m->q || !m->scale || misaligned(m->q, 16) || misaligned(m->scale, 4))) return DST_ERR_INVALID_ARG;
-    v = Fp8View{static_cast<uint8_t*>(m->q), m->scale, (long long)m->rows, (long long)m->cols, (long long)m->ld, (long long)m->ld_scale, shift};
+    if (m->ld % 16 != 0 || m->ld_scale < (m->cols + 511) / 512) return DST_ERR_INVALID_ARG;
+    if (m->rows > 0 && m->cols > 0 && (!m->q || !m->scale || misaligned(m->q, 16) || misaligned(m->scale, 16))) return DST_ERR_INVALID_ARG;
+    v = Fp8View{static_cast<uint8_t*>(m->q), static_cast<uint8_t*>(m->scale), (long long)m->rows, (long long)m->cols, (long long)m->ld,
+                (long long)m->ld_scale, m->block == DST_FP8_SQUARE};
     return DST_OK;
 }
 
@@ -71,9 +71,9 @@ struct LinearLayout { int64_t ld, ld_scale; size_t off_scale, off_matmul, total;
 static LinearLayout linear_layout(int64_t M, int64_t N, int64_t K) {
     LinearLayout L{};
     L.ld = (K + 15) / 16 * 16;
-    L.ld_scale = (M + 3) / 4 * 4;
+    L.ld_scale = (K + 511) / 512;
     L.off_scale = align_up(size_t(M) * size_t(L.ld), 256);
-    L.off_matmul = L.off_scale + align_up(size_t((K + 127) / 128) * size_t(L.ld_scale) * 4, 256);
+    L.off_matmul = L.off_scale + size_t((M + 127) / 128) * size_t(L.ld_scale) * kScaleTile;
     L.total = L.off_matmul + matmul_fp8_workspace_bound(M, N, K);
     return L;
 }
@@ -136,7 +136,7 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
         if (qt->rows != cols || qt->cols != rows || (q && qt->block != q->block)) return DST_ERR_INVALID_ARG;
     }
     if (rows == 0 || cols == 0) return DST_OK;
-    return done(launch_quantize(p, x_type, device_sm_count(), stream), 1);
+    return done(launch_quantize(p, x_type, stream), 1);
 }
 
 size_t dst_matmul_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
@@ -169,7 +169,7 @@ int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const 
         if (!workspace || misaligned(workspace, 256)) return DST_ERR_INVALID_ARG;
         if (workspace_bytes < L.off_matmul + matmul_fp8_workspace(M, w->rows, w->cols)) return DST_ERR_WORKSPACE_TOO_SMALL;
         a.q = workspace;
-        a.scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.off_scale);
+        a.scale = static_cast<char*>(workspace) + L.off_scale;
         const int rq = dst_quantize_fp8(x, ldx, x_type, M, w->cols, &a, nullptr, stream);
         if (rq != DST_OK) return rq;
     }

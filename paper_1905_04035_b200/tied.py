@@ -134,9 +134,9 @@ def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *,
 
 
 class Fp8Matrix:
-    """Owns a matrix [rows, cols] in 8-bit floating point (``dst_fp8_t``): ``q`` [rows, cols padded to 16] and one
-    scale for each block: 128 columns of a row (``DST_FP8_ROW``; ``scale`` [column blocks, rows padded]) or 128 x 128
-    (``DST_FP8_SQUARE``; ``scale`` [column blocks, row blocks])."""
+    """Owns a matrix [rows, cols] in 8-bit floating point (``dst_fp8_t``): ``q`` [rows, cols padded to 16] and a scale
+    (a power of two, as its exponent + 127) for each block of 128 columns of a row (``DST_FP8_ROW``) or 128 x 128
+    (``DST_FP8_SQUARE``), in ``scale`` [rows / 128, column blocks / 4, 512]."""
 
     def __init__(self, rows: int, cols: int, block: int = DST_FP8_ROW, *, device="cuda"):
         if block not in (DST_FP8_ROW, DST_FP8_SQUARE):
@@ -144,9 +144,8 @@ class Fp8Matrix:
         if rows < 0 or cols < 0:
             raise ValueError("rows and cols must not be negative")
         self.rows, self.cols, self.block = rows, cols, block
-        across = -(-rows // 128) if block == DST_FP8_SQUARE else rows
         self.q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)
-        self.scale = torch.empty(-(-cols // 128), -(-across // 4) * 4, dtype=torch.float32, device=device)
+        self.scale = torch.empty(-(-rows // 128), -(-cols // 512), 512, dtype=torch.uint8, device=device)
         self.device = self.q.device
         self._c = _Fp8(self.q.data_ptr(), self.scale.data_ptr(), rows, cols, self.q.shape[1], self.scale.shape[1], block, 0)
 
@@ -159,10 +158,16 @@ class Fp8Matrix:
         m._c = _Fp8(self._c.q, self._c.scale, rows, cols, self._c.ld, self._c.ld_scale, self.block, 0)
         return m
 
+    def scales(self) -> torch.Tensor:
+        """The scale of every row and column block, fp32 [rows, column blocks]."""
+        tiles, groups = self.scale.shape[:2]
+        e = self.scale.view(tiles, groups, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(tiles * 128, groups * 4)
+        e = e[:self.rows, :-(-self.cols // 128)].int()
+        return torch.where(e == 255, torch.nan, torch.ldexp(torch.ones_like(e, dtype=torch.float32), e - 127))
+
     def dequantize(self) -> torch.Tensor:
         """The fp32 matrix that the 8-bit one stands for."""
-        across = self.scale.T.repeat_interleave(128, 0) if self.block == DST_FP8_SQUARE else self.scale.T
-        return self.q[:, :self.cols].float() * across[:self.rows, :-(-self.cols // 128)].repeat_interleave(128, 1)[:, :self.cols]
+        return self.q[:, :self.cols].float() * self.scales().repeat_interleave(128, 1)[:, :self.cols]
 
 
 def dst_quantize_fp8(x: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, *, stream=None) -> None:

@@ -207,7 +207,7 @@ def test_quantize(rows, cols, xt, pad, skew, block, which):
         if m is not None:
             want, scale = o.quantize(v, size)
             assert np.array_equal(codes(m), want)
-            assert np.array_equal(np64(m.scale)[:, :scale.shape[1]], scale)
+            assert np.array_equal(np64(m.scales()), np.repeat(scale.T, size, 0)[:m.rows])
             assert np.array_equal(np64(m.dequantize()), o.dequantize(want, scale, size))
 
 
@@ -220,7 +220,7 @@ def test_quantize_limits():
     dst.dst_quantize_fp8(x, m)
     want, scale = o.quantize(np64(x), 1)
     ok = np.isfinite(scale.T).repeat(128, 1)
-    assert np.array_equal(codes(m)[ok], want[ok]) and np.array_equal(np64(m.scale), scale, equal_nan=True)
+    assert np.array_equal(codes(m)[ok], want[ok]) and np.array_equal(np64(m.scales()), scale.T, equal_nan=True)
     assert np.isnan(np64(m.dequantize())[~ok]).all()
 
 

@@ -24,8 +24,7 @@ def drop(p=0.1, seed=1, offset=0, device=None, row_offset=0):
 
 def fp8(rows, cols, ld=None, ld_scale=None, block=0, q=FAKE, scale=FAKE):
     ld = -(-cols // 16) * 16 if ld is None else ld
-    across = -(-rows // 128) if block else rows
-    return ctypes.byref(binding._Fp8(q, scale, rows, cols, ld, across if ld_scale is None else ld_scale, block, 0))
+    return ctypes.byref(binding._Fp8(q, scale, rows, cols, ld, -(-cols // 512) if ld_scale is None else ld_scale, block, 0))
 
 
 def dropout(lib, x=FAKE, ldx=8, xt=F32, res=None, ldr=0, out=FAKE * 2, ldo=8, ot=F32, rows=4, d=8, dr=None):
@@ -71,7 +70,7 @@ def test_quantize_refusals(lib):
     assert call(q=fp8(11, 200)) == 1 and call(q=fp8(10, 199)) == 1 and call(qt=fp8(10, 200)) == 1
     assert call(q=fp8(10, 200, ld=200)) == 1 and call(q=fp8(10, 200, ld=192)) == 1                    # not a multiple of 16, too short
     assert call(q=fp8(10, 200, q=FAKE + 8)) == 1 and call(q=fp8(10, 200, q=None)) == 1 and call(q=fp8(10, 200, scale=None)) == 1
-    assert call(q=fp8(10, 200, ld_scale=9)) == 1 and call(q=fp8(10, 200, block=2)) == 1
+    assert call(q=fp8(10, 200, ld_scale=0)) == 1 and call(q=fp8(10, 200, scale=FAKE + 8)) == 1 and call(q=fp8(10, 200, block=2)) == 1
     assert call(q=fp8(10, 200, block=1), qt=fp8(200, 10, block=0)) == 1                              # kinds that disagree
     assert call(rows=-1) == 1
     assert lib.dst_quantize_fp8(None, 0, F32, 0, 0, fp8(0, 0), None, None) == 0
@@ -135,4 +134,4 @@ def test_binding_refuses_tensors_off_the_gpu_and_of_other_types():
     m = dst.Fp8Matrix(300, 200, device="cpu")
     with pytest.raises(ValueError):
         m.part(301, 200)
-    assert m.part(10, 130).q.shape[0] == 10 and m.q.shape == (300, 208) and m.scale.shape == (2, 300)
+    assert m.part(10, 130).q.shape[0] == 10 and m.q.shape == (300, 208) and m.scale.shape == (3, 1, 512)

@@ -195,6 +195,7 @@ cudaError_t launch_quantize(const QuantParams& p, int x_type, cudaStream_t strea
 constexpr int kBlockK = 128;                              // one scale's worth of the inner dimension, in bytes too
 constexpr int kTileP = 128;                               // rows of P a CTA
 constexpr int kSmemMost = 232448;
+constexpr int kOutPitch = 272;                            // bytes of shared memory a lane stages a row in: 256, and room to start anywhere in 16
 
 template <int CG, int NT>
 struct TileShape {
@@ -205,7 +206,7 @@ struct TileShape {
     static constexpr int kStageBytes = (kTileP + kQRows) * kBlockK;
     static constexpr int kQScaleTiles = (NT + 127) / 128;
     static constexpr int kScaleBytes = (1 + kQScaleTiles) * kScaleTile;   // of four blocks
-    static constexpr int kOutBytes = kEpiWarps * 4096;    // 32 x 32 words a warp, for turning rows into runs
+    static constexpr int kOutBytes = kEpiWarps * 32 * kOutPitch;
     static constexpr int kHeaderBytes = 1024;
     static constexpr int kFit = (kSmemMost - kOutBytes - kHeaderBytes) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kFit < 8 ? kFit : 8;
@@ -317,41 +318,64 @@ __device__ __forceinline__ uint64_t scale_desc(unsigned addr) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-// The columns [c0, c0 + kCols) of a warp's 32 rows, from one row a lane to runs of consecutive columns.
-template <typename OT, int COLS>
-__device__ __forceinline__ void store_rows(const MatmulParams& p, OT* out, const float (&acc)[COLS], unsigned* words, int row0, int col0) {
-    const int lane = lane_id();
-    const int rows = min(32, p.rows_p - row0);
-    constexpr int kPerWord = 4 / (int)sizeof(OT);
-    constexpr int kWords = COLS / kPerWord < 32 ? COLS / kPerWord : 32;   // of a row, a round
-    const bool pairs = kPerWord == 1 || ((reinterpret_cast<uintptr_t>(out) & 3u) == 0 && (p.ldo & 1) == 0);
+// A lane's row of the tile, 256 bytes a round: into a row of shared memory that is the lane's own, at the place within 16
+// bytes that it has in the output, and from there by one asynchronous bulk copy of the 16-byte pieces that lie wholly in
+// the row; what is left at either end is stored plainly.  No lane waits for another one, nor for the copies until it needs its
+// row of shared memory again.  (Runs of 128 bytes through registers instead: 344 us for 8192 x 33708 x 1024, whose
+// rows are 8-byte aligned.)  ALIGN: bytes that rows of the output are aligned to.
+template <typename OT, int COLS, int ALIGN>
+__device__ __forceinline__ void store_row_aligned(const MatmulParams& p, OT* out, const float (&acc)[COLS], unsigned char* buffer, int row, int col0) {
+    constexpr int kSize = (int)sizeof(OT), kRound = COLS * kSize < 256 ? COLS : 256 / kSize, kWords = kRound * kSize / 4;
+    if (row >= p.rows_p) return;
 #pragma unroll
-    for (int c = 0; c < COLS; c += kWords * kPerWord) {
+    for (int c = 0; c < COLS; c += kRound) {
         if (col0 + c >= p.rows_q) break;
-        __syncwarp();
+        unsigned char* const at = reinterpret_cast<unsigned char*>(out + (long long)row * p.ldo + col0 + c);
+        const int shift = (int)(reinterpret_cast<uintptr_t>(at) & 15u), total = min(kRound, p.rows_q - col0 - c) * kSize;
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        unsigned v[kWords];
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
-            words[lane * 32 + (w ^ lane)] = kPerWord == 1 ? __float_as_uint(acc[c + w]) : pack_bf16(acc[c + w * kPerWord], acc[c + w * kPerWord + kPerWord - 1]);
-        __syncwarp();
-        if (pairs) {
-            const int col = col0 + c + lane * kPerWord;
-            for (int r = 0; r < rows; ++r) {
-                const unsigned v = words[r * 32 + (lane ^ r)];
-                OT* const at = out + (long long)(row0 + r) * p.ldo + col;
-                if (lane < kWords && col + kPerWord <= p.rows_q) *reinterpret_cast<unsigned*>(at) = v;
-                else if (lane < kWords && col < p.rows_q) *reinterpret_cast<unsigned short*>(at) = (unsigned short)v;
-            }
-        } else {
-            for (int r = 0; r < rows; ++r)
+            v[w] = kSize == 4 ? __float_as_uint(acc[c + w]) : pack_bf16(acc[c + w * 4 / kSize], acc[c + w * 4 / kSize + 4 / kSize - 1]);
+        unsigned char* const base = buffer + (ALIGN >= 4 ? shift : shift & ~3);
+        if (ALIGN == 16) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int i = h * 32 + lane, col = col0 + c + i;
-                    const unsigned v = words[r * 32 + (((i >> 1) & 31) ^ r)] >> ((i & 1) * 16);
-                    if (i < kWords * kPerWord && col < p.rows_q)
-                        *reinterpret_cast<unsigned short*>(out + (long long)(row0 + r) * p.ldo + col) = (unsigned short)v;
-                }
+            for (int w = 0; w < kWords; w += 4) *reinterpret_cast<uint4*>(base + w * 4) = make_uint4(v[w], v[w + 1], v[w + 2], v[w + 3]);
+        } else if (ALIGN == 8) {
+#pragma unroll
+            for (int w = 0; w < kWords; w += 2) *reinterpret_cast<uint2*>(base + w * 4) = make_uint2(v[w], v[w + 1]);
+        } else if (ALIGN == 4) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) *reinterpret_cast<unsigned*>(base + w * 4) = v[w];
+        } else {                                             // half a word further where the row starts in the middle of one
+            const unsigned pick = shift & 2 ? 0x5432u : 0x7654u;
+#pragma unroll
+            for (int w = 0; w <= kWords; ++w)
+                *reinterpret_cast<unsigned*>(base + w * 4) = __byte_perm(w > 0 ? v[w - 1] : 0u, w < kWords ? v[w] : 0u, pick);
         }
+        const int head = min((16 - shift) & 15, total), body = (total - head) & ~15;
+        if (body > 0) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;"
+                         ::"l"(at + head), "r"(smem_addr(buffer + shift + head)), "r"(body) : "memory");
+        }
+        auto plain = [&](int from, int n) {
+            const unsigned char* const src = buffer + shift;
+            if (ALIGN >= 8)
+                for (; n >= 8; from += 8, n -= 8) *reinterpret_cast<uint2*>(at + from) = *reinterpret_cast<const uint2*>(src + from);
+            for (; n > 0; from += kSize, n -= kSize) *reinterpret_cast<OT*>(at + from) = *reinterpret_cast<const OT*>(src + from);
+        };
+        if (ALIGN < 16) plain(0, head);
+        plain(head + body, total - head - body);
     }
+}
+template <typename OT, int COLS>
+__device__ __forceinline__ void store_row(const MatmulParams& p, OT* out, const float (&acc)[COLS], unsigned char* buffer, int row, int col0) {
+    const unsigned at = (unsigned)reinterpret_cast<uintptr_t>(out) | (unsigned)(p.ldo * sizeof(OT));
+    if ((at & 15) == 0) store_row_aligned<OT, COLS, 16>(p, out, acc, buffer, row, col0);
+    else if ((at & 7) == 0) store_row_aligned<OT, COLS, 8>(p, out, acc, buffer, row, col0);
+    else if (sizeof(OT) == 4 || (at & 3) == 0) store_row_aligned<OT, COLS, 4>(p, out, acc, buffer, row, col0);
+    else store_row_aligned<OT, COLS, 2>(p, out, acc, buffer, row, col0);
 }
 // The result is [q, p]: a lane's row is its column there, neighbouring lanes write neighbouring elements.
 template <typename OT, int COLS>
@@ -369,8 +393,8 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     using S = TileShape<CG, NT>;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const scale_ring = smem + S::kStages * S::kStageBytes;
-    unsigned char* const out_words = scale_ring + S::kStages * S::kScaleBytes;
-    unsigned char* const header = out_words + S::kOutBytes;
+    unsigned char* const out_rows = scale_ring + S::kStages * S::kScaleBytes;
+    unsigned char* const header = out_rows + S::kOutBytes;
     unsigned* const tmem_slot = reinterpret_cast<unsigned*>(header);
     const unsigned bars = smem_addr(header + 16);
     const unsigned full = bars, empty = bars + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 8 * S::kBufs;
@@ -485,7 +509,7 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     } else {                                                                       // ---- epilogue ----
         const int group = warp >> 2, quarter = warp & 3;                           // a warp reaches the 32 lanes of its quarter
         const unsigned mine = tmem + ((unsigned)(quarter * 32) << 16) + group * 128;
-        unsigned* const words = reinterpret_cast<unsigned*>(out_words + warp * 4096);
+        unsigned char* const buffer = out_rows + threadIdx.x * kOutPitch;
         const unsigned free_bar = in_cta(tmem_empty, 0);
         int buf = 0;
         unsigned buf_phase = 0;
@@ -513,8 +537,9 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
             }
             OT* const out = static_cast<OT*>(p.out) + part * p.split_stride;
             if (p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
-            else if (row0 < p.rows_p) store_rows<OT, S::kCols>(p, out, acc, words, row0, col0);
+            else store_row<OT, S::kCols>(p, out, acc, buffer, row0 + lane, col0);
         }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) {                                                                     // let copies and instructions in flight land
         const long long t0 = clock64();

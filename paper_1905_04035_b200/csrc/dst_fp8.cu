@@ -9,14 +9,16 @@ namespace dst {
 // ---- quantisation -----------------------------------------------------------------
 // The scale of a block whose largest magnitude has the bits `amax`, as an exponent plus 127: the smallest power of two
 // 2^e with amax <= 448 * 2^e.  448 = 1.75 * 2^8, so e is amax's exponent less 8, one more where its mantissa is above
-// 1.75.  255 (NaN) where the block holds an infinity or a NaN (their bits are the largest).
-__device__ __forceinline__ unsigned block_exponent(unsigned amax) {
-    if (amax >= 0x7F800000u) return 255u;
-    amax = max(amax, 0x0D800000u);                          // 2^-100
-    return (amax >> 23) - 8u + ((amax & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
+// 1.75: adding all that 1.75 leaves of a mantissa, less one, carries exactly there.  255 (NaN) where the block holds an
+// infinity or a NaN (their bits are the largest).
+struct BlockScale {
+    unsigned exponent;
+    float inverse;                                          // 2^-e, exact (any number where the scale is NaN)
+};
+__device__ __forceinline__ BlockScale block_scale(unsigned amax) {
+    const unsigned carried = max(amax, 0x0D800000u) + 0x1FFFFFu;   // 2^-100 at least
+    return BlockScale{amax >= 0x7F800000u ? 255u : (carried >> 23) - 8u, __uint_as_float(0x83000000u - (carried & 0xFF800000u))};
 }
-// 2^-e: exact (what a block with the scale NaN is multiplied by does not matter)
-__device__ __forceinline__ float block_unscale(unsigned exponent) { return __uint_as_float((254u - min(exponent, 253u)) << 23); }
 __device__ __forceinline__ uint8_t* scale_byte(const Fp8View& m, long long row, long long block) {
     return m.scale + ((row >> 7) * m.ld_scale + (block >> 2)) * kScaleTile + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
@@ -27,16 +29,18 @@ __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d
     return lo | hi << 16;
 }
 
-// four neighbouring elements as they are stored
+// Four neighbouring elements as they are stored; the largest magnitudes of four rows' elements in each of the columns.
 template <typename T> struct Four;
 template <> struct Four<float> {
     float4 v;
     __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void set(int j, float x) { (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) = x; }
     __device__ __forceinline__ float get(int j) const { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
-    __device__ __forceinline__ unsigned amax() const {
-        const unsigned m = 0x7FFFFFFFu;
-        return max(max(__float_as_uint(v.x) & m, __float_as_uint(v.y) & m), max(__float_as_uint(v.z) & m, __float_as_uint(v.w) & m));
+    __device__ __forceinline__ unsigned abs(int j) const { return __float_as_uint(get(j)) & 0x7FFFFFFFu; }
+    __device__ __forceinline__ unsigned amax() const { return max(max(abs(0), abs(1)), max(abs(2), abs(3))); }
+    __device__ static __forceinline__ void column_amax(const Four (&w)[4], unsigned (&top)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = max(max(w[0].abs(i), w[1].abs(i)), max(w[2].abs(i), w[3].abs(i)));
     }
 };
 template <> struct Four<__nv_bfloat16> {
@@ -55,106 +59,122 @@ template <> struct Four<__nv_bfloat16> {
         const unsigned m = __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu);
         return max(m << 16, m & 0xFFFF0000u);
     }
+    __device__ static __forceinline__ void column_amax(const Four (&w)[4], unsigned (&top)[4]) {
+        const unsigned k = 0x7FFF7FFFu;
+        const unsigned a = __vmaxu2(__vmaxu2(w[0].v.x & k, w[1].v.x & k), __vmaxu2(w[2].v.x & k, w[3].v.x & k));
+        const unsigned b = __vmaxu2(__vmaxu2(w[0].v.y & k, w[1].v.y & k), __vmaxu2(w[2].v.y & k, w[3].v.y & k));
+        top[0] = a << 16; top[1] = a & 0xFFFF0000u; top[2] = b << 16; top[3] = b & 0xFFFF0000u;
+    }
 };
 
-constexpr int kQuantThreads = 256, kQuantWarps = kQuantThreads / 32, kQuantRows = 128 / kQuantWarps;
+// fp32 tiles take twice the warps: a warp then holds eight rows, 32 registers a lane, and two CTAs share an SM
+template <typename T> struct QuantShape {
+    static constexpr int kThreads = sizeof(T) == 4 ? 512 : 256, kWarps = kThreads / 32, kRows = 128 / kWarps, kCtas = sizeof(T) == 4 ? 2 : 4;
+};
 constexpr int kQuantPitch = 132;                           // elements between rows of the staged tile
 
-// A CTA takes 128 x 128 elements, read once: a warp holds 16 whole rows of the tile, four neighbouring columns a lane,
+// A CTA takes 128 x 128 elements, read once: a warp holds whole rows of the tile, four neighbouring columns a lane,
 // so a row's largest magnitude is one reduction over the warp and its 128 bytes go out in one store.  For the transpose
 // the tile passes through shared memory: row r is kept in place (r % 4) * 32 + r / 4, so that a lane that wants rows
 // 4 l .. 4 l + 3 (the four bytes of a transposed row it writes) reads, with the whole warp, neighbouring places.
-// VEC: rows are aligned to four elements.
-template <typename T, bool SQUARE, bool VEC>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize(const __grid_constant__ QuantParams p) {
-    extern __shared__ __align__(16) unsigned char dyn[];
-    __shared__ unsigned warp_max[kQuantWarps];
-    T* const tile = reinterpret_cast<T*>(dyn);
-    pdl_trigger();
-    pdl_wait();
-    const int col_tiles = (int)((p.cols + 127) >> 7);
-    const long long rb = blockIdx.x / col_tiles, cb = blockIdx.x - rb * col_tiles, r0 = rb * 128, c0 = cb * 128;
-    const int nr = (int)min(p.rows - r0, 128ll), nc = (int)min(p.cols - c0, 128ll);
+// VEC: rows are aligned to four elements.  FULL: the whole tile is inside the matrix.
+template <typename T, bool SQUARE, bool VEC, bool FULL>
+__device__ __forceinline__ void quantize_tile(const QuantParams& p, T* tile, unsigned* warp_max, long long rb, long long cb) {
+    using S = QuantShape<T>;
+    const long long r0 = rb * 128, c0 = cb * 128;
+    const int nr = FULL ? 128 : (int)min(p.rows - r0, 128ll), nc = FULL ? 128 : (int)min(p.cols - c0, 128ll);
     const int lane = lane_id(), warp = warp_id();
-    const T* const x = static_cast<const T*>(p.x) + r0 * p.ldx + c0 + lane * 4;
-    Four<T> v[kQuantRows];
+    using Raw = decltype(Four<T>::v);
+    Four<T> v[S::kRows];
+    {
+        const T* x = static_cast<const T*>(p.x) + (r0 + warp) * p.ldx + c0 + lane * 4;
 #pragma unroll
-    for (int i = 0; i < kQuantRows; ++i) {
-        const int r = i * kQuantWarps + warp;
-        v[i].clear();
-        if (r < nr) {
-            if (VEC && lane * 4 + 4 <= nc) v[i].v = __ldcs(reinterpret_cast<const decltype(v[i].v)*>(x + r * p.ldx));
+        for (int i = 0; i < S::kRows; ++i, x += S::kWarps * p.ldx) {
+            if (VEC && FULL) { v[i].v = __ldcs(reinterpret_cast<const Raw*>(x)); continue; }
+            v[i].clear();
+            if (i * S::kWarps + warp >= nr) continue;
+            if (VEC && lane * 4 + 4 <= nc) v[i].v = __ldcs(reinterpret_cast<const Raw*>(x));
             else
-                for (int j = 0; j < 4; ++j) if (lane * 4 + j < nc) v[i].set(j, x[r * p.ldx + j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (lane * 4 + j < nc) v[i].set(j, x[j]);
         }
     }
-    unsigned square = 0;
     if (SQUARE) {
         unsigned top = 0;
 #pragma unroll
-        for (int i = 0; i < kQuantRows; ++i) top = max(top, v[i].amax());
+        for (int i = 0; i < S::kRows; ++i) top = max(top, v[i].amax());
         top = __reduce_max_sync(0xFFFFFFFFu, top);
         if (lane == 0) warp_max[warp] = top;
     }
     if (p.qt.q) {
 #pragma unroll
-        for (int i = 0; i < kQuantRows; ++i) {
-            const int r = i * kQuantWarps + warp;
-            *reinterpret_cast<decltype(v[i].v)*>(tile + ((r & 3) * 32 + (r >> 2)) * kQuantPitch + lane * 4) = v[i].v;
+        for (int i = 0; i < S::kRows; ++i) {
+            const int r = i * S::kWarps + warp;
+            *reinterpret_cast<Raw*>(tile + ((r & 3) * 32 + (r >> 2)) * kQuantPitch + lane * 4) = v[i].v;
         }
     }
     if (SQUARE || p.qt.q) __syncthreads();
+    BlockScale sc{0, 0.f};
     if (SQUARE) {
         unsigned top = 0;
-        for (int w = 0; w < kQuantWarps; ++w) top = max(top, warp_max[w]);
-        square = block_exponent(top);
+        for (int w = 0; w < S::kWarps; ++w) top = max(top, warp_max[w]);
+        sc = block_scale(top);
         if (threadIdx.x < 128) {                            // every row's byte, as the product wants it
-            if (p.q.q) *scale_byte(p.q, r0 + threadIdx.x, cb) = (uint8_t)square;
-            if (p.qt.q) *scale_byte(p.qt, c0 + threadIdx.x, rb) = (uint8_t)square;
+            if (p.q.q) *scale_byte(p.q, r0 + threadIdx.x, cb) = (uint8_t)sc.exponent;
+            if (p.qt.q) *scale_byte(p.qt, c0 + threadIdx.x, rb) = (uint8_t)sc.exponent;
         }
     }
     if (p.q.q) {
+        uint8_t* q = p.q.q + (r0 + warp) * p.q.ld + c0 + lane * 4;
+        unsigned mine = 0;                                  // lane i: the exponent of the warp's i-th row
 #pragma unroll
-        for (int i = 0; i < kQuantRows; ++i) {
-            const int r = i * kQuantWarps + warp;
-            if (r >= nr) break;
-            unsigned e = square;
+        for (int i = 0; i < S::kRows; ++i, q += S::kWarps * p.q.ld) {
             if (!SQUARE) {
-                e = block_exponent(__reduce_max_sync(0xFFFFFFFFu, v[i].amax()));
-                if (lane == 0) *scale_byte(p.q, r0 + r, cb) = (uint8_t)e;
+                sc = block_scale(__reduce_max_sync(0xFFFFFFFFu, v[i].amax()));
+                if (lane == i) mine = sc.exponent;
             }
-            const float u = block_unscale(e);
-            if (lane * 4 < nc)                              // (up to three bytes of a row's padding are written too)
-                *reinterpret_cast<unsigned*>(p.q.q + (r0 + r) * p.q.ld + c0 + lane * 4) =
-                    to_e4m3x4(v[i].get(0) * u, v[i].get(1) * u, v[i].get(2) * u, v[i].get(3) * u);
+            const float u = sc.inverse;
+            if (FULL || (i * S::kWarps + warp < nr && lane * 4 < nc))   // (up to three bytes of a row's padding are written too)
+                *reinterpret_cast<unsigned*>(q) = to_e4m3x4(v[i].get(0) * u, v[i].get(1) * u, v[i].get(2) * u, v[i].get(3) * u);
         }
+        if (!SQUARE && lane < S::kRows && lane * S::kWarps + warp < nr) *scale_byte(p.q, r0 + lane * S::kWarps + warp, cb) = (uint8_t)mine;
     }
     if (p.qt.q) {
+        constexpr int kCols = 128 / S::kWarps;              // of the warp, consecutive
+        uint8_t* q = p.qt.q + (c0 + warp * kCols) * p.qt.ld + r0 + lane * 4;
+        const T* from = tile + lane * kQuantPitch + warp * kCols;
+        unsigned mine = 0;
 #pragma unroll
-        for (int k = 0; k < 32 / kQuantWarps; ++k) {
-            const int c = (k * kQuantWarps + warp) * 4;      // four columns, rows 4 lane .. 4 lane + 3
-            if (c >= nc) break;
+        for (int k = 0; k < kCols; k += 4) {                // four columns, rows 4 lane .. 4 lane + 3
             Four<T> w[4];
+            unsigned top[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j].v = *reinterpret_cast<const decltype(w[j].v)*>(tile + (j * 32 + lane) * kQuantPitch + c);
+            for (int j = 0; j < 4; ++j) w[j].v = *reinterpret_cast<const Raw*>(from + j * 32 * kQuantPitch + k);
+            if (!SQUARE) Four<T>::column_amax(w, top);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (c + i >= nc) break;
-                const float a0 = w[0].get(i), a1 = w[1].get(i), a2 = w[2].get(i), a3 = w[3].get(i);
-                unsigned e = square;
+            for (int i = 0; i < 4; ++i, q += p.qt.ld) {
                 if (!SQUARE) {
-                    const unsigned m = 0x7FFFFFFFu;
-                    const unsigned top = max(max(__float_as_uint(a0) & m, __float_as_uint(a1) & m), max(__float_as_uint(a2) & m, __float_as_uint(a3) & m));
-                    e = block_exponent(__reduce_max_sync(0xFFFFFFFFu, top));
-                    if (lane == 0) *scale_byte(p.qt, c0 + c + i, rb) = (uint8_t)e;
+                    sc = block_scale(__reduce_max_sync(0xFFFFFFFFu, top[i]));
+                    if (lane == k + i) mine = sc.exponent;
                 }
-                const float u = block_unscale(e);
-                if (lane * 4 < nr)
-                    *reinterpret_cast<unsigned*>(p.qt.q + (c0 + c + i) * p.qt.ld + r0 + lane * 4) = to_e4m3x4(a0 * u, a1 * u, a2 * u, a3 * u);
+                const float u = sc.inverse;
+                if (FULL || (warp * kCols + k + i < nc && lane * 4 < nr))
+                    *reinterpret_cast<unsigned*>(q) = to_e4m3x4(w[0].get(i) * u, w[1].get(i) * u, w[2].get(i) * u, w[3].get(i) * u);
             }
         }
+        if (!SQUARE && lane < kCols && warp * kCols + lane < nc) *scale_byte(p.qt, c0 + warp * kCols + lane, rb) = (uint8_t)mine;
     }
+}
+
+template <typename T, bool SQUARE, bool VEC>
+__global__ void __launch_bounds__(QuantShape<T>::kThreads, QuantShape<T>::kCtas) k_quantize(const __grid_constant__ QuantParams p) {
+    extern __shared__ __align__(16) unsigned char dyn[];
+    __shared__ unsigned warp_max[QuantShape<T>::kWarps];
+    pdl_trigger();
+    pdl_wait();
+    const int col_tiles = (int)((p.cols + 127) >> 7), rb = blockIdx.x / col_tiles, cb = blockIdx.x - rb * col_tiles;
+    if (rb * 128ll + 128 <= p.rows && cb * 128ll + 128 <= p.cols) quantize_tile<T, SQUARE, VEC, true>(p, reinterpret_cast<T*>(dyn), warp_max, rb, cb);
+    else quantize_tile<T, SQUARE, VEC, false>(p, reinterpret_cast<T*>(dyn), warp_max, rb, cb);
 }
 
 template <typename T, bool SQUARE, bool VEC>
@@ -164,7 +184,7 @@ static cudaError_t quantize_v(const QuantParams& p, cudaStream_t stream) {
     const cudaError_t e = ensure_dynamic_smem(k_quantize<T, SQUARE, VEC>, smem, opt);
     if (e != cudaSuccess) return e;
     const long long tiles = ((p.cols + 127) / 128) * ((p.rows + 127) / 128);
-    return launch_pdl(k_quantize<T, SQUARE, VEC>, dim3((unsigned)tiles), dim3(kQuantThreads), smem, stream, p);
+    return launch_pdl(k_quantize<T, SQUARE, VEC>, dim3((unsigned)tiles), dim3(QuantShape<T>::kThreads), smem, stream, p);
 }
 template <typename T>
 static cudaError_t quantize_t(const QuantParams& p, cudaStream_t stream) {

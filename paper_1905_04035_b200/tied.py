@@ -19,55 +19,66 @@ _INDEX = {torch.int32: DST_I32, torch.int64: DST_I64}
 _nothing = contextlib.nullcontext()
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, name: str):
-    """(pointer, leading dimension, type) of a [rows, cols] matrix with contiguous rows."""
+# the stream that work goes to unless one is given; torch's own accessor of the raw handle, without a Stream object a call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, index: int, name: str):
+    """(pointer, leading dimension, type) of a [rows, cols] matrix with contiguous rows on CUDA device `index`."""
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
+    _here(t, index)
     ld, step = t.stride()
-    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+    if rows <= 1:
+        ld = cols
+    if (step != 1 and cols > 1) or ld < cols:
         raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    return t.data_ptr(), max(ld, cols) if rows > 1 else max(cols, 1), kind
+    return t.data_ptr(), ld, kind
 
 
-def _vector(t: Optional[torch.Tensor], n: int, dtype, device, name: str):
+def _vector(t: Optional[torch.Tensor], n: int, dtype, index: int, name: str):
     if t is None:
         return None
     if t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s must be contiguous [%d]" % (name, n))
-    if t.device != device:
-        raise ValueError("all tensors must live on the same device")
+    _here(t, index)
     return t.data_ptr()
 
 
-def _same_device(device, *tensors) -> None:
-    if device.type != "cuda":
+def _device(t: torch.Tensor) -> int:
+    index = t.get_device()
+    if index < 0:
         raise ValueError("tensors must be CUDA tensors")
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError("all tensors must live on the same device")
+    return index
 
 
-def _on(device):
-    """The context in which work for `device` is enqueued (nothing to do where it is current already)."""
-    return _nothing if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _here(t: torch.Tensor, index: int) -> None:
+    if t.get_device() != index:
+        raise ValueError("all tensors must live on the same device")
 
 
-def _stream(stream, device) -> int:
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _on(index: int):
+    """The context in which work for a device is enqueued (nothing to do where it is current already)."""
+    return _nothing if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
-def _drop(p, seed, offset, offset_tensor, row_offset, device) -> _Dropout:
+def _stream(stream, index: int) -> int:
+    return _raw_stream(index) if stream is None else stream.cuda_stream
+
+
+def _drop(p, seed, offset, offset_tensor, row_offset, index) -> _Dropout:
+    at = None
     if offset_tensor is not None:
         if offset_tensor.dtype != torch.int64 or offset_tensor.numel() != 1:
             raise TypeError("offset_tensor must hold one int64")
-        _same_device(device, offset_tensor)
-    return _Dropout(p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF,
-                    None if offset_tensor is None else offset_tensor.data_ptr(), row_offset)
+        _here(offset_tensor, index)
+        at = offset_tensor.data_ptr()
+    return _Dropout(p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF, at, row_offset)
 
 
 def dst_dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, offset: int = 0, *,
@@ -75,21 +86,20 @@ def dst_dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, offset:
                 offset_tensor: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue ``dst_dropout``: out = residual + scale * dropout(x).  The same call on the output's gradient, without
     the residual, is the gradient of ``x``.  ``out`` may be ``x`` or ``residual``."""
+    index = _device(out)
     if x.dim() != 2:
         raise ValueError("x must be [rows, d]")
     rows, d = x.shape
-    device = out.device
-    _same_device(device, x, residual)
-    px, ldx, tx = _matrix(x, rows, d, "x")
-    po, ldo, to = _matrix(out, rows, d, "out")
+    px, ldx, tx = _matrix(x, rows, d, index, "x")
+    po, ldo, to = _matrix(out, rows, d, index, "out")
     pr, ldr = None, 0
     if residual is not None:
-        pr, ldr, tr = _matrix(residual, rows, d, "residual")
+        pr, ldr, tr = _matrix(residual, rows, d, index, "residual")
         if tr != to:
             raise TypeError("residual and out must share a dtype")
-    drop = _drop(p, seed, offset, offset_tensor, row_offset, device)
-    with _on(device):
-        rc = load_library().dst_dropout(px, ldx, tx, pr, ldr, po, ldo, to, rows, d, scale, drop, _stream(stream, device))
+    drop = _drop(p, seed, offset, offset_tensor, row_offset, index)
+    with _on(index):
+        rc = load_library().dst_dropout(px, ldx, tx, pr, ldr, po, ldo, to, rows, d, scale, drop, _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_dropout")
     return out
@@ -106,28 +116,33 @@ def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *,
     index_type = _INDEX.get(indices.dtype)
     if index_type is None:
         raise TypeError("indices must be int32 or int64, got %s" % indices.dtype)
-    if indices.dim() != 1 or not indices.is_contiguous() or weight.dim() != 2:
-        raise ValueError("indices must be 1-D contiguous and weight [vocab, d]")
+    index = _device(out)
+    if indices.dim() != 1 or weight.dim() != 2:
+        raise ValueError("indices must be 1-D and weight [vocab, d]")
     n, (vocab, d) = indices.shape[0], weight.shape
-    device = out.device
-    _same_device(device, indices, weight, position, result)
-    pw, _, tw = _matrix(weight, vocab, d, "weight")
-    po, _, to = _matrix(out, n, d, "out")
-    if not weight.is_contiguous() or not out.is_contiguous():
+    pi = _vector(indices, n, indices.dtype, index, "indices")
+    pw, ldw, tw = _matrix(weight, vocab, d, index, "weight")
+    po, ldo, to = _matrix(out, n, d, index, "out")
+    if ldw != d or ldo != d:
         raise ValueError("weight and out must be contiguous")
     n_pos, pp = 0, None
     if position is not None:
-        if position.dtype != torch.float32:
+        n_pos = position.shape[0] if position.dim() == 2 else 0
+        pp, ldp, tp = _matrix(position, n_pos, d, index, "position")
+        if tp != DST_F32:
             raise TypeError("position must be float32, got %s" % position.dtype)
-        if position.dim() != 2 or position.shape[1] != d or not position.is_contiguous():
+        if ldp != d:
             raise ValueError("position must be contiguous [n_positions, d]")
-        n_pos, pp = position.shape[0], position.data_ptr()
-    if result is not None and (not result.is_contiguous() or result.numel() * result.element_size() < 24):
-        raise ValueError("result must be contiguous and hold 24 bytes")
-    drop = _drop(p, seed, offset, offset_tensor, row_offset, device)
-    with _on(device):
-        rc = load_library().dst_embed(indices.data_ptr(), n, index_type, pw, vocab, d, tw, pp, n_pos, po, to, scale, drop,
-                                      None if result is None else result.data_ptr(), _stream(stream, device))
+    pres = None
+    if result is not None:
+        if not result.is_contiguous() or result.numel() * result.element_size() < 24:
+            raise ValueError("result must be contiguous and hold 24 bytes")
+        _here(result, index)
+        pres = result.data_ptr()
+    drop = _drop(p, seed, offset, offset_tensor, row_offset, index)
+    with _on(index):
+        rc = load_library().dst_embed(pi, n, index_type, pw, vocab, d, tw, pp, n_pos, po, to, scale, drop, pres,
+                                      _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_embed")
     return out
@@ -172,17 +187,19 @@ class Fp8Matrix:
 
 def dst_quantize_fp8(x: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, *, stream=None) -> None:
     """Enqueue ``dst_quantize_fp8``: x into ``q`` and its transpose into ``qt`` (either may be None)."""
-    some = q if q is not None else qt
-    if some is None:
+    if q is None and qt is None:
         raise ValueError("q or qt must be given")
+    index = _device(x)
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
     rows, cols = x.shape
-    _same_device(some.device, x, None if q is None else q.q, None if qt is None else qt.q)
-    px, ldx, tx = _matrix(x, rows, cols, "x")
-    with _on(some.device):
+    px, ldx, tx = _matrix(x, rows, cols, index, "x")
+    for m in (q, qt):
+        if m is not None:
+            _here(m.q, index)
+    with _on(index):
         rc = load_library().dst_quantize_fp8(px, ldx, tx, rows, cols, None if q is None else q._c,
-                                             None if qt is None else qt._c, _stream(stream, some.device))
+                                             None if qt is None else qt._c, _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_quantize_fp8")
 
@@ -195,19 +212,23 @@ def dst_linear_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(load_library().dst_linear_fp8_workspace_bytes(M, N, K))
 
 
-def _workspace(t: Optional[torch.Tensor]):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+def _workspace(t: Optional[torch.Tensor], index: int):
+    if t is None:
+        return None, 0
+    _here(t, index)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def dst_matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
                    stream=None) -> torch.Tensor:
     """Enqueue ``dst_matmul_fp8``: out [a.rows, b.rows] = a b^T."""
-    device = out.device
-    _same_device(device, a.q, b.q, workspace)
-    po, ldo, to = _matrix(out, a.rows, b.rows, "out")
-    ws, ws_bytes = _workspace(workspace)
-    with _on(device):
-        rc = load_library().dst_matmul_fp8(a._c, b._c, po, ldo, to, ws, ws_bytes, _stream(stream, device))
+    index = _device(out)
+    _here(a.q, index)
+    _here(b.q, index)
+    po, ldo, to = _matrix(out, a.rows, b.rows, index, "out")
+    ws, ws_bytes = _workspace(workspace, index)
+    with _on(index):
+        rc = load_library().dst_matmul_fp8(a._c, b._c, po, ldo, to, ws, ws_bytes, _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_matmul_fp8")
     return out
@@ -216,15 +237,16 @@ def dst_matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor, workspace: Opt
 def dst_linear_fp8(x: torch.Tensor, w: Fp8Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
                    stream=None) -> torch.Tensor:
     """Enqueue ``dst_linear_fp8``: out [x.rows, w.rows] = quantised(x) w^T."""
+    index = _device(out)
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
-    device, m = out.device, x.shape[0]
-    _same_device(device, x, w.q, workspace)
-    px, ldx, tx = _matrix(x, m, w.cols, "x")
-    po, ldo, to = _matrix(out, m, w.rows, "out")
-    ws, ws_bytes = _workspace(workspace)
-    with _on(device):
-        rc = load_library().dst_linear_fp8(px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes, _stream(stream, device))
+    m = x.shape[0]
+    px, ldx, tx = _matrix(x, m, w.cols, index, "x")
+    po, ldo, to = _matrix(out, m, w.rows, index, "out")
+    _here(w.q, index)
+    ws, ws_bytes = _workspace(workspace, index)
+    with _on(index):
+        rc = load_library().dst_linear_fp8(px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes, _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_linear_fp8")
     return out
@@ -235,24 +257,24 @@ def dst_sample(logits: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor
                top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
                prob: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue ``dst_sample``: a token per row of ``logits`` from the row's uniform number and filters."""
-    if logits.dim() != 2:
-        raise ValueError("logits must be [rows, vocab]")
-    rows, vocab = logits.shape
-    device = logits.device
     token_type = _INDEX.get(tokens.dtype)
     if token_type is None:
         raise TypeError("tokens must be int32 or int64, got %s" % tokens.dtype)
-    _same_device(device)
-    pl, ld, tl = _matrix(logits, rows, vocab, "logits")
-    f32, lib = torch.float32, load_library()
-    args = (_vector(uniform, rows, f32, device, "uniform"), _vector(temperature, rows, f32, device, "temperature"),
-            _vector(top_k, rows, torch.int32, device, "top_k"), _vector(top_p, rows, f32, device, "top_p"),
-            _vector(min_p, rows, f32, device, "min_p"), _vector(tokens, rows, tokens.dtype, device, "tokens"))
-    if args[0] is None:
-        raise ValueError("uniform must be given")
-    with _on(device):
-        rc = lib.dst_sample(pl, ld, tl, rows, vocab, *args, token_type, _vector(prob, rows, f32, device, "prob"),
-                            _stream(stream, device))
+    index = _device(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    rows, vocab = logits.shape
+    pl, ld, tl = _matrix(logits, rows, vocab, index, "logits")
+    f32 = torch.float32
+    pu = _vector(uniform, rows, f32, index, "uniform")
+    pt = _vector(temperature, rows, f32, index, "temperature")
+    pk = _vector(top_k, rows, torch.int32, index, "top_k")
+    pp = _vector(top_p, rows, f32, index, "top_p")
+    pm = _vector(min_p, rows, f32, index, "min_p")
+    po = _vector(tokens, rows, tokens.dtype, index, "tokens")
+    pb = _vector(prob, rows, f32, index, "prob")
+    with _on(index):
+        rc = load_library().dst_sample(pl, ld, tl, rows, vocab, pu, pt, pk, pp, pm, po, token_type, pb, _stream(stream, index))
     if rc != 0:
         raise DstError(rc, "dst_sample")
     return tokens

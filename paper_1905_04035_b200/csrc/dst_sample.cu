@@ -1,12 +1,17 @@
 // One token per row of logits from a given uniform number, with temperature, top-k, top-p and min-p.
 //
-// No sort.  The filters keep the entries above some value and the first few (in index order) of those equal to it, so
-// a row needs that value and that count alone: a histogram over equal steps of the scaled logit finds the step in
-// which top-k's count, or top-p's mass, is reached, and finer histograms over the bits of the logit narrow the step
-// down to one value.  The weights are whole numbers (2^31 * exp, rounded), so every sum is exact whatever its order.
+// The filters keep the entries above some value and the first few (in index order) of those equal to it, so a row needs
+// that value and that count alone.  The weights are whole numbers (2^31 * exp, rounded), so every sum is exact whatever
+// its order, and a row may be split in any way.
 //
-// A row belongs to a cluster of 1, 2, 4 or 8 CTAs, each with a slice of it in shared memory; the histograms are
-// joined through distributed shared memory, and every CTA takes the same decisions from the joined one.
+// Few candidates (top-k up to some hundred, or a short row): every thread's largest logit gives a bound that at least
+// k logits reach; the few that do are collected in index order, their values sorted, and all that follows is on that list: the
+// row is read twice, with a few instructions an entry.
+// Otherwise: a histogram over equal steps of the scaled logit finds the step in which top-k's count, or top-p's mass, is
+// reached, finer histograms over the bits of the logit narrow the step down to one value, and a last pass sums what is
+// kept in index order.
+//
+// A row belongs to a cluster of 1, 2, 4 or 8 CTAs with a slice of it each, joined through distributed shared memory.
 #include <cooperative_groups.h>
 
 #include "dst_tied.cuh"
@@ -15,13 +20,15 @@ namespace dst {
 namespace cg = cooperative_groups;
 
 typedef unsigned long long u64;
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleCtas = 8;               // of a cluster, at most
 constexpr int kBins = 2048;
+constexpr int kListMost = 1024;              // candidates that are worked on as a list (twice the threads)
+constexpr int kListRank = 384;               // top-k for each CTA of a row up to which the threads' maxima bound it well
 constexpr float kZeroWeight = -22.25f;       // below this z the weight rounds to zero (2^31 e^z < 1/2 below -22.18)
 constexpr float kBinsPerZ = kBins / 22.25f;
-constexpr int kSampleSlice = 65536;          // entries a CTA takes, at most: its sums of 16-bit halves stay within 32 bits
+constexpr int kSampleSlice = 49152;          // entries a CTA takes, about: its sums of 16-bit halves stay within 32 bits
 constexpr unsigned kLowestKey = 0x007FFFFFu; // key of -infinity
 
 // order-preserving bits of a float; equal floats (the two zeros) have equal keys, NaN counts as -infinity
@@ -32,9 +39,10 @@ __device__ __forceinline__ unsigned key_of(float x) {
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-struct Row {                                 // what turns a logit into its weight
+struct Weigh {                               // what turns a logit into its weight
     float top, inv_t, min_p;
     __device__ __forceinline__ float z(float x) const { return x == top ? 0.f : __fmul_rn(x - top, inv_t); }
+    __device__ __forceinline__ float e(unsigned key) const { return expf(z(of_key(key))); }
     __device__ __forceinline__ static unsigned weight(float e) { return __float2uint_rn(e * 2147483648.f); }
 };
 
@@ -43,138 +51,348 @@ __device__ __forceinline__ u64 share(unsigned part, u64 total) {
     return (u64)part * (total >> 24) + (((u64)part * (total & 0xFFFFFFu)) >> 24);
 }
 
-struct SampleShared {
-    unsigned count[kBins], low[kBins], high[kBins];              // this CTA's histogram (the mass in halves of 16 bits)
-    u64 joined_mass[kBins];                                      // the cluster's
-    unsigned joined_count[kBins];
-    u64 seg_mass[kSampleWarps];
-    unsigned seg_ties[kSampleWarps];
-    unsigned top_key;
-    unsigned warp_key[kSampleWarps];
-    unsigned warp_count[kSampleWarps];
-    u64 warp_mass[kSampleWarps];
-    unsigned hit_bin, hit_count_above, hit_count;
-    u64 hit_mass_above, hit_mass;
-    unsigned pick_seg, pick_ties;
-    u64 pick_left, pick_total;
+// The slice's vectors of 16 bytes; the first and the last may lie partly outside the row and are read entry by entry.
+template <typename T> struct Vec {
+    static constexpr int kN = 16 / sizeof(T);
+    uint4 v;
+    __device__ __forceinline__ float get(int i) const;
+    __device__ __forceinline__ float largest() const;
+};
+template <> __device__ __forceinline__ float Vec<float>::get(int i) const { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
+template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::get(int i) const {
+    const unsigned w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+    return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+}
+// (the maximum of a NaN and a number is the number)
+template <> __device__ __forceinline__ float Vec<float>::largest() const { return fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))); }
+template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::largest() const {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+template <typename T> __device__ __forceinline__ T lowest();
+template <> __device__ __forceinline__ float lowest<float>() { return -INFINITY; }
+template <> __device__ __forceinline__ __nv_bfloat16 lowest<__nv_bfloat16>() { return __ushort_as_bfloat16(0xFF80); }
+
+template <typename T> struct Slice {
+    const T* base;                           // 16-byte aligned, at or before the row's first entry
+    int skew, vocab;                         // entries between base and the row; vector v holds entries v * kN - skew ...
+    int begin, end;                          // this warp's vectors
+    __device__ __forceinline__ Vec<T> load(int v) const {
+        constexpr int kN = Vec<T>::kN;
+        Vec<T> r;
+        const int first = v * kN - skew;
+        if (first >= 0 && first + kN <= vocab) r.v = *reinterpret_cast<const uint4*>(base + (long long)v * kN);
+        else {
+            T x[kN];
+#pragma unroll
+            for (int i = 0; i < kN; ++i) x[i] = first + i >= 0 && first + i < vocab ? base[(long long)v * kN + i] : lowest<T>();
+            r.v = *reinterpret_cast<const uint4*>(x);
+        }
+        return r;
+    }
+    // f(vector, its number) for the lane's vectors, four loads at a time; lanes beyond the end get one of nothing
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        for (int v0 = begin + lane_id(); v0 - lane_id() < end; v0 += 128) {
+            Vec<T> x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int v = v0 + i * 32;
+                if (v < end) x[i] = load(v);
+                else {
+                    T none[Vec<T>::kN];
+#pragma unroll
+                    for (int j = 0; j < Vec<T>::kN; ++j) none[j] = lowest<T>();
+                    x[i].v = *reinterpret_cast<const uint4*>(none);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v0 - lane_id() + i * 32 < end) f(x[i], v0 + i * 32);
+        }
+    }
 };
 
+struct SampleShared {
+    union {
+        struct { unsigned count[kBins], low[kBins], high[kBins], joined_count[kBins]; u64 joined_mass[kBins]; };   // the mass in halves of 16 bits
+        struct { unsigned key[kListMost]; int index[kListMost]; unsigned sorted[kListMost]; unsigned bins[kSampleThreads]; };
+    };
+    u64 warp_mass[kSampleWarps], seg_mass[kSampleWarps];
+    unsigned warp_count[kSampleWarps], seg_ties[kSampleWarps], warp_key[kSampleWarps], warp_low[kSampleWarps];
+    unsigned top_key, bound, candidates, before[kSampleCtas];
+    unsigned hit_bin, hit_count_above, pick_seg, pick_ties, kept, cut_key, cut_ties;
+    u64 hit_mass_above, pick_left, pick_total, list_mass;
+};
+
+__device__ __forceinline__ void warp_scan(unsigned& x) {
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) { const unsigned a = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane_id() >= d) x += a; }
+}
+__device__ __forceinline__ void warp_scan(u64& x) {
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) { const u64 a = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane_id() >= d) x += a; }
+}
+// inclusive sums over the CTA's threads, and the total; `part` is a word a warp of shared memory that is free
+template <typename N> __device__ __forceinline__ N cta_scan(N& x, N* part) {
+    warp_scan(x);
+    if (lane_id() == 31) part[warp_id()] = x;
+    __syncthreads();
+    N before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kSampleWarps; ++w) { const N p = part[w]; if (w < warp_id()) before += p; total += p; }
+    x += before;
+    __syncthreads();
+    return total;
+}
+
 // Where the running count (by_mass: mass) over the joined bins first reaches `need`: the bin, and what is above it.
-// `need` is at least 1 and at most the sum.
-__device__ void find_bin(SampleShared& s, u64 need, bool by_mass) {
+// `need` is at least 1 and at most the sum.  Returns the sums.
+__device__ void find_bin(SampleShared& s, u64 need, bool by_mass, unsigned* total = nullptr, u64* total_mass = nullptr) {
     constexpr int kPer = kBins / kSampleThreads;
-    const int first = threadIdx.x * kPer, lane = lane_id(), warp = warp_id();
+    const int first = threadIdx.x * kPer;
     unsigned c[kPer], n = 0;
     u64 m[kPer], mass = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        c[i] = s.joined_count[first + i];
-        m[i] = s.joined_mass[first + i];
-        n += c[i]; mass += m[i];
-    }
-    unsigned n_in = n;
-    u64 mass_in = mass;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const unsigned a = __shfl_up_sync(0xFFFFFFFFu, n_in, d);
-        const u64 b = __shfl_up_sync(0xFFFFFFFFu, mass_in, d);
-        if (lane >= d) { n_in += a; mass_in += b; }
-    }
-    if (lane == 31) { s.warp_count[warp] = n_in; s.warp_mass[warp] = mass_in; }
-    __syncthreads();
-    unsigned n_before = n_in - n;
-    u64 mass_before = mass_in - mass;
-    for (int w = 0; w < warp; ++w) { n_before += s.warp_count[w]; mass_before += s.warp_mass[w]; }
+    for (int i = 0; i < kPer; ++i) { c[i] = s.joined_count[first + i]; m[i] = s.joined_mass[first + i]; n += c[i]; mass += m[i]; }
+    unsigned n_before = n;
+    u64 mass_before = mass;
+    const unsigned all = cta_scan(n_before, s.warp_count);
+    const u64 all_mass = cta_scan(mass_before, s.warp_mass);
+    if (total) { *total = all; *total_mass = all_mass; }
+    n_before -= n; mass_before -= mass;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const u64 before = by_mass ? mass_before : n_before, here = by_mass ? m[i] : c[i];
-        if (before < need && need <= before + here) {
-            s.hit_bin = first + i; s.hit_count_above = n_before; s.hit_mass_above = mass_before;
-            s.hit_count = c[i]; s.hit_mass = m[i];
-        }
+        if (before < need && need <= before + here) { s.hit_bin = first + i; s.hit_count_above = n_before; s.hit_mass_above = mass_before; }
         n_before += c[i]; mass_before += m[i];
     }
     __syncthreads();
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) k_sample(const __grid_constant__ SampleParams p) {
+__global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_constant__ SampleParams p) {
     extern __shared__ __align__(16) unsigned char dyn[];
     SampleShared& s = *reinterpret_cast<SampleShared*>(dyn);
     cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const long long row = blockIdx.x / ctas;
     const int tid = threadIdx.x, lane = lane_id(), warp = warp_id();
+    constexpr int kN = Vec<T>::kN;
     pdl_trigger();
     pdl_wait();
 
-    // ---- the slice, into shared memory at its own offset within 16 bytes ----
-    const int slice = ((p.vocab + ctas - 1) / ctas + 7) / 8 * 8;
-    const int begin = min(rank * slice, p.vocab), n = min(slice, p.vocab - begin);
-    const T* src = static_cast<const T*>(p.logits) + row * p.ld + begin;
-    const int skew = (int)((reinterpret_cast<uintptr_t>(src) & 15u) / sizeof(T));
-    T* const x = reinterpret_cast<T*>(dyn + (sizeof(SampleShared) + 15) / 16 * 16) + skew;
-    {
-        constexpr int kVec = 16 / sizeof(T);
-        const int head = min(n, (kVec - skew) % kVec), body = (n - head) / kVec;
-        for (int i = tid; i < head; i += kSampleThreads) x[i] = src[i];
-        for (int i = tid; i < body; i += kSampleThreads)
-            reinterpret_cast<uint4*>(x + head)[i] = reinterpret_cast<const uint4*>(src + head)[i];
-        for (int i = head + body * kVec + tid; i < n; i += kSampleThreads) x[i] = src[i];
+    const T* const logits = static_cast<const T*>(p.logits) + row * p.ld;
+    Slice<T> x;
+    x.skew = (int)((reinterpret_cast<uintptr_t>(logits) & 15u) / sizeof(T));
+    x.base = logits - x.skew;
+    x.vocab = p.vocab;
+    {   // consecutive vectors for a CTA, and for a warp in it
+        const int all = (x.skew + p.vocab + kN - 1) / kN, share = (all + ctas * kSampleWarps - 1) / (ctas * kSampleWarps);
+        x.begin = min((rank * kSampleWarps + warp) * share, all);
+        x.end = min(x.begin + share, all);
     }
-    __syncthreads();
-
-    // ---- the largest logit ----
-    unsigned top_key = 0;
-    for (int i = tid; i < n; i += kSampleThreads) top_key = max(top_key, key_of(to_float(x[i])));
-    top_key = __reduce_max_sync(0xFFFFFFFFu, top_key);
-    if (lane == 0) s.warp_key[warp] = top_key;
-    __syncthreads();
-    if (warp == 0) {
-        top_key = __reduce_max_sync(0xFFFFFFFFu, s.warp_key[lane]);
-        if (lane == 0) s.top_key = top_key;
-    }
-    cluster.sync();
-    top_key = 0;
-    for (int c = 0; c < ctas; ++c) top_key = max(top_key, *cluster.map_shared_rank(&s.top_key, c));
-
-    Row r;
-    r.top = of_key(top_key);
     const float t = p.temperature ? p.temperature[row] : 1.f;
-    r.inv_t = 1.f / t;
-    r.min_p = p.min_p ? fminf(p.min_p[row], 1.f) : 0.f;
     int k = p.top_k ? p.top_k[row] : 0;
     if (k <= 0 || k >= p.vocab) k = 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f;
     const bool by_mass = top_p < 1.f;
-    const bool nothing = top_key <= kLowestKey;
+    const unsigned top_part = top_p > 0.f ? (unsigned)(fminf(top_p, 1.f) * 16777216.f) : 0u;
+    const float u = p.uniform[row];
+    const unsigned part = u > 0.f ? min((unsigned)(fminf(u, 1.f) * 16777216.f), 0xFFFFFFu) : 0u;
+    auto answer = [&](long long token, float prob) {
+        if (p.wide) static_cast<long long*>(p.tokens)[row] = token; else static_cast<int*>(p.tokens)[row] = (int)token;
+        if (p.prob) p.prob[row] = prob;
+    };
+
+    // ---- the largest logit; every thread's own, for the bound below ----
+    float mine = -INFINITY;
+    x.each([&](const Vec<T>& v, int) { mine = fmaxf(mine, v.largest()); });
+    const unsigned my_key = key_of(mine);
+    const unsigned wide_top = __reduce_max_sync(0xFFFFFFFFu, my_key);
+    const unsigned wide_low = __reduce_min_sync(0xFFFFFFFFu, my_key > kLowestKey ? my_key : 0xFFFFFFFFu);
+    if (lane == 0) { s.warp_key[warp] = wide_top; s.warp_low[warp] = wide_low; }
+    s.bins[tid] = 0;
+    __syncthreads();
+    unsigned top_key = 0, low_key = 0xFFFFFFFFu;
+#pragma unroll
+    for (int w = 0; w < kSampleWarps; ++w) { top_key = max(top_key, s.warp_key[w]); low_key = min(low_key, s.warp_low[w]); }
+    // ---- few candidates: a bound that at least ceil(k / ctas) of this CTA's threads reach; the least of the CTAs' bounds
+    //      is reached by k logits of the row ----
+    const bool short_row = p.vocab <= kListMost;
+    bool list = short_row ? k || by_mass : k > 0 && k <= kListRank * ctas;
+    if (list && !short_row) {
+        const unsigned want = (unsigned)((k + ctas - 1) / ctas);
+        const float hi = of_key(top_key), lo = of_key(low_key);
+        const float per = hi > lo && hi - lo < INFINITY ? (kSampleThreads - 1) / (hi - lo) : 0.f;
+        const unsigned bin = my_key > kLowestKey ? min((unsigned)((hi - mine) * per), (unsigned)kSampleThreads - 1) : 0xFFFFFFFFu;
+        if (bin < kSampleThreads) atomicAdd(&s.bins[bin], 1u);
+        if (tid == 0) s.hit_bin = kSampleThreads;               // (fewer threads than that have anything: no bound)
+        __syncthreads();
+        unsigned upto = s.bins[tid];
+        const unsigned here = upto;
+        cta_scan(upto, s.warp_count);
+        if (upto - here < want && want <= upto) s.hit_bin = tid;
+        __syncthreads();
+        const unsigned least = __reduce_min_sync(0xFFFFFFFFu, bin <= s.hit_bin ? my_key : 0xFFFFFFFFu);
+        if (lane == 0) s.warp_low[warp] = s.hit_bin < kSampleThreads ? least : kLowestKey + 1;
+        __syncthreads();
+        low_key = 0xFFFFFFFFu;
+#pragma unroll
+        for (int w = 0; w < kSampleWarps; ++w) low_key = min(low_key, s.warp_low[w]);
+    }
+    if (tid == 0) { s.top_key = top_key; s.bound = short_row ? kLowestKey + 1 : low_key; }
+    cluster.sync();
+    unsigned bound = 0xFFFFFFFFu;
+    top_key = 0;
+    for (int c = 0; c < ctas; ++c) {
+        top_key = max(top_key, *cluster.map_shared_rank(&s.top_key, c));
+        bound = min(bound, *cluster.map_shared_rank(&s.bound, c));
+    }
+
+    Weigh g;
+    g.top = of_key(top_key);
+    g.inv_t = 1.f / t;
+    g.min_p = p.min_p ? fminf(p.min_p[row], 1.f) : 0.f;
+    if (top_key <= kLowestKey) {                                // nothing left (everybody sees the same)
+        if (rank == 0 && tid == 0) answer(-1, 0.f);
+        cluster.sync();
+        return;
+    }
     const bool greedy = !(t > 0.f) || k == 1;
+    if (greedy) { list = false; g.inv_t = INFINITY; }
+
+    // ---- the candidates, in index order, in the first CTA's list ----
+    if (list) {
+        const float least = of_key(bound);
+        unsigned n = 0;
+        x.each([&](const Vec<T>& v, int) {
+            if (__any_sync(0xFFFFFFFFu, v.largest() >= least)) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) n += v.get(i) >= least;
+            }
+        });
+        unsigned warp_n = __reduce_add_sync(0xFFFFFFFFu, n);
+        if (lane == 0) s.warp_count[warp] = warp_n;
+        __syncthreads();
+        unsigned at = 0, here = 0;
+#pragma unroll
+        for (int w = 0; w < kSampleWarps; ++w) { if (w < warp) at += s.warp_count[w]; here += s.warp_count[w]; }
+        if (tid < ctas) cluster.map_shared_rank(&s, tid)->before[rank] = here;
+        cluster.sync();
+        unsigned total = 0;
+        for (int c = 0; c < ctas; ++c) { if (c < rank) at += s.before[c]; total += s.before[c]; }
+        list = total <= kListMost;
+        if (list) {
+            unsigned* const keys = cluster.map_shared_rank(s.key, 0);
+            int* const indices = cluster.map_shared_rank(s.index, 0);
+            if (warp_n)
+                x.each([&](const Vec<T>& v, int number) {
+                    if (!__any_sync(0xFFFFFFFFu, v.largest() >= least)) return;
+                    unsigned m = 0, upto;
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) m += v.get(i) >= least;
+                    upto = m;
+                    warp_scan(upto);
+                    unsigned to = at + upto - m;
+#pragma unroll
+                    for (int i = 0; i < kN; ++i)
+                        if (v.get(i) >= least) { keys[to] = key_of(v.get(i)); indices[to] = number * kN - x.skew + i; ++to; }
+                    at += __shfl_sync(0xFFFFFFFFu, upto, 31);
+                });
+            cluster.sync();
+            if (rank != 0) return;                              // the rest is the first CTA's, with nobody else's memory
+            const int count = (int)total;
+            // values in descending order (bitonic network over the next power of two)
+            int size = 64;
+            while (size < count) size *= 2;
+            for (int i = tid; i < size; i += kSampleThreads) s.sorted[i] = i < count ? s.key[i] : 0u;
+            __syncthreads();
+            for (int width = 2; width <= size; width *= 2)
+                for (int step = width / 2; step > 0; step /= 2) {
+                    for (int i = tid; i < size / 2; i += kSampleThreads) {
+                        const int a = 2 * i - (i & (step - 1)), b = a + step;
+                        const unsigned ka = s.sorted[a], kb = s.sorted[b];
+                        if ((ka < kb) == ((a & width) == 0)) { s.sorted[a] = kb; s.sorted[b] = ka; }
+                    }
+                    __syncthreads();
+                }
+            // how many of them the filters keep, and from that the value they keep down to and the count at it
+            const int limit = k ? min(k, count) : count;
+            const int i0 = tid * 2;
+            u64 w0 = 0, w1 = 0;
+            if (i0 < limit) w0 = Weigh::weight(g.e(s.sorted[i0]));
+            if (i0 + 1 < limit) w1 = Weigh::weight(g.e(s.sorted[i0 + 1]));
+            u64 upto = w0 + w1;
+            const u64 mass = cta_scan(upto, s.warp_mass);
+            int kept = limit;
+            if (by_mass) {
+                const u64 most = max(share(top_part, mass), (u64)1);
+                unsigned keep = (i0 < limit && upto - w1 - w0 < most) + (i0 + 1 < limit && upto - w1 < most);
+                kept = (int)cta_scan(keep, s.warp_count);
+            }
+            const unsigned cut = s.sorted[kept - 1];
+            unsigned ties = (i0 < kept && s.sorted[i0] == cut) + (i0 + 1 < kept && s.sorted[i0 + 1] == cut);
+            const unsigned cut_ties = cta_scan(ties, s.warp_count);
+            // the draw, in index order
+            unsigned same = 0;
+            unsigned key[2];
+            u64 w[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) { key[j] = i0 + j < count ? s.key[i0 + j] : 0u; same += key[j] == cut; }
+            unsigned same_upto = same;
+            cta_scan(same_upto, s.warp_count);
+            same_upto -= same;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                bool take = key[j] > cut;
+                if (key[j] == cut) take = same_upto++ < cut_ties;
+                if (take) {
+                    const float e = g.e(key[j]);
+                    if (e >= g.min_p) w[j] = Weigh::weight(e);
+                }
+            }
+            u64 run = w[0] + w[1];
+            const u64 sum = cta_scan(run, s.warp_mass), drawn = share(part, sum);
+            run -= w[0] + w[1];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (run <= drawn && drawn < run + w[j]) answer(s.index[i0 + j], (float)w[j] / (float)sum);
+                run += w[j];
+            }
+            return;
+        }
+        cluster.sync();                                         // the lists' memory becomes the histograms'
+    }
 
     // ---- the value the filters keep down to, and how many of the entries equal to it ----
     unsigned cut_key = 0, cut_ties = 0xFFFFFFFFu;
-    if (greedy) { cut_key = top_key; cut_ties = 1; r.inv_t = __int_as_float(0x7F800000); }
-    else if (!nothing && (k || by_mass)) {
+    if (greedy) { cut_key = top_key; cut_ties = 1; }
+    else if (k || by_mass) {
         constexpr int kShift = sizeof(T) == 2 ? 16 : 0;          // bf16 logits differ in the upper half of the key only
-        const float step = 1.f / (kBinsPerZ * r.inv_t);          // width of a bin in logits
+        const float step = 1.f / (kBinsPerZ * g.inv_t);          // width of a bin in logits
         auto histogram = [&](bool coarse, unsigned bin, unsigned hi, int shift) {
             for (int i = tid; i < kBins; i += kSampleThreads) { s.count[i] = 0; s.low[i] = 0; s.high[i] = 0; }
             __syncthreads();
-            for (int i = tid; i < n; i += kSampleThreads) {
-                const unsigned key = key_of(to_float(x[i]));
-                const float v = of_key(key), z = r.z(v);
-                if (!(z > kZeroWeight) || key <= kLowestKey) continue;
-                unsigned b = min((unsigned)(-z * kBinsPerZ), (unsigned)kBins - 1);
-                if (!coarse) {
-                    if (b != bin || (key >> kShift) > hi) continue;
-                    b = (hi - (key >> kShift)) >> shift;
-                    if (b >= kBins) continue;
+            x.each([&](const Vec<T>& v, int) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    const float f = v.get(i), z = g.z(f);
+                    if (!(z > kZeroWeight) || !(f > -INFINITY)) continue;
+                    unsigned b = min((unsigned)(-z * kBinsPerZ), (unsigned)kBins - 1);
+                    if (!coarse) {
+                        const unsigned key = key_of(f) >> kShift;
+                        if (b != bin || key > hi) continue;
+                        b = (hi - key) >> shift;
+                        if (b >= kBins) continue;
+                    }
+                    const unsigned w = Weigh::weight(expf(z));
+                    if (w == 0) continue;
+                    if (k) atomicAdd(&s.count[b], 1u);
+                    atomicAdd(&s.low[b], w & 0xFFFFu);
+                    if (w >> 16) atomicAdd(&s.high[b], w >> 16);
                 }
-                const unsigned w = Row::weight(expf(z));
-                if (w == 0) continue;
-                atomicAdd(&s.count[b], 1u);
-                atomicAdd(&s.low[b], w & 0xFFFFu);
-                atomicAdd(&s.high[b], w >> 16);
-            }
+            });
             cluster.sync();
             const int share_bins = kBins / ctas;
             for (int i = tid; i < share_bins; i += kSampleThreads) {
@@ -193,14 +411,14 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const __grid_constant
             cluster.sync();
         };
         // narrows the coarse bin in s.hit_* down to one key; `need` counts from the top of the row.  Leaves the sums
-        // above that key and at it.
+        // above that key.
         auto refine = [&](u64 need, bool mass, u64& mass_above, unsigned& count_above, unsigned& key) {
             const unsigned bin = s.hit_bin;
             mass_above = s.hit_mass_above; count_above = s.hit_count_above;
             // bounds of the bin's logits, a little wider than the roundings of z and of the bin number can move them
             const float near = bin ? (float)bin * step * (1.f - 0x1p-20f) : 0.f, far = (float)(bin + 1) * step * (1.f + 0x1p-20f);
-            unsigned hi = min(top_key, key_of(__fsub_ru(r.top, near))) >> kShift;
-            unsigned lo = key_of(bin == kBins - 1 ? -INFINITY : __fsub_rd(r.top, far)) >> kShift;
+            unsigned hi = min(top_key, key_of(__fsub_ru(g.top, near))) >> kShift;
+            unsigned lo = key_of(bin == kBins - 1 ? -INFINITY : __fsub_rd(g.top, far)) >> kShift;
             for (;;) {
                 int shift = 0;
                 while ((hi - lo) >> shift >= kBins) ++shift;
@@ -216,124 +434,108 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const __grid_constant
             key = kShift == 0 ? hi : hi << kShift | (hi >> 15 ? 0u : 0xFFFFu);   // a negative number's bits are inverted
         };
         histogram(true, 0, 0, 0);
-        unsigned total = 0;
-        u64 total_mass = 0;
-        {   // sums over all bins: the last thread's running sums in find_bin would do, but the filters may not ask for it
-            find_bin(s, 1, false);
-            for (int w = 0; w < kSampleWarps; ++w) { total += s.warp_count[w]; total_mass += s.warp_mass[w]; }
-            __syncthreads();
-        }
-        u64 kept_mass = total_mass;
-        u64 mass_above;
-        unsigned count_above;
+        unsigned total, count_above;
+        u64 kept_mass, mass_above;
+        find_bin(s, k ? (u64)k : 1, k == 0, &total, &kept_mass);
         if (k && (unsigned)k < total) {                           // fewer weights above zero than k: k keeps them all
-            find_bin(s, k, false);
             refine(k, false, mass_above, count_above, cut_key);
             cut_ties = k - count_above;
-            const unsigned w = Row::weight(expf(r.z(of_key(cut_key))));
-            kept_mass = mass_above + (u64)cut_ties * w;
+            kept_mass = mass_above + (u64)cut_ties * Weigh::weight(g.e(cut_key));
         }
         if (by_mass) {
-            const unsigned part = top_p > 0.f ? (unsigned)(top_p * 16777216.f) : 0u;
-            const u64 upto = max(share(part, kept_mass), (u64)1);
-            if (cut_key) { __syncthreads(); histogram(true, 0, 0, 0); }
+            const u64 upto = max(share(top_part, kept_mass), (u64)1);
+            __syncthreads();
+            if (cut_key) histogram(true, 0, 0, 0);
             find_bin(s, upto, true);
             unsigned key;
             refine(upto, true, mass_above, count_above, key);
-            const unsigned w = Row::weight(expf(r.z(of_key(key))));
+            const unsigned w = Weigh::weight(g.e(key));
             const u64 ties = (upto - mass_above + w - 1) / w;
             if (key > cut_key) { cut_key = key; cut_ties = (unsigned)min(ties, (u64)0xFFFFFFFFu); }
             else cut_ties = (unsigned)min(ties, (u64)cut_ties);
         }
     }
 
-    // ---- kept mass of every warp's segment (consecutive entries), in index order ----
-    const int seg_len = ((slice + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32;
-    const int seg_begin = min(warp * seg_len, n), seg_end = min(seg_begin + seg_len, n);
-    const float cut_e = expf(r.z(of_key(cut_key)));
-    const unsigned cut_w = cut_key && cut_e >= r.min_p ? Row::weight(cut_e) : 0u;
-    auto kept = [&](int i, unsigned& key) {                       // weight of an entry above the cut
-        key = key_of(to_float(x[i]));
-        if (key <= max(cut_key, kLowestKey)) return 0u;
-        const float e = expf(r.z(of_key(key)));
-        return e >= r.min_p ? Row::weight(e) : 0u;
+    // ---- kept mass of every warp's vectors (consecutive entries), in index order ----
+    const float cut_e = g.e(cut_key), least = cut_key > kLowestKey ? of_key(cut_key) : -INFINITY;
+    const unsigned cut_w = cut_key && cut_e >= g.min_p ? Weigh::weight(cut_e) : 0u;
+    auto kept = [&](float f) {                                    // weight of an entry above the cut
+        if (!(f > least)) return 0u;
+        const float z = g.z(f);
+        if (!(z > kZeroWeight)) return 0u;
+        const float e = expf(z);
+        return e >= g.min_p ? Weigh::weight(e) : 0u;
     };
     {
         u64 mass = 0;
         unsigned ties = 0;
-        for (int i = seg_begin + lane; i < seg_end; i += 32) {
-            unsigned key;
-            mass += kept(i, key);
-            ties += key == cut_key;
-        }
+        x.each([&](const Vec<T>& v, int) {
+            if (!(v.largest() >= least)) return;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) { mass += kept(v.get(i)); ties += v.get(i) == least; }
+        });
 #pragma unroll
         for (int d = 16; d; d >>= 1) { mass += __shfl_xor_sync(0xFFFFFFFFu, mass, d); ties += __shfl_xor_sync(0xFFFFFFFFu, ties, d); }
-        if (lane == 0) { s.seg_mass[warp] = mass; s.seg_ties[warp] = ties; }
+        if (lane == 0) { s.seg_mass[warp] = mass; s.seg_ties[warp] = cut_key ? ties : 0u; }
     }
     cluster.sync();
-    // ---- the segment the drawn number falls into ----
+    // ---- the warp whose entries the drawn number falls into ----
     {
-        const int segs = ctas * kSampleWarps;
         u64 mass = 0, upto;
-        unsigned ties = 0, ties_upto;
-        if (tid < segs) {
+        unsigned ties = 0, ties_before;
+        if (tid < ctas * kSampleWarps) {
             mass = *cluster.map_shared_rank(&s.seg_mass[tid % kSampleWarps], tid / kSampleWarps);
             ties = *cluster.map_shared_rank(&s.seg_ties[tid % kSampleWarps], tid / kSampleWarps);
         }
-        ties_upto = ties;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) { const unsigned a = __shfl_up_sync(0xFFFFFFFFu, ties_upto, d); if (lane >= d) ties_upto += a; }
-        if (lane == 31) s.warp_count[warp] = ties_upto;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) ties_upto += s.warp_count[w];
-        const unsigned ties_before = ties_upto - ties;
-        const unsigned ties_kept = ties_before >= cut_ties ? 0u : min(ties, cut_ties - ties_before);
-        mass += (u64)ties_kept * cut_w;
+        ties_before = ties;
+        cta_scan(ties_before, s.warp_count);
+        ties_before -= ties;
+        mass += (u64)(ties_before >= cut_ties ? 0u : min(ties, cut_ties - ties_before)) * cut_w;
         upto = mass;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) { const u64 a = __shfl_up_sync(0xFFFFFFFFu, upto, d); if (lane >= d) upto += a; }
-        if (lane == 31) s.warp_mass[warp] = upto;
-        __syncthreads();
-        u64 total = 0;
-        for (int w = 0; w < kSampleWarps; ++w) { if (w == warp) upto += total; total += s.warp_mass[w]; }
-        const float u = p.uniform[row];
-        const unsigned part = u > 0.f ? min((unsigned)(u * 16777216.f), 0xFFFFFFu) : 0u;
-        const u64 at = share(part, total);
-        if (mass && upto - mass <= at && at < upto) {
-            s.pick_seg = tid; s.pick_left = at - (upto - mass); s.pick_ties = ties_before; s.pick_total = total;
-        }
+        const u64 total = cta_scan(upto, s.warp_mass), at = share(part, total);
+        if (upto - mass <= at && at < upto) { s.pick_seg = tid; s.pick_left = at - (upto - mass); s.pick_ties = ties_before; s.pick_total = total; }
         __syncthreads();
     }
-    // ---- and the entry in it ----
-    if (nothing) {
-        if (rank == 0 && tid == 0) {
-            if (p.wide) static_cast<long long*>(p.tokens)[row] = -1; else static_cast<int*>(p.tokens)[row] = -1;
-            if (p.prob) p.prob[row] = 0.f;
-        }
-    } else if (s.pick_seg == (unsigned)(rank * kSampleWarps + warp)) {
+    // ---- and the entry among them ----
+    if (s.pick_seg == (unsigned)(rank * kSampleWarps + warp)) {
         u64 left = s.pick_left;
         unsigned ties = s.pick_ties;
-        for (int i0 = seg_begin; i0 < seg_end; i0 += 32) {
-            const int i = i0 + lane;
-            unsigned key = 0, w = 0;
-            if (i < seg_end) w = kept(i, key);
-            const unsigned same = __ballot_sync(0xFFFFFFFFu, i < seg_end && key == cut_key);
-            if (i < seg_end && key == cut_key && ties + __popc(same & ((1u << lane) - 1u)) < cut_ties) w = cut_w;
-            ties += __popc(same);
-            u64 upto = w;
+        bool found = false;
+        x.each([&](const Vec<T>& v, int number) {
+            if (found || !__any_sync(0xFFFFFFFFu, v.largest() >= least)) return;
+            unsigned same = 0, w[kN];
+            if (cut_key)
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) { const u64 a = __shfl_up_sync(0xFFFFFFFFu, upto, d); if (lane >= d) upto += a; }
+                for (int i = 0; i < kN; ++i) same += v.get(i) == least;
+            unsigned same_upto = same;
+            warp_scan(same_upto);
+            unsigned rank_of = ties + same_upto - same;
+            u64 mass = 0;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                w[i] = kept(v.get(i));
+                if (cut_key && v.get(i) == least && rank_of++ < cut_ties) w[i] = cut_w;
+                mass += w[i];
+            }
+            ties += __shfl_sync(0xFFFFFFFFu, same_upto, 31);
+            u64 upto = mass;
+            warp_scan(upto);
             const unsigned over = __ballot_sync(0xFFFFFFFFu, upto > left);
             if (over) {
+                found = true;
                 if (lane == __ffs(over) - 1) {
-                    const long long token = begin + i;
-                    if (p.wide) static_cast<long long*>(p.tokens)[row] = token; else static_cast<int*>(p.tokens)[row] = (int)token;
-                    if (p.prob) p.prob[row] = (float)w / (float)s.pick_total;
+                    u64 run = upto - mass;
+                    bool open = true;
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) {
+                        run += w[i];
+                        if (open && run > left) { open = false; answer((long long)number * kN - x.skew + i, (float)w[i] / (float)s.pick_total); }
+                    }
                 }
-                break;
+                return;
             }
             left -= __shfl_sync(0xFFFFFFFFu, upto, 31);
-        }
+        });
     }
     cluster.sync();                                               // nobody leaves while its shared memory is read
 }
@@ -341,16 +543,14 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const __grid_constant
 template <typename T>
 static cudaError_t sample_t(const SampleParams& p, int sms, cudaStream_t stream) {
     static SmemOptIn opt;
-    // CTAs a row: as many as the machine has SMs for, and enough for a slice to fit the shared memory
+    // CTAs a row: as many as fill the machine without a second round of CTAs (two share an SM), each with 2048 entries at least
     int ctas = 1;
-    const size_t fixed = (sizeof(SampleShared) + 15) / 16 * 16 + 32, most = 227 * 1024;
-    auto bytes = [&](int c) { return fixed + size_t(((p.vocab + c - 1) / c + 7) / 8 * 8) * sizeof(T); };
-    while (ctas < kSampleCtas && (bytes(ctas) > most || p.vocab > kSampleSlice * ctas || (p.rows * ctas * 2 <= sms && p.vocab > 2048 * ctas))) ctas *= 2;
-    const size_t smem = bytes(ctas);
-    const cudaError_t e = ensure_dynamic_smem(k_sample<T>, smem, opt);
+    while (ctas < kSampleCtas && p.rows * ctas * 2 <= sms && p.vocab > 2048 * ctas) ctas *= 2;
+    while (p.vocab > kSampleSlice * ctas) ctas *= 2;
+    const cudaError_t e = ensure_dynamic_smem(k_sample<T>, sizeof(SampleShared), opt);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.rows * ctas)); cfg.blockDim = dim3(kSampleThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.gridDim = dim3((unsigned)(p.rows * ctas)); cfg.blockDim = dim3(kSampleThreads); cfg.dynamicSmemBytes = sizeof(SampleShared); cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -5,8 +5,8 @@
 // its order, and a row may be split in any way.
 //
 // Few candidates (top-k up to some hundred, or a short row): every thread's largest logit gives a bound that at least
-// k logits reach; the few that do are collected in index order, their values sorted, and all that follows is on that list: the
-// row is read twice, with a few instructions an entry.
+// k logits reach; the few that do are collected, their values and their indices sorted, and all that follows is on that
+// list: the row is read twice, with a few instructions an entry.
 // Otherwise: a histogram over equal steps of the scaled logit finds the step in which top-k's count, or top-p's mass, is
 // reached, finer histograms over the bits of the logit narrow the step down to one value, and a last pass sums what is
 // kept in index order.
@@ -24,7 +24,7 @@ constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleCtas = 8;               // of a cluster, at most
 constexpr int kBins = 2048;
-constexpr int kListMost = 1024;              // candidates that are worked on as a list (twice the threads)
+constexpr int kListMost = 1024;              // candidates that are worked on as a list (twice the threads; a place in it has 10 bits)
 constexpr int kListRank = 384;               // top-k for each CTA of a row up to which the threads' maxima bound it well
 constexpr float kZeroWeight = -22.25f;       // below this z the weight rounds to zero (2^31 e^z < 1/2 below -22.18)
 constexpr float kBinsPerZ = kBins / 22.25f;
@@ -56,14 +56,27 @@ template <typename T> struct Vec {
     static constexpr int kN = 16 / sizeof(T);
     uint4 v;
     __device__ __forceinline__ float get(int i) const;
-    __device__ __forceinline__ float largest() const;
+    __device__ __forceinline__ float largest() const;                // (the maximum of a NaN and a number is the number)
+    __device__ __forceinline__ void raise(const Vec& o);            // to the larger, entry by entry
+    static __device__ __forceinline__ Vec nothing();
 };
 template <> __device__ __forceinline__ float Vec<float>::get(int i) const { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
 template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::get(int i) const {
     const unsigned w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
     return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
 }
-// (the maximum of a NaN and a number is the number)
+template <> __device__ __forceinline__ Vec<float> Vec<float>::nothing() { return Vec{make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u)}; }
+template <> __device__ __forceinline__ Vec<__nv_bfloat16> Vec<__nv_bfloat16>::nothing() { return Vec{make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u)}; }
+template <> __device__ __forceinline__ void Vec<float>::raise(const Vec& o) {
+    v.x = __float_as_uint(fmaxf(get(0), o.get(0))); v.y = __float_as_uint(fmaxf(get(1), o.get(1)));
+    v.z = __float_as_uint(fmaxf(get(2), o.get(2))); v.w = __float_as_uint(fmaxf(get(3), o.get(3)));
+}
+template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::raise(const Vec& o) {
+    __nv_bfloat162* a = reinterpret_cast<__nv_bfloat162*>(&v);
+    const __nv_bfloat162* b = reinterpret_cast<const __nv_bfloat162*>(&o.v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __hmax2(a[i], b[i]);
+}
 template <> __device__ __forceinline__ float Vec<float>::largest() const { return fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))); }
 template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::largest() const {
     const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
@@ -82,33 +95,32 @@ template <typename T> struct Slice {
         constexpr int kN = Vec<T>::kN;
         Vec<T> r;
         const int first = v * kN - skew;
-        if (first >= 0 && first + kN <= vocab) r.v = *reinterpret_cast<const uint4*>(base + (long long)v * kN);
+        if (first >= 0 && first + kN <= vocab && v < end) r.v = *reinterpret_cast<const uint4*>(base + (long long)v * kN);
         else {
             T x[kN];
 #pragma unroll
-            for (int i = 0; i < kN; ++i) x[i] = first + i >= 0 && first + i < vocab ? base[(long long)v * kN + i] : lowest<T>();
+            for (int i = 0; i < kN; ++i) x[i] = first + i >= 0 && first + i < vocab && v < end ? base[(long long)v * kN + i] : lowest<T>();
             r.v = *reinterpret_cast<const uint4*>(x);
         }
         return r;
     }
-    // f(vector, its number) for the lane's vectors, four loads at a time; lanes beyond the end get one of nothing
+    // f(vector, its number) for the lane's vectors, four loads at a time; where the warp's 128 are not all whole, one at a
+    // time, and lanes beyond the end get a vector of nothing (f may use the whole warp)
     template <typename F> __device__ __forceinline__ void each(F f) const {
-        for (int v0 = begin + lane_id(); v0 - lane_id() < end; v0 += 128) {
-            Vec<T> x[4];
+        constexpr int kN = Vec<T>::kN;
+        for (int v0 = begin; v0 < end; v0 += 128) {
+            const int v = v0 + lane_id();
+            if (v0 * kN >= skew && v0 + 128 <= end && (v0 + 128) * kN - skew <= vocab) {
+                const T* const from = base + (long long)v * kN;
+                Vec<T> x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int v = v0 + i * 32;
-                if (v < end) x[i] = load(v);
-                else {
-                    T none[Vec<T>::kN];
+                for (int i = 0; i < 4; ++i) x[i].v = *reinterpret_cast<const uint4*>(from + i * 32 * kN);
 #pragma unroll
-                    for (int j = 0; j < Vec<T>::kN; ++j) none[j] = lowest<T>();
-                    x[i].v = *reinterpret_cast<const uint4*>(none);
-                }
+                for (int i = 0; i < 4; ++i) f(x[i], v + i * 32);
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < 4 && v0 + i * 32 < end; ++i) f(load(v + i * 32), v + i * 32);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (v0 - lane_id() + i * 32 < end) f(x[i], v0 + i * 32);
         }
     }
 };
@@ -116,11 +128,11 @@ template <typename T> struct Slice {
 struct SampleShared {
     union {
         struct { unsigned count[kBins], low[kBins], high[kBins], joined_count[kBins]; u64 joined_mass[kBins]; };   // the mass in halves of 16 bits
-        struct { unsigned key[kListMost]; int index[kListMost]; unsigned sorted[kListMost]; unsigned bins[kSampleThreads]; };
+        struct { unsigned key[kListMost], sorted[kListMost], order[kListMost], bins[kSampleThreads]; };
     };
     u64 warp_mass[kSampleWarps], seg_mass[kSampleWarps];
     unsigned warp_count[kSampleWarps], seg_ties[kSampleWarps], warp_key[kSampleWarps], warp_low[kSampleWarps];
-    unsigned top_key, bound, candidates, before[kSampleCtas];
+    unsigned top_key, bound, candidates;
     unsigned hit_bin, hit_count_above, pick_seg, pick_ties, kept, cut_key, cut_ties;
     u64 hit_mass_above, pick_left, pick_total, list_mass;
 };
@@ -200,14 +212,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     const unsigned top_part = top_p > 0.f ? (unsigned)(fminf(top_p, 1.f) * 16777216.f) : 0u;
     const float u = p.uniform[row];
     const unsigned part = u > 0.f ? min((unsigned)(fminf(u, 1.f) * 16777216.f), 0xFFFFFFu) : 0u;
+    auto sync = [&] { if (ctas == 1) __syncthreads(); else cluster.sync(); };
     auto answer = [&](long long token, float prob) {
         if (p.wide) static_cast<long long*>(p.tokens)[row] = token; else static_cast<int*>(p.tokens)[row] = (int)token;
         if (p.prob) p.prob[row] = prob;
     };
 
     // ---- the largest logit; every thread's own, for the bound below ----
-    float mine = -INFINITY;
-    x.each([&](const Vec<T>& v, int) { mine = fmaxf(mine, v.largest()); });
+    Vec<T> most = Vec<T>::nothing();
+    x.each([&](const Vec<T>& v, int) { most.raise(v); });
+    const float mine = fmaxf(most.largest(), -INFINITY);
     const unsigned my_key = key_of(mine);
     const unsigned wide_top = __reduce_max_sync(0xFFFFFFFFu, my_key);
     const unsigned wide_low = __reduce_min_sync(0xFFFFFFFFu, my_key > kLowestKey ? my_key : 0xFFFFFFFFu);
@@ -241,8 +255,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
 #pragma unroll
         for (int w = 0; w < kSampleWarps; ++w) low_key = min(low_key, s.warp_low[w]);
     }
-    if (tid == 0) { s.top_key = top_key; s.bound = short_row ? kLowestKey + 1 : low_key; }
-    cluster.sync();
+    if (tid == 0) { s.candidates = 0; s.top_key = top_key; s.bound = short_row ? kLowestKey + 1 : low_key; }
+    sync();
     unsigned bound = 0xFFFFFFFFu;
     top_key = 0;
     for (int c = 0; c < ctas; ++c) {
@@ -256,64 +270,48 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     g.min_p = p.min_p ? fminf(p.min_p[row], 1.f) : 0.f;
     if (top_key <= kLowestKey) {                                // nothing left (everybody sees the same)
         if (rank == 0 && tid == 0) answer(-1, 0.f);
-        cluster.sync();
+        sync();
         return;
     }
     const bool greedy = !(t > 0.f) || k == 1;
     if (greedy) { list = false; g.inv_t = INFINITY; }
 
-    // ---- the candidates, in index order, in the first CTA's list ----
+    // ---- the candidates, in the first CTA's list: their keys, and their indices with their places in it ----
     if (list) {
         const float least = of_key(bound);
-        unsigned n = 0;
-        x.each([&](const Vec<T>& v, int) {
-            if (__any_sync(0xFFFFFFFFu, v.largest() >= least)) {
+        SampleShared* const first = cluster.map_shared_rank(&s, 0);
+        x.each([&](const Vec<T>& v, int number) {
+            if (!(v.largest() >= least)) return;
+            const int index = number * kN - x.skew;
 #pragma unroll
-                for (int i = 0; i < kN; ++i) n += v.get(i) >= least;
-            }
+            for (int i = 0; i < kN; ++i)
+                if (v.get(i) >= least) {
+                    const unsigned to = atomicAdd(&first->candidates, 1u);
+                    if (to < kListMost) { first->key[to] = key_of(v.get(i)); first->order[to] = (unsigned)(index + i) << 10 | to; }
+                }
         });
-        unsigned warp_n = __reduce_add_sync(0xFFFFFFFFu, n);
-        if (lane == 0) s.warp_count[warp] = warp_n;
-        __syncthreads();
-        unsigned at = 0, here = 0;
-#pragma unroll
-        for (int w = 0; w < kSampleWarps; ++w) { if (w < warp) at += s.warp_count[w]; here += s.warp_count[w]; }
-        if (tid < ctas) cluster.map_shared_rank(&s, tid)->before[rank] = here;
-        cluster.sync();
-        unsigned total = 0;
-        for (int c = 0; c < ctas; ++c) { if (c < rank) at += s.before[c]; total += s.before[c]; }
+        sync();
+        const unsigned total = first->candidates;
         list = total <= kListMost;
+        sync();                                                 // (everybody has read it; the lists' memory may become the histograms')
         if (list) {
-            unsigned* const keys = cluster.map_shared_rank(s.key, 0);
-            int* const indices = cluster.map_shared_rank(s.index, 0);
-            if (warp_n)
-                x.each([&](const Vec<T>& v, int number) {
-                    if (!__any_sync(0xFFFFFFFFu, v.largest() >= least)) return;
-                    unsigned m = 0, upto;
-#pragma unroll
-                    for (int i = 0; i < kN; ++i) m += v.get(i) >= least;
-                    upto = m;
-                    warp_scan(upto);
-                    unsigned to = at + upto - m;
-#pragma unroll
-                    for (int i = 0; i < kN; ++i)
-                        if (v.get(i) >= least) { keys[to] = key_of(v.get(i)); indices[to] = number * kN - x.skew + i; ++to; }
-                    at += __shfl_sync(0xFFFFFFFFu, upto, 31);
-                });
-            cluster.sync();
             if (rank != 0) return;                              // the rest is the first CTA's, with nobody else's memory
             const int count = (int)total;
-            // values in descending order (bitonic network over the next power of two)
+            // keys in descending order, indices in ascending order: one bitonic network over the next power of two for both
             int size = 64;
             while (size < count) size *= 2;
-            for (int i = tid; i < size; i += kSampleThreads) s.sorted[i] = i < count ? s.key[i] : 0u;
+            for (int i = tid; i < size; i += kSampleThreads) {
+                s.sorted[i] = i < count ? s.key[i] : 0u;
+                if (i >= count) s.order[i] = 0xFFFFFFFFu;
+            }
             __syncthreads();
             for (int width = 2; width <= size; width *= 2)
                 for (int step = width / 2; step > 0; step /= 2) {
-                    for (int i = tid; i < size / 2; i += kSampleThreads) {
-                        const int a = 2 * i - (i & (step - 1)), b = a + step;
-                        const unsigned ka = s.sorted[a], kb = s.sorted[b];
-                        if ((ka < kb) == ((a & width) == 0)) { s.sorted[a] = kb; s.sorted[b] = ka; }
+                    for (int i = tid; i < size; i += kSampleThreads) {
+                        const int pair = i & (size / 2 - 1), a = 2 * pair - (pair & (step - 1)), b = a + step;
+                        unsigned* const list_of = i < size / 2 ? s.sorted : s.order;
+                        const unsigned flip = i < size / 2 ? 0u : 0xFFFFFFFFu, va = list_of[a], vb = list_of[b];
+                        if (((va ^ flip) < (vb ^ flip)) == ((a & width) == 0)) { list_of[a] = vb; list_of[b] = va; }
                     }
                     __syncthreads();
                 }
@@ -339,7 +337,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
             unsigned key[2];
             u64 w[2] = {0, 0};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) { key[j] = i0 + j < count ? s.key[i0 + j] : 0u; same += key[j] == cut; }
+            for (int j = 0; j < 2; ++j) { key[j] = i0 + j < count ? s.key[s.order[i0 + j] & 1023u] : 0u; same += key[j] == cut; }
             unsigned same_upto = same;
             cta_scan(same_upto, s.warp_count);
             same_upto -= same;
@@ -357,12 +355,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
             run -= w[0] + w[1];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                if (run <= drawn && drawn < run + w[j]) answer(s.index[i0 + j], (float)w[j] / (float)sum);
+                if (run <= drawn && drawn < run + w[j]) answer(s.order[i0 + j] >> 10, (float)w[j] / (float)sum);
                 run += w[j];
             }
             return;
         }
-        cluster.sync();                                         // the lists' memory becomes the histograms'
     }
 
     // ---- the value the filters keep down to, and how many of the entries equal to it ----
@@ -393,7 +390,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
                     if (w >> 16) atomicAdd(&s.high[b], w >> 16);
                 }
             });
-            cluster.sync();
+            sync();
             const int share_bins = kBins / ctas;
             for (int i = tid; i < share_bins; i += kSampleThreads) {
                 const int at = rank * share_bins + i;
@@ -408,7 +405,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
                     *cluster.map_shared_rank(&s.joined_mass[at], c) = m;
                 }
             }
-            cluster.sync();
+            sync();
         };
         // narrows the coarse bin in s.hit_* down to one key; `need` counts from the top of the row.  Leaves the sums
         // above that key.
@@ -478,7 +475,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         for (int d = 16; d; d >>= 1) { mass += __shfl_xor_sync(0xFFFFFFFFu, mass, d); ties += __shfl_xor_sync(0xFFFFFFFFu, ties, d); }
         if (lane == 0) { s.seg_mass[warp] = mass; s.seg_ties[warp] = cut_key ? ties : 0u; }
     }
-    cluster.sync();
+    sync();
     // ---- the warp whose entries the drawn number falls into ----
     {
         u64 mass = 0, upto;
@@ -537,7 +534,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
             left -= __shfl_sync(0xFFFFFFFFu, upto, 31);
         });
     }
-    cluster.sync();                                               // nobody leaves while its shared memory is read
+    sync();                                               // nobody leaves while its shared memory is read
 }
 
 template <typename T>

@@ -28,7 +28,7 @@ constexpr int kListMost = 1024;              // candidates that are worked on as
 constexpr int kListRank = 384;               // top-k for each CTA of a row up to which the threads' maxima bound it well
 constexpr float kZeroWeight = -22.25f;       // below this z the weight rounds to zero (2^31 e^z < 1/2 below -22.18)
 constexpr float kBinsPerZ = kBins / 22.25f;
-constexpr int kSampleSlice = 49152;          // entries a CTA takes, about: its sums of 16-bit halves stay within 32 bits
+constexpr int kSampleSlice = 65536;          // entries a CTA takes, at most: its sums of 16-bit halves stay within 32 bits
 constexpr unsigned kLowestKey = 0x007FFFFFu; // key of -infinity
 
 // order-preserving bits of a float; equal floats (the two zeros) have equal keys, NaN counts as -infinity
@@ -104,37 +104,43 @@ template <typename T> struct Slice {
         }
         return r;
     }
-    // f(vector, its number) for the lane's vectors, four loads at a time; where the warp's 128 are not all whole, one at a
-    // time, and lanes beyond the end get a vector of nothing (f may use the whole warp)
-    template <typename F> __device__ __forceinline__ void each(F f) const {
+    // f(four vectors, 32 apart, the first one's number) for the lane's vectors; what lies outside is -infinity, and f may
+    // use the whole warp
+    template <typename F> __device__ __forceinline__ void groups(F f) const {
         constexpr int kN = Vec<T>::kN;
         for (int v0 = begin; v0 < end; v0 += 128) {
             const int v = v0 + lane_id();
+            Vec<T> x[4];
             if (v0 * kN >= skew && v0 + 128 <= end && (v0 + 128) * kN - skew <= vocab) {
                 const T* const from = base + (long long)v * kN;
-                Vec<T> x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i].v = *reinterpret_cast<const uint4*>(from + i * 32 * kN);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f(x[i], v + i * 32);
             } else {
-#pragma unroll 1
-                for (int i = 0; i < 4 && v0 + i * 32 < end; ++i) f(load(v + i * 32), v + i * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = load(v + i * 32);
             }
+            f(x, v);
         }
+    }
+    // f(vector, its number), one at a time
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        groups([&](const Vec<T> (&x)[4], int v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f(x[i], v + i * 32);
+        });
     }
 };
 
 struct SampleShared {
     union {
         struct { unsigned count[kBins], low[kBins], high[kBins], joined_count[kBins]; u64 joined_mass[kBins]; };   // the mass in halves of 16 bits
-        struct { unsigned key[kListMost], sorted[kListMost], order[kListMost], bins[kSampleThreads]; };
+        struct { unsigned key[kListMost], order[kListMost], bins[kSampleThreads]; uint2 sorted[kListMost], spare[kListMost]; };
     };
     u64 warp_mass[kSampleWarps], seg_mass[kSampleWarps];
     unsigned warp_count[kSampleWarps], seg_ties[kSampleWarps], warp_key[kSampleWarps], warp_low[kSampleWarps];
     unsigned top_key, bound, candidates;
-    unsigned hit_bin, hit_count_above, pick_seg, pick_ties, kept, cut_key, cut_ties;
-    u64 hit_mass_above, pick_left, pick_total, list_mass;
+    unsigned hit_bin, hit_count_above, pick_seg, pick_ties, cut_key;
+    u64 hit_mass_above, pick_left, pick_total;
 };
 
 __device__ __forceinline__ void warp_scan(unsigned& x) {
@@ -159,7 +165,7 @@ template <typename N> __device__ __forceinline__ N cta_scan(N& x, N* part) {
 }
 
 // Where the running count (by_mass: mass) over the joined bins first reaches `need`: the bin, and what is above it.
-// `need` is at least 1 and at most the sum.  Returns the sums.
+// `need` is at most the sum (0: no bin is looked for).
 __device__ void find_bin(SampleShared& s, u64 need, bool by_mass, unsigned* total = nullptr, u64* total_mass = nullptr) {
     constexpr int kPer = kBins / kSampleThreads;
     const int first = threadIdx.x * kPer;
@@ -232,30 +238,39 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
 #pragma unroll
     for (int w = 0; w < kSampleWarps; ++w) { top_key = max(top_key, s.warp_key[w]); low_key = min(low_key, s.warp_low[w]); }
     // ---- few candidates: a bound that at least ceil(k / ctas) of this CTA's threads reach; the least of the CTAs' bounds
-    //      is reached by k logits of the row ----
+    //      is reached by k logits of the row.  It is the lower edge of a bin of the threads' maxima: every warp finds it
+    //      for itself ----
     const bool short_row = p.vocab <= kListMost;
     bool list = short_row ? k || by_mass : k > 0 && k <= kListRank * ctas;
+    unsigned edge = kLowestKey + 1;
     if (list && !short_row) {
         const unsigned want = (unsigned)((k + ctas - 1) / ctas);
         const float hi = of_key(top_key), lo = of_key(low_key);
         const float per = hi > lo && hi - lo < INFINITY ? (kSampleThreads - 1) / (hi - lo) : 0.f;
-        const unsigned bin = my_key > kLowestKey ? min((unsigned)((hi - mine) * per), (unsigned)kSampleThreads - 1) : 0xFFFFFFFFu;
-        if (bin < kSampleThreads) atomicAdd(&s.bins[bin], 1u);
-        if (tid == 0) s.hit_bin = kSampleThreads;               // (fewer threads than that have anything: no bound)
+        if (my_key > kLowestKey) atomicAdd(&s.bins[per > 0.f ? min((unsigned)((hi - mine) * per), (unsigned)kSampleThreads - 1) : 0u], 1u);
         __syncthreads();
-        unsigned upto = s.bins[tid];
-        const unsigned here = upto;
-        cta_scan(upto, s.warp_count);
-        if (upto - here < want && want <= upto) s.hit_bin = tid;
-        __syncthreads();
-        const unsigned least = __reduce_min_sync(0xFFFFFFFFu, bin <= s.hit_bin ? my_key : 0xFFFFFFFFu);
-        if (lane == 0) s.warp_low[warp] = s.hit_bin < kSampleThreads ? least : kLowestKey + 1;
-        __syncthreads();
-        low_key = 0xFFFFFFFFu;
+        constexpr int kPer = kSampleThreads / 32;
+        unsigned c[kPer], sum = 0, upto;
 #pragma unroll
-        for (int w = 0; w < kSampleWarps; ++w) low_key = min(low_key, s.warp_low[w]);
+        for (int i = 0; i < kPer; i += 4) {
+            const uint4 four = *reinterpret_cast<const uint4*>(&s.bins[lane * kPer + i]);
+            c[i] = four.x; c[i + 1] = four.y; c[i + 2] = four.z; c[i + 3] = four.w;
+            sum += four.x + four.y + four.z + four.w;
+        }
+        upto = sum;
+        warp_scan(upto);
+        const unsigned reached = __ballot_sync(0xFFFFFFFFu, upto >= want);
+        if (reached) {                                          // (otherwise fewer threads than that have anything: no bound)
+            int bin = lane * kPer;
+            unsigned before = upto - sum;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { before += c[i]; bin += before < want; }
+            bin = __shfl_sync(0xFFFFFFFFu, bin, __ffs(reached) - 1);
+            // a little lower than the roundings of the bin number can move the edge; with one bin: the least of the maxima
+            edge = per > 0.f ? max(key_of(__fsub_rd(hi, (float)(bin + 1) / per * (1.f + 0x1p-20f))), kLowestKey + 1) : low_key;
+        }
     }
-    if (tid == 0) { s.candidates = 0; s.top_key = top_key; s.bound = short_row ? kLowestKey + 1 : low_key; }
+    if (tid == 0) { s.candidates = 0; s.top_key = top_key; s.bound = edge; }
     sync();
     unsigned bound = 0xFFFFFFFFu;
     top_key = 0;
@@ -280,15 +295,19 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     if (list) {
         const float least = of_key(bound);
         SampleShared* const first = cluster.map_shared_rank(&s, 0);
-        x.each([&](const Vec<T>& v, int number) {
-            if (!(v.largest() >= least)) return;
-            const int index = number * kN - x.skew;
+        x.groups([&](const Vec<T> (&v)[4], int number) {
+            unsigned hits = 0;
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
-                if (v.get(i) >= least) {
-                    const unsigned to = atomicAdd(&first->candidates, 1u);
-                    if (to < kListMost) { first->key[to] = key_of(v.get(i)); first->order[to] = (unsigned)(index + i) << 10 | to; }
-                }
+            for (int j = 0; j < 4; ++j)
+                if (v[j].largest() >= least)
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) hits |= (v[j].get(i) >= least ? 1u : 0u) << (j * kN + i);
+            if (!hits) return;
+            unsigned to = atomicAdd(&first->candidates, (unsigned)__popc(hits));
+            for (; hits; hits &= hits - 1, ++to) {
+                const int bit = __ffs(hits) - 1, index = (number + bit / kN * 32) * kN + bit % kN - x.skew;
+                if (to < kListMost) { first->key[to] = key_of(to_float(logits[index])); first->order[to] = (unsigned)index << 10 | to; }
+            }
         });
         sync();
         const unsigned total = first->candidates;
@@ -297,67 +316,128 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         if (list) {
             if (rank != 0) return;                              // the rest is the first CTA's, with nobody else's memory
             const int count = (int)total;
-            // keys in descending order, indices in ascending order: one bitonic network over the next power of two for both
-            int size = 64;
+            // Keys in descending order, indices (with places) in ascending order, entry i of both in register i / 512 of
+            // thread i % 512: a bitonic network for both at once.  Stretches of 32 are put in order by shuffles alone;
+            // only wider steps pass through shared memory, and warps without entries have no part in it.
+            const int halves = count > kSampleThreads ? 2 : 1;
+            int size = 32;
             while (size < count) size *= 2;
-            for (int i = tid; i < size; i += kSampleThreads) {
-                s.sorted[i] = i < count ? s.key[i] : 0u;
-                if (i >= count) s.order[i] = 0xFFFFFFFFu;
+            unsigned key[2], order[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = r * kSampleThreads + tid;
+                key[r] = i < count ? s.key[i] : 0u;
+                order[r] = i < count ? s.order[i] : 0xFFFFFFFFu;
             }
-            __syncthreads();
-            for (int width = 2; width <= size; width *= 2)
-                for (int step = width / 2; step > 0; step /= 2) {
-                    for (int i = tid; i < size; i += kSampleThreads) {
-                        const int pair = i & (size / 2 - 1), a = 2 * pair - (pair & (step - 1)), b = a + step;
-                        unsigned* const list_of = i < size / 2 ? s.sorted : s.order;
-                        const unsigned flip = i < size / 2 ? 0u : 0xFFFFFFFFu, va = list_of[a], vb = list_of[b];
-                        if (((va ^ flip) < (vb ^ flip)) == ((a & width) == 0)) { list_of[a] = vb; list_of[b] = va; }
-                    }
-                    __syncthreads();
+            // the larger key and the smaller index stay where `larger` says
+            auto exchange = [](unsigned& k0, unsigned& o0, unsigned k1, unsigned o1, bool larger) {
+                k0 = larger ? max(k0, k1) : min(k0, k1);
+                o0 = larger ? min(o0, o1) : max(o0, o1);
+            };
+            if (warp * 32 < size) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (r >= halves) break;
+                    const int i = r * kSampleThreads + tid;
+#pragma unroll
+                    for (int width = 2; width <= 32; width *= 2)
+#pragma unroll
+                        for (int step = width / 2; step > 0; step /= 2)
+                            exchange(key[r], order[r], __shfl_xor_sync(0xFFFFFFFFu, key[r], step), __shfl_xor_sync(0xFFFFFFFFu, order[r], step),
+                                     ((i & step) == 0) == ((i & width) == 0));
                 }
+                int buffer = 0;
+                const int threads = min(size, kSampleThreads);
+#pragma unroll 1
+                for (int width = 64; width <= size; width *= 2) {
+#pragma unroll 1
+                    for (int step = width / 2; step >= 32; step /= 2) {
+                        if (step == kSampleThreads) {               // the two registers of a thread
+                            const unsigned k1 = key[1], o1 = order[1];
+                            exchange(key[1], order[1], key[0], order[0], false);
+                            exchange(key[0], order[0], k1, o1, true);
+                            continue;
+                        }
+                        uint2* const at = buffer ? s.spare : s.sorted;
+                        buffer ^= 1;                                // the next exchange writes elsewhere: no second wait
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) if (r < halves) at[r * kSampleThreads + tid] = make_uint2(key[r], order[r]);
+                        asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            if (r < halves) {
+                                const int i = r * kSampleThreads + tid;
+                                const uint2 other = at[i ^ step];
+                                exchange(key[r], order[r], other.x, other.y, ((i & step) == 0) == ((i & width) == 0));
+                            }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if (r >= halves) break;
+                        const bool descending = ((r * kSampleThreads + tid) & width) == 0;
+#pragma unroll
+                        for (int step = 16; step > 0; step /= 2)
+                            exchange(key[r], order[r], __shfl_xor_sync(0xFFFFFFFFu, key[r], step), __shfl_xor_sync(0xFFFFFFFFu, order[r], step),
+                                     ((tid & step) == 0) == descending);
+                    }
+                }
+            }
             // how many of them the filters keep, and from that the value they keep down to and the count at it
             const int limit = k ? min(k, count) : count;
-            const int i0 = tid * 2;
-            u64 w0 = 0, w1 = 0;
-            if (i0 < limit) w0 = Weigh::weight(g.e(s.sorted[i0]));
-            if (i0 + 1 < limit) w1 = Weigh::weight(g.e(s.sorted[i0 + 1]));
-            u64 upto = w0 + w1;
-            const u64 mass = cta_scan(upto, s.warp_mass);
             int kept = limit;
             if (by_mass) {
+                u64 w[2] = {0, 0}, upto[2], mass = 0;
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    if (r < halves) {
+                        if (r * kSampleThreads + tid < limit) w[r] = Weigh::weight(g.e(key[r]));
+                        upto[r] = w[r];
+                        const u64 all = cta_scan(upto[r], s.warp_mass);
+                        upto[r] += mass - w[r];
+                        mass += all;
+                    }
                 const u64 most = max(share(top_part, mass), (u64)1);
-                unsigned keep = (i0 < limit && upto - w1 - w0 < most) + (i0 + 1 < limit && upto - w1 < most);
-                kept = (int)cta_scan(keep, s.warp_count);
+                kept = 0;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) if (r < halves) kept += __syncthreads_count(r * kSampleThreads + tid < limit && upto[r] < most);
             }
-            const unsigned cut = s.sorted[kept - 1];
-            unsigned ties = (i0 < kept && s.sorted[i0] == cut) + (i0 + 1 < kept && s.sorted[i0 + 1] == cut);
-            const unsigned cut_ties = cta_scan(ties, s.warp_count);
-            // the draw, in index order
-            unsigned same = 0;
-            unsigned key[2];
-            u64 w[2] = {0, 0};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) { key[j] = i0 + j < count ? s.key[s.order[i0 + j] & 1023u] : 0u; same += key[j] == cut; }
-            unsigned same_upto = same;
-            cta_scan(same_upto, s.warp_count);
-            same_upto -= same;
+            for (int r = 0; r < 2; ++r) if (r * kSampleThreads + tid == kept - 1) s.cut_key = key[r];
+            __syncthreads();
+            const unsigned cut = s.cut_key;
+            unsigned ties = 0, same_all = 0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                bool take = key[j] > cut;
-                if (key[j] == cut) take = same_upto++ < cut_ties;
-                if (take) {
-                    const float e = g.e(key[j]);
-                    if (e >= g.min_p) w[j] = Weigh::weight(e);
+            for (int r = 0; r < 2; ++r)
+                if (r < halves) {
+                    ties += __syncthreads_count(r * kSampleThreads + tid < kept && key[r] == cut);
+                    same_all += __syncthreads_count(key[r] == cut);
                 }
-            }
-            u64 run = w[0] + w[1];
-            const u64 sum = cta_scan(run, s.warp_mass), drawn = share(part, sum);
-            run -= w[0] + w[1];
+            // the draw, in index order
+            u64 w[2] = {0, 0}, upto[2] = {0, 0}, sum = 0;
+            unsigned same_before = 0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (run <= drawn && drawn < run + w[j]) answer(s.order[i0 + j] >> 10, (float)w[j] / (float)sum);
-                run += w[j];
-            }
+            for (int r = 0; r < 2; ++r)
+                if (r < halves) {
+                    const unsigned mine_key = r * kSampleThreads + tid < count ? s.key[order[r] & 1023u] : 0u;
+                    bool take = mine_key >= cut;
+                    if (ties < same_all) {                          // only the first ones of those equal to the cut
+                        unsigned same = mine_key == cut;
+                        const unsigned here = same;
+                        const unsigned all = cta_scan(same, s.warp_count);
+                        if (here && same_before + same > ties) take = false;
+                        same_before += all;
+                    }
+                    const float e = g.e(mine_key);
+                    if (take && e >= g.min_p) w[r] = Weigh::weight(e);
+                    upto[r] = w[r];
+                    const u64 all = cta_scan(upto[r], s.warp_mass);
+                    upto[r] += sum;
+                    sum += all;
+                }
+            const u64 drawn = share(part, sum);
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                if (upto[r] - w[r] <= drawn && drawn < upto[r]) answer(order[r] >> 10, (float)w[r] / (float)sum);
             return;
         }
     }
@@ -368,94 +448,106 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     else if (k || by_mass) {
         constexpr int kShift = sizeof(T) == 2 ? 16 : 0;          // bf16 logits differ in the upper half of the key only
         const float step = 1.f / (kBinsPerZ * g.inv_t);          // width of a bin in logits
-        auto histogram = [&](bool coarse, unsigned bin, unsigned hi, int shift) {
+        // One round: a histogram of the whole row over the steps of z (coarse), or of one such bin's entries over the bits
+        // of their keys below `hi`; joined; and the bin in which the sum reaches what is still wanted.  First top-k's
+        // count is narrowed down to one key, then top-p's mass.
+        bool for_k = k > 0, coarse = true, first = true;
+        unsigned bin = 0, hi = 0, lo = 0, count_above = 0;
+        int shift = 0;
+        u64 mass_above = 0, need = 0, kept_mass = 0;
+        float floor_of = -INFINITY;                               // no entry of the bin lies below it
+        for (;;) {
             for (int i = tid; i < kBins; i += kSampleThreads) { s.count[i] = 0; s.low[i] = 0; s.high[i] = 0; }
             __syncthreads();
             x.each([&](const Vec<T>& v, int) {
+                if (!(v.largest() >= floor_of)) return;
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
                     const float f = v.get(i), z = g.z(f);
-                    if (!(z > kZeroWeight) || !(f > -INFINITY)) continue;
-                    unsigned b = min((unsigned)(-z * kBinsPerZ), (unsigned)kBins - 1);
+                    // to the nearest whole number of steps, by the bits of a sum with 2^23 (z is at least kZeroWeight here)
+                    unsigned b = __float_as_uint(fminf(-z * kBinsPerZ, (float)(kBins - 1)) + 8388608.f) & 0x7FFFFFu;
+                    bool in = z > kZeroWeight && f > -INFINITY;
                     if (!coarse) {
                         const unsigned key = key_of(f) >> kShift;
-                        if (b != bin || key > hi) continue;
+                        in = in && b == bin && key <= hi && (hi - key) >> shift < kBins;
                         b = (hi - key) >> shift;
-                        if (b >= kBins) continue;
                     }
-                    const unsigned w = Weigh::weight(expf(z));
-                    if (w == 0) continue;
-                    if (k) atomicAdd(&s.count[b], 1u);
-                    atomicAdd(&s.low[b], w & 0xFFFFu);
-                    if (w >> 16) atomicAdd(&s.high[b], w >> 16);
+                    const unsigned w = in ? Weigh::weight(expf(z)) : 0u;
+                    if (w) {
+                        if (k) atomicAdd(&s.count[b], 1u);
+                        atomicAdd(&s.low[b], w & 0xFFFFu);
+                        if (w >> 16) atomicAdd(&s.high[b], w >> 16);
+                    }
                 }
             });
             sync();
             const int share_bins = kBins / ctas;
             for (int i = tid; i < share_bins; i += kSampleThreads) {
                 const int at = rank * share_bins + i;
-                unsigned a = 0;
+                unsigned n = 0;
                 u64 m = 0;
                 for (int c = 0; c < ctas; ++c) {
-                    a += *cluster.map_shared_rank(&s.count[at], c);
+                    n += *cluster.map_shared_rank(&s.count[at], c);
                     m += *cluster.map_shared_rank(&s.low[at], c) + ((u64)*cluster.map_shared_rank(&s.high[at], c) << 16);
                 }
                 for (int c = 0; c < ctas; ++c) {
-                    *cluster.map_shared_rank(&s.joined_count[at], c) = a;
+                    *cluster.map_shared_rank(&s.joined_count[at], c) = n;
                     *cluster.map_shared_rank(&s.joined_mass[at], c) = m;
                 }
             }
             sync();
-        };
-        // narrows the coarse bin in s.hit_* down to one key; `need` counts from the top of the row.  Leaves the sums
-        // above that key.
-        auto refine = [&](u64 need, bool mass, u64& mass_above, unsigned& count_above, unsigned& key) {
-            const unsigned bin = s.hit_bin;
-            mass_above = s.hit_mass_above; count_above = s.hit_count_above;
-            // bounds of the bin's logits, a little wider than the roundings of z and of the bin number can move them
-            const float near = bin ? (float)bin * step * (1.f - 0x1p-20f) : 0.f, far = (float)(bin + 1) * step * (1.f + 0x1p-20f);
-            unsigned hi = min(top_key, key_of(__fsub_ru(g.top, near))) >> kShift;
-            unsigned lo = key_of(bin == kBins - 1 ? -INFINITY : __fsub_rd(g.top, far)) >> kShift;
-            for (;;) {
-                int shift = 0;
-                while ((hi - lo) >> shift >= kBins) ++shift;
-                __syncthreads();                                  // everybody has read s.hit_*
-                histogram(false, bin, hi, shift);
-                find_bin(s, need - (mass ? mass_above : (u64)count_above), mass);
-                mass_above += s.hit_mass_above; count_above += s.hit_count_above;
+            if (first) {
+                first = false;
+                unsigned all;
+                find_bin(s, 0, false, &all, &kept_mass);          // the sums alone
+                if ((unsigned)k >= all) for_k = false;            // fewer weights above zero than k: k keeps them all
+                if (!for_k && !by_mass) break;
+                need = for_k ? (u64)k : max(share(top_part, kept_mass), (u64)1);
+            }
+            find_bin(s, need - (for_k ? (u64)count_above : mass_above), !for_k);
+            if (coarse) {
+                bin = s.hit_bin; count_above = s.hit_count_above; mass_above = s.hit_mass_above;
+                // bounds of the bin's logits, a little wider than the roundings of z and of the bin number can move them
+                const float near = bin ? ((float)bin - 0.5f) * step * (1.f - 0x1p-19f) : 0.f, far = ((float)bin + 0.5f) * step * (1.f + 0x1p-19f);
+                floor_of = bin == kBins - 1 ? -INFINITY : __fsub_rd(g.top, far);
+                hi = min(top_key, key_of(__fsub_ru(g.top, near))) >> kShift;
+                lo = key_of(floor_of) >> kShift;
+                coarse = false;
+            } else {
+                count_above += s.hit_count_above; mass_above += s.hit_mass_above;
                 hi -= s.hit_bin << shift;
                 const unsigned low = hi - ((1u << shift) - 1u);
                 lo = low > hi || low < lo ? lo : low;
-                if (shift == 0) break;
+                if (shift == 0) {                                 // one key
+                    const unsigned key = kShift == 0 ? hi : hi << kShift | (hi >> 15 ? 0u : 0xFFFFu);   // a negative number's bits are inverted
+                    const unsigned w = Weigh::weight(g.e(key));
+                    if (for_k) {
+                        cut_key = key; cut_ties = k - count_above;
+                        kept_mass = mass_above + (u64)cut_ties * w;
+                        if (!by_mass) break;
+                        for_k = false; coarse = true;
+                        count_above = 0; mass_above = 0; floor_of = -INFINITY;
+                        need = max(share(top_part, kept_mass), (u64)1);
+                        __syncthreads();
+                        continue;
+                    }
+                    const u64 ties = (need - mass_above + w - 1) / w;
+                    if (key > cut_key) { cut_key = key; cut_ties = (unsigned)min(ties, (u64)0xFFFFFFFFu); }
+                    else cut_ties = (unsigned)min(ties, (u64)cut_ties);
+                    break;
+                }
             }
-            key = kShift == 0 ? hi : hi << kShift | (hi >> 15 ? 0u : 0xFFFFu);   // a negative number's bits are inverted
-        };
-        histogram(true, 0, 0, 0);
-        unsigned total, count_above;
-        u64 kept_mass, mass_above;
-        find_bin(s, k ? (u64)k : 1, k == 0, &total, &kept_mass);
-        if (k && (unsigned)k < total) {                           // fewer weights above zero than k: k keeps them all
-            refine(k, false, mass_above, count_above, cut_key);
-            cut_ties = k - count_above;
-            kept_mass = mass_above + (u64)cut_ties * Weigh::weight(g.e(cut_key));
-        }
-        if (by_mass) {
-            const u64 upto = max(share(top_part, kept_mass), (u64)1);
-            __syncthreads();
-            if (cut_key) histogram(true, 0, 0, 0);
-            find_bin(s, upto, true);
-            unsigned key;
-            refine(upto, true, mass_above, count_above, key);
-            const unsigned w = Weigh::weight(g.e(key));
-            const u64 ties = (upto - mass_above + w - 1) / w;
-            if (key > cut_key) { cut_key = key; cut_ties = (unsigned)min(ties, (u64)0xFFFFFFFFu); }
-            else cut_ties = (unsigned)min(ties, (u64)cut_ties);
+            shift = 0;
+            while ((hi - lo) >> shift >= kBins) ++shift;
+            __syncthreads();                                      // everybody has read s.hit_*
         }
     }
 
     // ---- kept mass of every warp's vectors (consecutive entries), in index order ----
     const float cut_e = g.e(cut_key), least = cut_key > kLowestKey ? of_key(cut_key) : -INFINITY;
     const unsigned cut_w = cut_key && cut_e >= g.min_p ? Weigh::weight(cut_e) : 0u;
+    // nothing below `skip` is kept: the cut, or what min-p leaves at most, taken a little lower than its logarithm can be off
+    const float skip = fmaxf(least, g.min_p > 0.f ? g.top + (logf(g.min_p) - 1e-3f) / g.inv_t * 1.0001f - fabsf(g.top) * 1e-6f : -INFINITY);
     auto kept = [&](float f) {                                    // weight of an entry above the cut
         if (!(f > least)) return 0u;
         const float z = g.z(f);
@@ -467,7 +559,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         u64 mass = 0;
         unsigned ties = 0;
         x.each([&](const Vec<T>& v, int) {
-            if (!(v.largest() >= least)) return;
+            if (v.largest() < skip) return;
 #pragma unroll
             for (int i = 0; i < kN; ++i) { mass += kept(v.get(i)); ties += v.get(i) == least; }
         });
@@ -499,7 +591,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         unsigned ties = s.pick_ties;
         bool found = false;
         x.each([&](const Vec<T>& v, int number) {
-            if (found || !__any_sync(0xFFFFFFFFu, v.largest() >= least)) return;
+            if (found || __all_sync(0xFFFFFFFFu, v.largest() < skip)) return;
             unsigned same = 0, w[kN];
             if (cut_key)
 #pragma unroll
@@ -543,9 +635,20 @@ static cudaError_t sample_t(const SampleParams& p, int sms, cudaStream_t stream)
     // CTAs a row: as many as fill the machine without a second round of CTAs (two share an SM), each with 2048 entries at least
     int ctas = 1;
     while (ctas < kSampleCtas && p.rows * ctas * 2 <= sms && p.vocab > 2048 * ctas) ctas *= 2;
-    while (p.vocab > kSampleSlice * ctas) ctas *= 2;
+    auto slice = [&](int c) {                                    // the most entries of a CTA
+        const int n = Vec<T>::kN, vectors = (p.vocab + 2 * n - 2) / n;
+        return c == 1 ? p.vocab : (vectors + c * kSampleWarps - 1) / (c * kSampleWarps) * kSampleWarps * n;
+    };
+    while (slice(ctas) > kSampleSlice) ctas *= 2;
     const cudaError_t e = ensure_dynamic_smem(k_sample<T>, sizeof(SampleShared), opt);
     if (e != cudaSuccess) return e;
+    static std::atomic<bool> carved[64];                         // two CTAs share an SM's shared memory only if it is told to be that large
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || !carved[dev].load()) {
+        const cudaError_t c = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (c != cudaSuccess) return c;
+        if (dev >= 0 && dev < 64) carved[dev].store(true);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * ctas)); cfg.blockDim = dim3(kSampleThreads); cfg.dynamicSmemBytes = sizeof(SampleShared); cfg.stream = stream;
     cudaLaunchAttribute attr[2];

@@ -26,8 +26,7 @@ constexpr int kSampleCtas = 8;               // of a cluster, at most
 constexpr int kBins = 2048;
 constexpr int kListMost = 1024;              // candidates that are worked on as a list (twice the threads; a place in it has 10 bits)
 constexpr int kListRank = 384;               // top-k for each CTA of a row up to which the threads' maxima bound it well
-constexpr float kZeroWeight = -22.25f;       // below this z the weight rounds to zero (2^31 e^z < 1/2 below -22.18)
-constexpr float kBinsPerZ = kBins / 22.25f;
+constexpr float kBinsPerZ = kBins / 22.25f;  // below z = -22.18 the weight rounds to zero (2^31 e^z < 1/2)
 constexpr int kSampleSlice = 65536;          // entries a CTA takes, at most: its sums of 16-bit halves stay within 32 bits
 constexpr unsigned kLowestKey = 0x007FFFFFu; // key of -infinity
 
@@ -39,11 +38,17 @@ __device__ __forceinline__ unsigned key_of(float x) {
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-struct Weigh {                               // what turns a logit into its weight
+// What turns a logit into its weight, where the largest logit is finite and 1 / temperature too (z is then 0 at the largest).
+struct Weigh {
     float top, inv_t, min_p;
-    __device__ __forceinline__ float z(float x) const { return x == top ? 0.f : __fmul_rn(x - top, inv_t); }
+    __device__ __forceinline__ float z(float x) const { return __fmul_rn(x - top, inv_t); }
     __device__ __forceinline__ float e(unsigned key) const { return expf(z(of_key(key))); }
-    __device__ __forceinline__ static unsigned weight(float e) { return __float2uint_rn(e * 2147483648.f); }
+    // 2^31 e, rounded.  Below 2^23 by the bits of a sum with 2^23, which saves the conversion (a quarter-rate instruction,
+    // as the exponential is); a NaN gives 0
+    __device__ __forceinline__ static unsigned weight(float e) {
+        const float v = e * 2147483648.f;
+        return v < 8388608.f ? __float_as_uint(v + 8388608.f) & 0x7FFFFFu : __float2uint_rn(v);
+    }
 };
 
 // part / 2^24 of total, rounded down
@@ -288,8 +293,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         sync();
         return;
     }
-    const bool greedy = !(t > 0.f) || k == 1;
-    if (greedy) { list = false; g.inv_t = INFINITY; }
+    // All weight on the entries equal to the largest: only the first of them for a temperature of 0; all of them where the
+    // largest is infinite or the temperature next to nothing (their differences have no finite z)
+    const bool greedy = !(t > 0.f) || k == 1, equal_only = greedy || !(g.top < INFINITY) || !(g.inv_t < INFINITY);
+    if (equal_only) list = false;
 
     // ---- the candidates, in the first CTA's list: their keys, and their indices with their places in it ----
     if (list) {
@@ -444,8 +451,25 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
 
     // ---- the value the filters keep down to, and how many of the entries equal to it ----
     unsigned cut_key = 0, cut_ties = 0xFFFFFFFFu;
-    if (greedy) { cut_key = top_key; cut_ties = 1; }
-    else if (k || by_mass) {
+    if (equal_only) {
+        cut_key = top_key;
+        cut_ties = greedy ? 1u : k ? (unsigned)k : 0xFFFFFFFFu;
+        if (!greedy && by_mass) {
+            unsigned same = 0;
+            x.each([&](const Vec<T>& v, int) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) same += v.get(i) == g.top;
+            });
+            same = __reduce_add_sync(0xFFFFFFFFu, same);
+            if (lane == 0) s.seg_ties[warp] = same;
+            sync();
+            u64 all = 0;
+            for (int c = 0; c < ctas * kSampleWarps; ++c) all += *cluster.map_shared_rank(&s.seg_ties[c % kSampleWarps], c / kSampleWarps);
+            sync();
+            const u64 one = 1ull << 31, upto = max(share(top_part, min(all, (u64)cut_ties) * one), (u64)1);
+            cut_ties = (unsigned)min((u64)cut_ties, (upto + one - 1) / one);
+        }
+    } else if (k || by_mass) {
         constexpr int kShift = sizeof(T) == 2 ? 16 : 0;          // bf16 logits differ in the upper half of the key only
         const float step = 1.f / (kBinsPerZ * g.inv_t);          // width of a bin in logits
         // One round: a histogram of the whole row over the steps of z (coarse), or of one such bin's entries over the bits
@@ -464,16 +488,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
                     const float f = v.get(i), z = g.z(f);
-                    // to the nearest whole number of steps, by the bits of a sum with 2^23 (z is at least kZeroWeight here)
-                    unsigned b = __float_as_uint(fminf(-z * kBinsPerZ, (float)(kBins - 1)) + 8388608.f) & 0x7FFFFFu;
-                    bool in = z > kZeroWeight && f > -INFINITY;
+                    // to the nearest whole number of steps, by the bits of a sum with 2^23 (anything where the weight is 0)
+                    unsigned b = min(__float_as_uint(__fmaf_rn(z, -kBinsPerZ, 8388608.f)) & 0x7FFFFFu, kBins - 1u);
+                    bool in = true;
                     if (!coarse) {
                         const unsigned key = key_of(f) >> kShift;
-                        in = in && b == bin && key <= hi && (hi - key) >> shift < kBins;
+                        in = b == bin && key <= hi && (hi - key) >> shift < kBins;
                         b = (hi - key) >> shift;
                     }
-                    const unsigned w = in ? Weigh::weight(expf(z)) : 0u;
-                    if (w) {
+                    const unsigned w = Weigh::weight(expf(z));
+                    if (w && in) {
                         if (k) atomicAdd(&s.count[b], 1u);
                         atomicAdd(&s.low[b], w & 0xFFFFu);
                         if (w >> 16) atomicAdd(&s.high[b], w >> 16);
@@ -544,24 +568,27 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     }
 
     // ---- kept mass of every warp's vectors (consecutive entries), in index order ----
-    const float cut_e = g.e(cut_key), least = cut_key > kLowestKey ? of_key(cut_key) : -INFINITY;
+    const float cut_e = equal_only ? 1.f : g.e(cut_key), least = cut_key > kLowestKey ? of_key(cut_key) : -INFINITY;
     const unsigned cut_w = cut_key && cut_e >= g.min_p ? Weigh::weight(cut_e) : 0u;
     // nothing below `skip` is kept: the cut, or what min-p leaves at most, taken a little lower than its logarithm can be off
     const float skip = fmaxf(least, g.min_p > 0.f ? g.top + (logf(g.min_p) - 1e-3f) / g.inv_t * 1.0001f - fabsf(g.top) * 1e-6f : -INFINITY);
     auto kept = [&](float f) {                                    // weight of an entry above the cut
-        if (!(f > least)) return 0u;
-        const float z = g.z(f);
-        if (!(z > kZeroWeight)) return 0u;
-        const float e = expf(z);
-        return e >= g.min_p ? Weigh::weight(e) : 0u;
+        const float e = expf(g.z(f));
+        return f > least && e >= g.min_p ? Weigh::weight(e) : 0u;
     };
     {
         u64 mass = 0;
         unsigned ties = 0;
         x.each([&](const Vec<T>& v, int) {
             if (v.largest() < skip) return;
+            unsigned small = 0;                                   // eight weights below 2^23 stay within 32 bits
 #pragma unroll
-            for (int i = 0; i < kN; ++i) { mass += kept(v.get(i)); ties += v.get(i) == least; }
+            for (int i = 0; i < kN; ++i) {
+                const unsigned w = kept(v.get(i));
+                if (w < 8388608u) small += w; else mass += w;
+                ties += v.get(i) == least;
+            }
+            mass += small;
         });
 #pragma unroll
         for (int d = 16; d; d >>= 1) { mass += __shfl_xor_sync(0xFFFFFFFFu, mass, d); ties += __shfl_xor_sync(0xFFFFFFFFu, ties, d); }

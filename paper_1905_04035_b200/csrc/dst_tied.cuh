@@ -11,16 +11,20 @@ int device_sm_count();                      // of the current device, asked of t
 void count_launches(int n);                 // what dst_kernel_launches reports
 
 // ---- dropout and embedding (dst_dropout.cu) ---------------------------------------
-struct DropParams {                         // the generator's key and counter, and the factor of a kept element
-    unsigned key0, key1;
-    unsigned cut;                           // 16-bit halves below it are dropped
+struct DropParams {                         // the generator's keys of every round and counter, and the factor of a kept element
+    unsigned key0[10], key1[10];
+    unsigned below;                         // 16-bit halves, in the upper half of a word, up to this are dropped
+    int none;                               // nothing is dropped, no bits are drawn
     float keep;                             // 65536 / (65536 - cut), 0 when everything is dropped
     unsigned long long offset;
     const unsigned long long* offset_device;
     unsigned row_offset;
 };
+// Units (parts of a row) that a thread takes are a fixed number apart; where the next one lies follows by additions.
+struct UnitStep { long long units, rows; unsigned per_row, part; };   // in all, rows on, parts of a row, parts on
 struct DropoutParams {
     DropParams drop;
+    UnitStep step;
     const void* x;
     const void* residual;
     void* out;
@@ -31,6 +35,7 @@ struct DropoutParams {
 };
 struct EmbedParams {
     DropParams drop;
+    UnitStep step;
     const void* indices;
     const void* weight;
     const float* position;

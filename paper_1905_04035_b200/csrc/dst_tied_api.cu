@@ -19,13 +19,19 @@ constexpr int64_t kMaxCols = int64_t(1) << 30;   // columns of a row, and rows o
 
 // The generator's parameters; false: refused.
 static bool drop_params(const dst_dropout_t* d, int64_t rows, DropParams& p) {
-    p = DropParams{0, 0, 0, 1.f, 0, nullptr, 0};
+    p = DropParams{};
+    p.none = 1; p.keep = 1.f;
     if (!d) return true;
     if (!(d->p >= 0.0 && d->p <= 1.0) || d->row_offset < 0 || d->row_offset > (int64_t(1) << 32) - rows) return false;
     if (misaligned(d->offset_device, 8)) return false;
-    p.key0 = unsigned(d->seed); p.key1 = unsigned(d->seed >> 32);
-    p.cut = unsigned(rint(d->p * 65536.0));
-    p.keep = p.cut >= 65536u ? 0.f : 65536.f / float(65536u - p.cut);
+    for (unsigned r = 0; r < 10; ++r) {                  // each round moves the keys by a fixed step
+        p.key0[r] = unsigned(d->seed) + r * 0x9E3779B9u;
+        p.key1[r] = unsigned(d->seed >> 32) + r * 0xBB67AE85u;
+    }
+    const unsigned cut = unsigned(rint(d->p * 65536.0));
+    p.none = cut == 0;
+    p.below = cut == 0 ? 0u : unsigned((uint64_t(cut) << 16) - 1);
+    p.keep = cut >= 65536u ? 0.f : 65536.f / float(65536u - cut);
     p.offset = d->offset;
     p.offset_device = reinterpret_cast<const unsigned long long*>(d->offset_device);
     p.row_offset = unsigned(d->row_offset);
@@ -96,6 +102,7 @@ int dst_dropout(const void* x, int64_t ldx, int32_t x_type, const void* residual
     if (out == x && (ldo != ldx || out_type != x_type)) return DST_ERR_INVALID_ARG;
     if (residual && out == residual && ldo != ldr) return DST_ERR_INVALID_ARG;
     if (rows == 0 || d == 0) return DST_OK;
+    p.step = UnitStep{};
     p.x = x; p.residual = residual; p.out = out;
     p.ldx = ldx; p.ldr = ldr; p.ldo = ldo; p.rows = rows; p.d = int(d); p.scale = scale;
     return done(launch_dropout(p, x_type, out_type, device_sm_count(), stream), 1);
@@ -115,6 +122,7 @@ int dst_embed(const void* indices, int64_t n_rows, int32_t index_type, const voi
     if (!drop_params(drop, n_rows, p.drop)) return DST_ERR_INVALID_ARG;
     if (result && cudaMemsetAsync(result, 0, sizeof *result, stream) != cudaSuccess) return DST_ERR_CUDA;
     if (n_rows == 0 || d == 0) return DST_OK;
+    p.step = UnitStep{};
     p.indices = indices; p.weight = weight; p.position = position; p.out = out; p.result = result;
     p.rows = n_rows; p.vocab = vocab; p.n_positions = n_positions; p.d = int(d); p.scale = scale;
     return done(launch_embed(p, index_type, weight_type, out_type, device_sm_count(), stream), 1);

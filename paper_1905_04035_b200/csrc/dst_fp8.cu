@@ -215,7 +215,6 @@ cudaError_t launch_quantize(const QuantParams& p, int x_type, cudaStream_t strea
 constexpr int kBlockK = 128;                              // one scale's worth of the inner dimension, in bytes too
 constexpr int kTileP = 128;                               // rows of P a CTA
 constexpr int kSmemMost = 232448;
-constexpr int kOutPitch = 272;                            // bytes of shared memory a lane stages a row in: 256, and room to start anywhere in 16
 
 template <int CG, int NT>
 struct TileShape {
@@ -226,9 +225,12 @@ struct TileShape {
     static constexpr int kStageBytes = (kTileP + kQRows) * kBlockK;
     static constexpr int kQScaleTiles = (NT + 127) / 128;
     static constexpr int kScaleBytes = (1 + kQScaleTiles) * kScaleTile;   // of four blocks
-    static constexpr int kOutBytes = kEpiWarps * 32 * kOutPitch;
+    // bytes of shared memory a lane stages its row in: 256 at most, and room to start anywhere in 16
+    static constexpr int kOutPitch = (kCols < 64 ? kCols * 4 : 256) + 16, kOutBytes = kEpiWarps * 32 * kOutPitch;
     static constexpr int kHeaderBytes = 1024;
-    static constexpr int kFit = (kSmemMost - kOutBytes - kHeaderBytes) / (kStageBytes + kScaleBytes);
+    // small tiles wait for memory, not for each other: two CTAs share an SM
+    static constexpr int kCtas = NT <= 64 ? 2 : 1;
+    static constexpr int kFit = (kSmemMost / kCtas - (kCtas - 1) * 1024 - kOutBytes - kHeaderBytes) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kFit < 8 ? kFit : 8;
     static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kOutBytes + kHeaderBytes;
     // tensor memory: one or two results, then a ring of scales (P's four columns, then Q's; four groups of four blocks)
@@ -407,7 +409,7 @@ __device__ __forceinline__ void store_swapped(const MatmulParams& p, OT* out, co
 }
 
 template <int CG, int NT, typename OT>
-__global__ void __launch_bounds__(TileShape<CG, NT>::kThreads, 1)
+__global__ void __launch_bounds__(TileShape<CG, NT>::kThreads, TileShape<CG, NT>::kCtas)
 k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
              const __grid_constant__ CUtensorMap map_sq, const __grid_constant__ MatmulParams p) {
     using S = TileShape<CG, NT>;
@@ -529,7 +531,7 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     } else {                                                                       // ---- epilogue ----
         const int group = warp >> 2, quarter = warp & 3;                           // a warp reaches the 32 lanes of its quarter
         const unsigned mine = tmem + ((unsigned)(quarter * 32) << 16) + group * 128;
-        unsigned char* const buffer = out_rows + threadIdx.x * kOutPitch;
+        unsigned char* const buffer = out_rows + threadIdx.x * S::kOutPitch;
         const unsigned free_bar = in_cta(tmem_empty, 0);
         int buf = 0;
         unsigned buf_phase = 0;
@@ -596,9 +598,13 @@ struct MatmulPlan { int cg, nt, swap; long long rows_p, rows_q, tiles_p, tiles_q
 static MatmulPlan plan_matmul(long long M, long long N, long long K) {
     MatmulPlan L{};
     const long long small = M < N ? M : N;
-    L.swap = small <= 128 && M < N;
-    L.cg = small <= 128 ? 1 : 2;
-    L.nt = small <= 16 ? 16 : small <= 32 ? 32 : small <= 64 ? 64 : small <= 128 ? 128 : 256;
+    // Up to 64 rows the small side is Q (and for Q = a the result leaves transposed, a column a lane).  With 65 to 128 it
+    // is still b's case, but a of so few rows does better as half a pair's tile: 128 x 33708 x 1024 takes 17.5 us as
+    // Q and 14.8 us so.
+    const bool narrow = small <= 64 || (small <= 128 && N <= M);
+    L.swap = narrow && M < N;
+    L.cg = narrow ? 1 : 2;
+    L.nt = !narrow ? 256 : small <= 16 ? 16 : small <= 32 ? 32 : small <= 64 ? 64 : 128;
     L.rows_p = L.swap ? N : M; L.rows_q = L.swap ? M : N;
     L.tiles_p = (L.rows_p + kTileP * L.cg - 1) / (kTileP * L.cg);
     L.tiles_q = (L.rows_q + L.nt - 1) / L.nt;
@@ -671,7 +677,7 @@ static cudaError_t matmul_launch(const MatmulMaps& m, const MatmulParams& p, int
     static SmemOptIn opt;
     const cudaError_t e = ensure_dynamic_smem(k_matmul_fp8<CG, NT, OT>, S::kSmem, opt);
     if (e != cudaSuccess) return e;
-    const long long items = (long long)p.tiles_p * p.tiles_q * p.splits, workers = sms / CG;
+    const long long items = (long long)p.tiles_p * p.tiles_q * p.splits, workers = sms / CG * S::kCtas;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((items < workers ? items : workers) * CG)); cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem; cfg.stream = stream;

@@ -5,7 +5,6 @@ Matrices are 2-D CUDA tensors with contiguous rows (any distance between rows); 
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from typing import Optional
 
@@ -16,11 +15,13 @@ from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _F
 DST_FP8_ROW, DST_FP8_SQUARE = 0, 1
 _TYPES = {torch.float32: DST_F32, torch.bfloat16: DST_BF16}
 _INDEX = {torch.int32: DST_I32, torch.int64: DST_I64}
-_nothing = contextlib.nullcontext()
 
 
 # the stream that work goes to unless one is given; torch's own accessor of the raw handle, without a Stream object a call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_current_device = torch.cuda.current_device
 
 
 def _matrix(t: torch.Tensor, rows: int, cols: int, index: int, name: str):
@@ -30,12 +31,13 @@ def _matrix(t: torch.Tensor, rows: int, cols: int, index: int, name: str):
         raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
     if t.shape != (rows, cols):
         raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
-    _here(t, index)
+    if t.get_device() != index:
+        raise ValueError("all tensors must live on the same device")
     ld, step = t.stride()
-    if rows <= 1:
+    if step != 1 or ld < cols:
+        if (step != 1 and cols > 1) or rows > 1:
+            raise ValueError("%s must have contiguous rows that do not overlap" % name)
         ld = cols
-    if (step != 1 and cols > 1) or ld < cols:
-        raise ValueError("%s must have contiguous rows that do not overlap" % name)
     return t.data_ptr(), ld, kind
 
 
@@ -62,13 +64,16 @@ def _here(t: torch.Tensor, index: int) -> None:
         raise ValueError("all tensors must live on the same device")
 
 
-def _on(index: int):
-    """The context in which work for a device is enqueued (nothing to do where it is current already)."""
-    return _nothing if torch.cuda.current_device() == index else torch.cuda.device(index)
-
-
-def _stream(stream, index: int) -> int:
-    return _raw_stream(index) if stream is None else stream.cuda_stream
+def _enqueue(name: str, index: int, stream, *args) -> None:
+    """Call a C entry whose last argument is the stream, with device `index` current; raises on a status."""
+    fn = getattr(load_library(), name)
+    if _current_device() == index:
+        rc = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    if rc != 0:
+        raise DstError(rc, name)
 
 
 def _drop(p, seed, offset, offset_tensor, row_offset, index) -> _Dropout:
@@ -98,10 +103,7 @@ def dst_dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, offset:
         if tr != to:
             raise TypeError("residual and out must share a dtype")
     drop = _drop(p, seed, offset, offset_tensor, row_offset, index)
-    with _on(index):
-        rc = load_library().dst_dropout(px, ldx, tx, pr, ldr, po, ldo, to, rows, d, scale, drop, _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_dropout")
+    _enqueue("dst_dropout", index, stream, px, ldx, tx, pr, ldr, po, ldo, to, rows, d, scale, drop)
     return out
 
 
@@ -123,7 +125,7 @@ def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *,
     pi = _vector(indices, n, indices.dtype, index, "indices")
     pw, ldw, tw = _matrix(weight, vocab, d, index, "weight")
     po, ldo, to = _matrix(out, n, d, index, "out")
-    if ldw != d or ldo != d:
+    if (ldw != d and vocab > 1) or (ldo != d and n > 1):
         raise ValueError("weight and out must be contiguous")
     n_pos, pp = 0, None
     if position is not None:
@@ -131,7 +133,7 @@ def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *,
         pp, ldp, tp = _matrix(position, n_pos, d, index, "position")
         if tp != DST_F32:
             raise TypeError("position must be float32, got %s" % position.dtype)
-        if ldp != d:
+        if ldp != d and n_pos > 1:
             raise ValueError("position must be contiguous [n_positions, d]")
     pres = None
     if result is not None:
@@ -140,11 +142,7 @@ def dst_embed(indices: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *,
         _here(result, index)
         pres = result.data_ptr()
     drop = _drop(p, seed, offset, offset_tensor, row_offset, index)
-    with _on(index):
-        rc = load_library().dst_embed(pi, n, index_type, pw, vocab, d, tw, pp, n_pos, po, to, scale, drop, pres,
-                                      _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_embed")
+    _enqueue("dst_embed", index, stream, pi, n, index_type, pw, vocab, d, tw, pp, n_pos, po, to, scale, drop, pres)
     return out
 
 
@@ -197,11 +195,7 @@ def dst_quantize_fp8(x: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Ma
     for m in (q, qt):
         if m is not None:
             _here(m.q, index)
-    with _on(index):
-        rc = load_library().dst_quantize_fp8(px, ldx, tx, rows, cols, None if q is None else q._c,
-                                             None if qt is None else qt._c, _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_quantize_fp8")
+    _enqueue("dst_quantize_fp8", index, stream, px, ldx, tx, rows, cols, None if q is None else q._c, None if qt is None else qt._c)
 
 
 def dst_matmul_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -227,10 +221,7 @@ def dst_matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor, workspace: Opt
     _here(b.q, index)
     po, ldo, to = _matrix(out, a.rows, b.rows, index, "out")
     ws, ws_bytes = _workspace(workspace, index)
-    with _on(index):
-        rc = load_library().dst_matmul_fp8(a._c, b._c, po, ldo, to, ws, ws_bytes, _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_matmul_fp8")
+    _enqueue("dst_matmul_fp8", index, stream, a._c, b._c, po, ldo, to, ws, ws_bytes)
     return out
 
 
@@ -245,10 +236,7 @@ def dst_linear_fp8(x: torch.Tensor, w: Fp8Matrix, out: torch.Tensor, workspace: 
     po, ldo, to = _matrix(out, m, w.rows, index, "out")
     _here(w.q, index)
     ws, ws_bytes = _workspace(workspace, index)
-    with _on(index):
-        rc = load_library().dst_linear_fp8(px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes, _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_linear_fp8")
+    _enqueue("dst_linear_fp8", index, stream, px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes)
     return out
 
 
@@ -273,10 +261,7 @@ def dst_sample(logits: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor
     pm = _vector(min_p, rows, f32, index, "min_p")
     po = _vector(tokens, rows, tokens.dtype, index, "tokens")
     pb = _vector(prob, rows, f32, index, "prob")
-    with _on(index):
-        rc = load_library().dst_sample(pl, ld, tl, rows, vocab, pu, pt, pk, pp, pm, po, token_type, pb, _stream(stream, index))
-    if rc != 0:
-        raise DstError(rc, "dst_sample")
+    _enqueue("dst_sample", index, stream, pl, ld, tl, rows, vocab, pu, pt, pk, pp, pm, po, token_type, pb)
     return tokens
 
 

@@ -11,13 +11,14 @@ namespace dst {
 // 2^e with amax <= 448 * 2^e.  448 = 1.75 * 2^8, so e is amax's exponent less 8, one more where its mantissa is above
 // 1.75: adding all that 1.75 leaves of a mantissa, less one, carries exactly there.  255 (NaN) where the block holds an
 // infinity or a NaN (their bits are the largest).
-struct BlockScale {
-    unsigned exponent;
-    float inverse;                                          // 2^-e, exact (any number where the scale is NaN)
-};
-__device__ __forceinline__ BlockScale block_scale(unsigned amax) {
-    const unsigned carried = max(amax, 0x0D800000u) + 0x1FFFFFu;   // 2^-100 at least
-    return BlockScale{amax >= 0x7F800000u ? 255u : (carried >> 23) - 8u, __uint_as_float(0x83000000u - (carried & 0xFF800000u))};
+constexpr unsigned kLeastAmax = 0x0D800000u;                // 2^-100
+__device__ __forceinline__ unsigned block_exponent(unsigned amax) {
+    return amax >= 0x7F800000u ? 255u : ((max(amax, kLeastAmax) + 0x1FFFFFu) >> 23) - 8u;
+}
+// 2^-e, exact (any number where the scale is NaN): the exponent field 262 less the carried one above, in one subtraction
+// whose lower bits never borrow
+__device__ __forceinline__ float block_inverse(unsigned amax) {
+    return __uint_as_float((0x837FFFFFu - 0x1FFFFFu - max(amax, kLeastAmax)) & 0xFF800000u);
 }
 __device__ __forceinline__ uint8_t* scale_byte(const Fp8View& m, long long row, long long block) {
     return m.scale + ((row >> 7) * m.ld_scale + (block >> 2)) * kScaleTile + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
@@ -114,30 +115,31 @@ __device__ __forceinline__ void quantize_tile(const QuantParams& p, T* tile, uns
         }
     }
     if (SQUARE || p.qt.q) __syncthreads();
-    BlockScale sc{0, 0.f};
+    float u = 0.f;
     if (SQUARE) {
         unsigned top = 0;
         for (int w = 0; w < S::kWarps; ++w) top = max(top, warp_max[w]);
-        sc = block_scale(top);
+        u = block_inverse(top);
+        const uint8_t e = (uint8_t)block_exponent(top);
         if (threadIdx.x < 128) {                            // every row's byte, as the product wants it
-            if (p.q.q) *scale_byte(p.q, r0 + threadIdx.x, cb) = (uint8_t)sc.exponent;
-            if (p.qt.q) *scale_byte(p.qt, c0 + threadIdx.x, rb) = (uint8_t)sc.exponent;
+            if (p.q.q) *scale_byte(p.q, r0 + threadIdx.x, cb) = e;
+            if (p.qt.q) *scale_byte(p.qt, c0 + threadIdx.x, rb) = e;
         }
     }
     if (p.q.q) {
         uint8_t* q = p.q.q + (r0 + warp) * p.q.ld + c0 + lane * 4;
-        unsigned mine = 0;                                  // lane i: the exponent of the warp's i-th row
+        unsigned mine = 0;                                  // lane i: the largest magnitude of the warp's i-th row
 #pragma unroll
         for (int i = 0; i < S::kRows; ++i, q += S::kWarps * p.q.ld) {
             if (!SQUARE) {
-                sc = block_scale(__reduce_max_sync(0xFFFFFFFFu, v[i].amax()));
-                if (lane == i) mine = sc.exponent;
+                const unsigned top = __reduce_max_sync(0xFFFFFFFFu, v[i].amax());
+                if (lane == i) mine = top;
+                u = block_inverse(top);
             }
-            const float u = sc.inverse;
             if (FULL || (i * S::kWarps + warp < nr && lane * 4 < nc))   // (up to three bytes of a row's padding are written too)
                 *reinterpret_cast<unsigned*>(q) = to_e4m3x4(v[i].get(0) * u, v[i].get(1) * u, v[i].get(2) * u, v[i].get(3) * u);
         }
-        if (!SQUARE && lane < S::kRows && lane * S::kWarps + warp < nr) *scale_byte(p.q, r0 + lane * S::kWarps + warp, cb) = (uint8_t)mine;
+        if (!SQUARE && lane < S::kRows && lane * S::kWarps + warp < nr) *scale_byte(p.q, r0 + lane * S::kWarps + warp, cb) = (uint8_t)block_exponent(mine);
     }
     if (p.qt.q) {
         constexpr int kCols = 128 / S::kWarps;              // of the warp, consecutive
@@ -154,15 +156,15 @@ __device__ __forceinline__ void quantize_tile(const QuantParams& p, T* tile, uns
 #pragma unroll
             for (int i = 0; i < 4; ++i, q += p.qt.ld) {
                 if (!SQUARE) {
-                    sc = block_scale(__reduce_max_sync(0xFFFFFFFFu, top[i]));
-                    if (lane == k + i) mine = sc.exponent;
+                    const unsigned most = __reduce_max_sync(0xFFFFFFFFu, top[i]);
+                    if (lane == k + i) mine = most;
+                    u = block_inverse(most);
                 }
-                const float u = sc.inverse;
                 if (FULL || (warp * kCols + k + i < nc && lane * 4 < nr))
                     *reinterpret_cast<unsigned*>(q) = to_e4m3x4(w[0].get(i) * u, w[1].get(i) * u, w[2].get(i) * u, w[3].get(i) * u);
             }
         }
-        if (!SQUARE && lane < kCols && warp * kCols + lane < nc) *scale_byte(p.qt, c0 + warp * kCols + lane, rb) = (uint8_t)mine;
+        if (!SQUARE && lane < kCols && warp * kCols + lane < nc) *scale_byte(p.qt, c0 + warp * kCols + lane, rb) = (uint8_t)block_exponent(mine);
     }
 }
 

@@ -103,8 +103,8 @@ int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ld
                    size_t workspace_bytes, dst_stream_t stream);
 
 /*
- * out[m, n] = sum_k x[m, k] w[n, k] with x quantised on the way (ROW blocks, into the workspace):
- * dst_quantize_fp8 and dst_matmul_fp8 in one call.
+ * out[m, n] = sum_k x[m, k] w[n, k] with x quantised on the way (ROW blocks): dst_quantize_fp8 and dst_matmul_fp8 in one
+ * call, and for a few rows (up to 40 blocks of 128 elements, of up to 2048 columns) in one kernel.
  */
 size_t dst_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const dst_fp8_t* w, void* out, int64_t ldo,

@@ -64,19 +64,18 @@ def quantize(x, block_rows):
     x = np.asarray(x, np.float64)
     rows, cols = x.shape
     kb, rb = -(-cols // 128), -(-rows // block_rows)
-    codes, scale = np.zeros((rows, cols), np.uint8), np.zeros((kb, rb))
-    for j in range(kb):
-        for i in range(rb):
-            part = x[i * block_rows:(i + 1) * block_rows, j * 128:(j + 1) * 128]
-            if not np.isfinite(part).all():
-                scale[j, i] = np.nan
-                continue
-            amax, e = max(np.abs(part).max(), 2.0 ** -100), -200
-            while 448 * 2.0 ** e < amax:
-                e += 1
-            scale[j, i] = 2.0 ** e
-            codes[i * block_rows:(i + 1) * block_rows, j * 128:(j + 1) * 128] = to_e4m3(part / 2.0 ** e)
-    return codes, scale
+    blocks = np.zeros((rb * block_rows, kb * 128))
+    blocks[:rows, :cols] = x
+    blocks = blocks.reshape(rb, block_rows, kb, 128)
+    bad = ~np.isfinite(blocks).all((1, 3))
+    amax = np.maximum(np.abs(np.where(bad[:, None, :, None], 0, blocks)).max((1, 3)), 2.0 ** -100)
+    e = np.full(amax.shape, -120.0)
+    while (short := 448 * 2.0 ** e < amax).any():          # the smallest power of two that is large enough
+        e += short
+    unit = 2.0 ** e
+    with np.errstate(invalid="ignore"):
+        codes = to_e4m3(np.where(bad[:, None, :, None], 0, blocks) / unit[:, None, :, None])
+    return codes.reshape(rb * block_rows, kb * 128)[:rows, :cols], np.where(bad, np.nan, unit).T
 
 
 def dequantize(codes, scale, block_rows):

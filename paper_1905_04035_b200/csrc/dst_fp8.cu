@@ -218,23 +218,27 @@ constexpr int kBlockK = 128;                              // one scale's worth o
 constexpr int kTileP = 128;                               // rows of P a CTA
 constexpr int kSmemMost = 232448;
 
-template <int CG, int NT>
+// FUSED: Q is quantised by the CTA itself from the rows of x, kept whole in shared memory (kResident bytes) and used for
+// every tile; its result leaves swapped.
+template <int CG, int NT, bool FUSED = false>
 struct TileShape {
     static constexpr int kQRows = NT / CG;                // rows of Q a CTA holds
     static constexpr int kEpiWarps = NT > 128 ? 8 : 4;
     static constexpr int kCols = NT > 128 ? 128 : NT;     // columns of the result an epilogue warp holds
     static constexpr int kThreads = (kEpiWarps + 2) * 32;
-    static constexpr int kStageBytes = (kTileP + kQRows) * kBlockK;
+    static constexpr int kStageBytes = (kTileP + (FUSED ? 0 : kQRows)) * kBlockK;
     static constexpr int kQScaleTiles = (NT + 127) / 128;
-    static constexpr int kScaleBytes = (1 + kQScaleTiles) * kScaleTile;   // of four blocks
+    static constexpr int kScaleBytes = (1 + (FUSED ? 0 : kQScaleTiles)) * kScaleTile;   // of four blocks
+    static constexpr int kResident = FUSED ? 32768 : 0;
+    static constexpr int kResidentScales = FUSED ? kResident / NT / 512 * kScaleTile : 0;
     // bytes of shared memory a lane stages its row in: 256 at most, and room to start anywhere in 16
-    static constexpr int kOutPitch = (kCols < 64 ? kCols * 4 : 256) + 16, kOutBytes = kEpiWarps * 32 * kOutPitch;
+    static constexpr int kOutPitch = (kCols < 64 ? kCols * 4 : 256) + 16, kOutBytes = FUSED ? 0 : kEpiWarps * 32 * kOutPitch;
     static constexpr int kHeaderBytes = 1024;
     // small tiles wait for memory, not for each other: two CTAs share an SM
     static constexpr int kCtas = NT <= 64 ? 2 : 1;
-    static constexpr int kFit = (kSmemMost / kCtas - (kCtas - 1) * 1024 - kOutBytes - kHeaderBytes) / (kStageBytes + kScaleBytes);
+    static constexpr int kFit = (kSmemMost / kCtas - (kCtas - 1) * 1024 - kOutBytes - kResident - kResidentScales - kHeaderBytes) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kFit < 8 ? kFit : 8;
-    static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kOutBytes + kHeaderBytes;
+    static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kResident + kResidentScales + kOutBytes + kHeaderBytes;
     // tensor memory: one or two results, then a ring of scales (P's four columns, then Q's; four groups of four blocks)
     static constexpr int kBufs = NT > 128 ? 1 : 2;
     static constexpr int kScaleCols = 4 * (1 + kQScaleTiles), kScaleRing = 4;
@@ -250,6 +254,10 @@ struct MatmulParams {
     void* out;
     long long ldo;
     long long split_stride;                               // elements between the parts' results (splits > 1)
+    const void* x;                                        // FUSED: Q before its quantisation
+    long long ldx;
+    long long cols;
+    int x_type, x_vec;                                    // rows aligned to four elements
 };
 
 __device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -410,18 +418,54 @@ __device__ __forceinline__ void store_swapped(const MatmulParams& p, OT* out, co
         if (col0 + c < p.rows_q) out[(long long)(col0 + c) * p.ldo + row] = from_float<OT>(acc[c]);
 }
 
-template <int CG, int NT, typename OT>
-__global__ void __launch_bounds__(TileShape<CG, NT>::kThreads, TileShape<CG, NT>::kCtas)
+// x's rows as ROW blocks straight into the shared-memory form of an operand: the swizzle exchanges the 16-byte pieces of a
+// 128-byte row by the row's number.  A unit is a block of a row and belongs to a warp, eight at a time.
+template <typename T, int NT>
+__device__ __forceinline__ void quantize_resident(const MatmulParams& p, long long cols, unsigned char* q, unsigned char* scales, int warps) {
+    const int lane = lane_id(), units = p.rows_q * p.blocks;
+    using Raw = decltype(Four<T>::v);
+    for (int u0 = warp_id(); u0 < units; u0 += 8 * warps) {
+        Four<T> v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int unit = u0 + j * warps, row = unit % p.rows_q, block = unit / p.rows_q;
+            const long long c = (long long)block * kBlockK + lane * 4;
+            const T* const x = static_cast<const T*>(p.x) + row * p.ldx + c;
+            v[j].clear();
+            if (unit < units) {
+                if (p.x_vec && c + 4 <= cols) v[j].v = *reinterpret_cast<const Raw*>(x);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (c + i < cols) v[j].set(i, x[i]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int unit = u0 + j * warps, row = unit % p.rows_q, block = unit / p.rows_q;
+            if (unit >= units) break;
+            const unsigned top = __reduce_max_sync(0xFFFFFFFFu, v[j].amax());
+            const float u = block_inverse(top);
+            *reinterpret_cast<unsigned*>(q + block * (NT * kBlockK) + row * kBlockK + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4) =
+                to_e4m3x4(v[j].get(0) * u, v[j].get(1) * u, v[j].get(2) * u, v[j].get(3) * u);
+            if (lane == 0) scales[(block >> 2) * kScaleTile + (row & 31) * 16 + (row >> 5) * 4 + (block & 3)] = (uint8_t)block_exponent(top);
+        }
+    }
+}
+
+template <int CG, int NT, bool FUSED, typename OT>
+__global__ void __launch_bounds__(TileShape<CG, NT, FUSED>::kThreads, TileShape<CG, NT, FUSED>::kCtas)
 k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
              const __grid_constant__ CUtensorMap map_sq, const __grid_constant__ MatmulParams p) {
-    using S = TileShape<CG, NT>;
+    using S = TileShape<CG, NT, FUSED>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    unsigned char* const scale_ring = smem + S::kStages * S::kStageBytes;
-    unsigned char* const out_rows = scale_ring + S::kStages * S::kScaleBytes;
+    unsigned char* const resident = smem + S::kStages * S::kStageBytes;              // FUSED: Q, a block after the other
+    unsigned char* const scale_ring = resident + S::kResident;
+    unsigned char* const resident_scales = scale_ring + S::kStages * S::kScaleBytes;
+    unsigned char* const out_rows = resident_scales + S::kResidentScales;
     unsigned char* const header = out_rows + S::kOutBytes;
     unsigned* const tmem_slot = reinterpret_cast<unsigned*>(header);
     const unsigned bars = smem_addr(header + 16);
-    const unsigned full = bars, empty = bars + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 8 * S::kBufs;
+    const unsigned full = bars, empty = bars + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 8 * S::kBufs, q_ready = tmem_empty + 8 * S::kBufs;
     const int warp = warp_id(), lane = lane_id();
     const unsigned rank = CG == 2 ? (unsigned)(blockIdx.x & 1) : 0u;               // of the pair; 0 issues for both
     const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
@@ -430,6 +474,7 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) { bar_init(full + 8 * i, 1); bar_init(empty + 8 * i, 1); }
         for (int i = 0; i < S::kBufs; ++i) { bar_init(tmem_full + 8 * i, 1); bar_init(tmem_empty + 8 * i, CG * S::kEpiWarps); }
+        if (FUSED) bar_init(q_ready, S::kEpiWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -478,10 +523,11 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
                     if (rank == 0) bar_expect(full + 8 * s, CG * (S::kStageBytes + (scales ? S::kScaleBytes : 0)));
                     const unsigned at = stages + s * S::kStageBytes, sc = ring + s * S::kScaleBytes;
                     copy_tile<CG>(at, &map_p, b * kBlockK, (tp * CG + (int)rank) * kTileP, bar);
-                    copy_tile<CG>(at + kTileP * kBlockK, &map_q, b * kBlockK, tq * NT + (int)rank * S::kQRows, bar);
+                    if (!FUSED) copy_tile<CG>(at + kTileP * kBlockK, &map_q, b * kBlockK, tq * NT + (int)rank * S::kQRows, bar);
                     if (scales) {                                                  // all of Q's for both CTAs: each has every column
                         copy_scales<CG>(sc, &map_sp, b >> 2, tp * CG + (int)rank, bar);
-                        for (int i = 0; i < S::kQScaleTiles; ++i) copy_scales<CG>(sc + (1 + i) * kScaleTile, &map_sq, b >> 2, tq * S::kQScaleTiles + i, bar);
+                        if (!FUSED)
+                            for (int i = 0; i < S::kQScaleTiles; ++i) copy_scales<CG>(sc + (1 + i) * kScaleTile, &map_sq, b >> 2, tq * S::kQScaleTiles + i, bar);
                     }
                     used = min(used + 1, S::kStages);
                     if (++s == S::kStages) { s = 0; phase ^= 1; }
@@ -500,6 +546,8 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
             // The instruction queue is shallow: whatever this thread does between two blocks beyond two instructions' time
             // leaves the tensor cores idle, so the loop counts and never divides.
             const uint64_t operands = operand_desc(smem_addr(smem)), scales = scale_desc(smem_addr(scale_ring));
+            const uint64_t own = operand_desc(smem_addr(resident)), own_scales = scale_desc(smem_addr(resident_scales));
+            if (FUSED) ok = bar_wait(q_ready, 0);
             int s = 0, buf = 0, slot = 0;
             unsigned phase = 0, buf_phase = 1;
             for (int item = worker; item < items && ok; item += workers) {
@@ -516,9 +564,10 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
                         sc = tmem + S::kBufs * NT + slot * S::kScaleCols;
                         slot = (slot + 1) & (S::kScaleRing - 1);
 #pragma unroll
-                        for (int i = 0; i < 1 + S::kQScaleTiles; ++i) tmem_copy_scales<CG>(sc + 4 * i, scales + ((s * S::kScaleBytes + i * kScaleTile) >> 4));
+                        for (int i = 0; i < 1 + S::kQScaleTiles; ++i)
+                            tmem_copy_scales<CG>(sc + 4 * i, FUSED && i > 0 ? own_scales + (((b >> 2) * kScaleTile) >> 4) : scales + ((s * S::kScaleBytes + i * kScaleTile) >> 4));
                     }
-                    const uint64_t a = operands + ((s * S::kStageBytes) >> 4), q = a + ((kTileP * kBlockK) >> 4);
+                    const uint64_t a = operands + ((s * S::kStageBytes) >> 4), q = FUSED ? own + ((b * NT * kBlockK) >> 4) : a + ((kTileP * kBlockK) >> 4);
                     const unsigned id = idesc | (unsigned)(b & 3) << 4 | (unsigned)(b & 3) << 29;   // which of the four bytes
 #pragma unroll
                     for (int k = 0; k < kBlockK / 32; ++k)                          // 32 bytes of the inner dimension each
@@ -535,6 +584,13 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
         const unsigned mine = tmem + ((unsigned)(quarter * 32) << 16) + group * 128;
         unsigned char* const buffer = out_rows + threadIdx.x * S::kOutPitch;
         const unsigned free_bar = in_cta(tmem_empty, 0);
+        if (FUSED) {
+            if (p.x_type == DST_F32) quantize_resident<float, NT>(p, p.cols, resident, resident_scales, S::kEpiWarps);
+            else quantize_resident<__nv_bfloat16, NT>(p, p.cols, resident, resident_scales, S::kEpiWarps);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // the tensor cores read it
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(in_cta(q_ready, 0));
+        }
         int buf = 0;
         unsigned buf_phase = 0;
         for (int item = worker; item < items; item += workers) {
@@ -560,7 +616,7 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
                 for (int i = 0; i < S::kCols; ++i) acc[i] = __uint_as_float(0x7FC00000u);
             }
             OT* const out = static_cast<OT*>(p.out) + part * p.split_stride;
-            if (p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
+            if (FUSED || p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
             else store_row<OT, S::kCols>(p, out, acc, buffer, row0 + lane, col0);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -673,11 +729,11 @@ static bool scale_map(CUtensorMap& map, const Fp8View& m) {
 }
 
 struct MatmulMaps { CUtensorMap p, q, sp, sq; };
-template <int CG, int NT, typename OT>
+template <int CG, int NT, bool FUSED, typename OT>
 static cudaError_t matmul_launch(const MatmulMaps& m, const MatmulParams& p, int sms, cudaStream_t stream) {
-    using S = TileShape<CG, NT>;
+    using S = TileShape<CG, NT, FUSED>;
     static SmemOptIn opt;
-    const cudaError_t e = ensure_dynamic_smem(k_matmul_fp8<CG, NT, OT>, S::kSmem, opt);
+    const cudaError_t e = ensure_dynamic_smem(k_matmul_fp8<CG, NT, FUSED, OT>, S::kSmem, opt);
     if (e != cudaSuccess) return e;
     const long long items = (long long)p.tiles_p * p.tiles_q * p.splits, workers = sms / CG * S::kCtas;
     cudaLaunchConfig_t cfg = {};
@@ -689,11 +745,11 @@ static cudaError_t matmul_launch(const MatmulMaps& m, const MatmulParams& p, int
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_matmul_fp8<CG, NT, OT>, m.p, m.q, m.sp, m.sq, p);
+    return cudaLaunchKernelEx(&cfg, k_matmul_fp8<CG, NT, FUSED, OT>, m.p, m.q, m.sp, m.sq, p);
 }
-template <int CG, int NT>
+template <int CG, int NT, bool FUSED = false>
 static cudaError_t matmul_nt(const MatmulMaps& m, const MatmulParams& p, int out_type, int sms, cudaStream_t stream) {
-    return out_type == DST_F32 ? matmul_launch<CG, NT, float>(m, p, sms, stream) : matmul_launch<CG, NT, __nv_bfloat16>(m, p, sms, stream);
+    return out_type == DST_F32 ? matmul_launch<CG, NT, FUSED, float>(m, p, sms, stream) : matmul_launch<CG, NT, FUSED, __nv_bfloat16>(m, p, sms, stream);
 }
 
 cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace, int sms, cudaStream_t stream) {
@@ -701,7 +757,7 @@ cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, lon
     const Fp8View &vp = L.swap ? b : a, &vq = L.swap ? a : b;
     MatmulMaps m;
     if (!operand_map(m.p, vp, kTileP) || !operand_map(m.q, vq, L.nt / L.cg) || !scale_map(m.sp, vp) || !scale_map(m.sq, vq)) return cudaErrorInvalidValue;
-    MatmulParams p{(int)vp.rows, (int)vq.rows, (int)L.blocks, L.splits, (int)L.tiles_p, (int)L.tiles_q, L.swap, out, ldo, 0};
+    MatmulParams p{(int)vp.rows, (int)vq.rows, (int)L.blocks, L.splits, (int)L.tiles_p, (int)L.tiles_q, L.swap, out, ldo, 0, nullptr, 0, 0, 0, 0};
     int type = out_type;
     if (L.splits > 1) { p.out = workspace; p.ldo = b.rows; p.split_stride = a.rows * b.rows; type = DST_F32; }
     cudaError_t e;
@@ -718,6 +774,26 @@ cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, lon
     const float* parts = static_cast<const float*>(workspace);
     if (out_type == DST_F32) return launch_pdl(k_join_parts<float>, grid, dim3(256), 0, stream, parts, p.split_stride, L.splits, static_cast<float*>(out), ldo, (long long)a.rows, (int)b.rows);
     return launch_pdl(k_join_parts<__nv_bfloat16>, grid, dim3(256), 0, stream, parts, p.split_stride, L.splits, static_cast<__nv_bfloat16*>(out), ldo, (long long)a.rows, (int)b.rows);
+}
+
+// A few rows of x against a whole weight, quantised by every CTA for itself while the weight's first tiles are on their way:
+// where they fit next to the ring of stages, the inner dimension stays whole, and the blocks are few enough for the four
+// epilogue warps (against the two-kernel form, 1024 columns: 1 row 7.9 and 10.3 us, 4 rows 9.1 and 10.3, 6 rows 10.8 and 10.7,
+// 16 rows 15.0 and 11.0).
+bool linear_fp8_fused(long long M, long long N, long long K) {
+    const MatmulPlan L = plan_matmul(M, N, K);
+    return L.swap && L.nt == 16 && L.splits == 1 && L.blocks * L.nt * kBlockK <= TileShape<1, 16, true>::kResident && M * L.blocks <= 40;
+}
+cudaError_t launch_linear_fp8_fused(const void* x, long long ldx, int x_type, long long M, const Fp8View& w, void* out, long long ldo, int out_type,
+                                    int sms, cudaStream_t stream) {
+    const MatmulPlan L = plan_matmul(M, w.rows, w.cols);
+    MatmulMaps m;
+    if (!operand_map(m.p, w, kTileP) || !scale_map(m.sp, w)) return cudaErrorInvalidValue;
+    m.q = m.p; m.sq = m.sp;                                      // (not read)
+    const size_t size = x_type == DST_F32 ? 4 : 2;
+    const int vec = (reinterpret_cast<uintptr_t>(x) & (4 * size - 1)) == 0 && ldx % 4 == 0;
+    const MatmulParams p{(int)w.rows, (int)M, (int)L.blocks, 1, (int)L.tiles_p, 1, 1, out, ldo, 0, x, ldx, w.cols, x_type, vec};
+    return matmul_nt<1, 16, true>(m, p, out_type, sms, stream);
 }
 
 }  // namespace dst

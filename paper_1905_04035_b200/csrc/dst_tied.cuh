@@ -67,6 +67,10 @@ size_t matmul_fp8_workspace_bound(long long M, long long N, long long K);  // of
 cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace,
                               int sms, cudaStream_t stream);
 
+bool linear_fp8_fused(long long M, long long N, long long K);               // x can be quantised inside the product
+cudaError_t launch_linear_fp8_fused(const void* x, long long ldx, int x_type, long long M, const Fp8View& w, void* out, long long ldo,
+                                    int out_type, int sms, cudaStream_t stream);
+
 // ---- sampling (dst_sample.cu) -----------------------------------------------------
 struct SampleParams {
     const void* logits;

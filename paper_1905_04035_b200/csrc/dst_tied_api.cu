@@ -176,6 +176,8 @@ int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const 
     if (w->cols > 0) {
         if (!workspace || misaligned(workspace, 256)) return DST_ERR_INVALID_ARG;
         if (workspace_bytes < L.off_matmul + matmul_fp8_workspace(M, w->rows, w->cols)) return DST_ERR_WORKSPACE_TOO_SMALL;
+        if (linear_fp8_fused(M, w->rows, w->cols))
+            return done(launch_linear_fp8_fused(x, ldx, x_type, M, v, out, ldo, out_type, device_sm_count(), stream), 1);
         a.q = workspace;
         a.scale = static_cast<char*>(workspace) + L.off_scale;
         const int rq = dst_quantize_fp8(x, ldx, x_type, M, w->cols, &a, nullptr, stream);

@@ -293,7 +293,7 @@ def test_matmul_of_nothing():
     dst.dst_matmul_fp8(dst.Fp8Matrix(0, 64), dst.Fp8Matrix(5, 64), torch.empty(0, 5, device="cuda"))
 
 
-@pytest.mark.parametrize("M,V,D", [(1, 1000, 64), (7, 500, 130), (150, 1000, 512), (300, 2000, 333)])
+@pytest.mark.parametrize("M,V,D", [(1, 1000, 64), (7, 500, 130), (150, 1000, 512), (300, 2000, 333), (2, 10000, 2048), (5, 9000, 700), (33, 1500, 500), (64, 2000, 512), (17, 40, 64), (3, 8000, 1021)])
 @pytest.mark.parametrize("xt,ot", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
 def test_projection_and_its_gradients(M, V, D, xt, ot):
     """logits, dx and dweight against the formulas on the 8-bit operands; a smaller batch through the same object."""

@@ -94,7 +94,7 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
 /*
  * out[m, n] = sum over column blocks b of a.scale(m, b) * b.scale(n, b) * sum_{k in b} a.q[m, k] * b.q[n, k]
  * a [M, K], b [N, K], out [M, N] in out_type (fp32 or bf16, rounded once).  All sums are fp32 in an order fixed by the
- * shapes.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes (may be 0), 256-byte aligned;
+ * shapes and out_type.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes (may be 0), 256-byte aligned;
  * as much is enough for every smaller M, N and K too.  A device-side wait that gives up leaves NaN in the part of `out`
  * that was still to be written.
  */

@@ -202,8 +202,7 @@ cudaError_t launch_quantize(const QuantParams& p, int x_type, cudaStream_t strea
 // ---- product ----------------------------------------------------------------------
 // D[p, q] = sum over blocks b of sp[b, p] sq[b, q] (P_b Q_b^T).  The scales are powers of two in the form the tensor
 // cores multiply by themselves (one scale for 32 elements of the inner dimension; the four steps of a block use the same
-// byte), so the whole sum stays in tensor memory and the epilogue sees a finished tile (fp32 sums:
-// 1.3e-7 relative for random signs over 33,708 terms, 5e-7 where all terms are positive).  P is the operand whose rows are
+// byte), so whole stretches of the inner dimension are summed in tensor memory and the epilogue sees finished tiles.  P is the operand whose rows are
 // the 128 lanes of tensor memory, Q the one whose rows are its columns.
 //
 // Both sides large: two CTAs share a 256 x 256 tile (each holds 128 rows of P, half of Q's rows, and 128 x 256 of
@@ -457,6 +456,13 @@ __global__ void __launch_bounds__(TileShape<CG, NT, FUSED>::kThreads, TileShape<
 k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
              const __grid_constant__ CUtensorMap map_sq, const __grid_constant__ MatmulParams p) {
     using S = TileShape<CG, NT, FUSED>;
+    // Blocks summed in tensor memory before that sum is added to the one in registers.  Additions there do not round to
+    // nearest: where one block outweighs the ones after it, each of them takes up to a unit off.  On the gradients of 8111
+    // tokens by 33,708 words (K 33,708 and 8111) the error is 3.3e-5 and 4.8e-6 with no limit, 1.9e-6 and 1.2e-6 with 16
+    // blocks, 9e-7 and 6e-7 with 8, 4.8e-7 and 3.2e-7 with 4 (fp32 products: 3.8e-6 and 1.2e-6), for 520, 542, 556 and 593 us.
+    // A bf16 result has 2e-3 from its own rounding, and no limit.
+    constexpr bool kChunked = sizeof(OT) == 4;
+    constexpr int kChunk = 8;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const resident = smem + S::kStages * S::kStageBytes;              // FUSED: Q, a block after the other
     unsigned char* const scale_ring = resident + S::kResident;
@@ -553,30 +559,34 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
             for (int item = worker; item < items && ok; item += workers) {
                 int tp, tq, k0, k1;
                 item_of(item, tp, tq, k0, k1);
-                ok = bar_wait(tmem_empty + 8 * buf, buf_phase);
-                const unsigned d = tmem + buf * NT;
                 unsigned sc = 0;
-                for (int b = k0; b < k1 && ok; ++b) {
-                    ok = bar_wait(full + 8 * s, phase);
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if ((b & 3) == 0) {
-                        sc = tmem + S::kBufs * NT + slot * S::kScaleCols;
-                        slot = (slot + 1) & (S::kScaleRing - 1);
+                for (int start = k0; start < k1 && ok; start += kChunk) {
+                    ok = bar_wait(tmem_empty + 8 * buf, buf_phase);
+                    const unsigned d = tmem + buf * NT;
+                    const int end = kChunked ? min(start + kChunk, k1) : k1;
+                    for (int b = start; b < end && ok; ++b) {
+                        ok = bar_wait(full + 8 * s, phase);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if ((b & 3) == 0) {
+                            sc = tmem + S::kBufs * NT + slot * S::kScaleCols;
+                            slot = (slot + 1) & (S::kScaleRing - 1);
 #pragma unroll
-                        for (int i = 0; i < 1 + S::kQScaleTiles; ++i)
-                            tmem_copy_scales<CG>(sc + 4 * i, FUSED && i > 0 ? own_scales + (((b >> 2) * kScaleTile) >> 4) : scales + ((s * S::kScaleBytes + i * kScaleTile) >> 4));
+                            for (int i = 0; i < 1 + S::kQScaleTiles; ++i)
+                                tmem_copy_scales<CG>(sc + 4 * i, FUSED && i > 0 ? own_scales + (((b >> 2) * kScaleTile) >> 4) : scales + ((s * S::kScaleBytes + i * kScaleTile) >> 4));
+                        }
+                        const uint64_t a = operands + ((s * S::kStageBytes) >> 4), q = FUSED ? own + ((b * NT * kBlockK) >> 4) : a + ((kTileP * kBlockK) >> 4);
+                        const unsigned id = idesc | (unsigned)(b & 3) << 4 | (unsigned)(b & 3) << 29;   // which of the four bytes
+#pragma unroll
+                        for (int k = 0; k < kBlockK / 32; ++k)                      // 32 bytes of the inner dimension each
+                            mma_fp8<CG>(d, a + 2 * k, q + 2 * k, id, sc, sc + 4, b > start || k > 0);
+                        mma_commit<CG>(empty + 8 * s);
+                        if (++s == S::kStages) { s = 0; phase ^= 1; }
                     }
-                    const uint64_t a = operands + ((s * S::kStageBytes) >> 4), q = FUSED ? own + ((b * NT * kBlockK) >> 4) : a + ((kTileP * kBlockK) >> 4);
-                    const unsigned id = idesc | (unsigned)(b & 3) << 4 | (unsigned)(b & 3) << 29;   // which of the four bytes
-#pragma unroll
-                    for (int k = 0; k < kBlockK / 32; ++k)                          // 32 bytes of the inner dimension each
-                        mma_fp8<CG>(d, a + 2 * k, q + 2 * k, id, sc, sc + 4, b > k0 || k > 0);
-                    mma_commit<CG>(empty + 8 * s);
-                    if (++s == S::kStages) { s = 0; phase ^= 1; }
+                    if (ok) mma_commit<CG>(tmem_full + 8 * buf);
+                    if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
+                    if (!kChunked) break;
                 }
-                if (ok) mma_commit<CG>(tmem_full + 8 * buf);
-                if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
             }
         }
     } else {                                                                       // ---- epilogue ----
@@ -598,19 +608,40 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
             const int part = item_of(item, tp, tq, k0, k1);
             const int row0 = (tp * CG + (int)rank) * kTileP + quarter * 32, col0 = tq * NT + group * 128;
             float acc[S::kCols];
-            if (ok) ok = bar_wait(tmem_full + 8 * buf, buf_phase);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (ok) {
+            auto sums_ready = [&] {
+                if (ok) ok = bar_wait(tmem_full + 8 * buf, buf_phase);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            auto sums_taken = [&] {                                                // the next ones may start
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(free_bar + 8 * buf);
+                if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
+            };
+            if (sums_ready()) {
 #pragma unroll
                 for (int c = 0; c < S::kCols; c += 16) tmem_load16(mine + buf * NT + c, *reinterpret_cast<float (*)[16]>(acc + c));
 #pragma unroll
                 for (int c = 0; c < S::kCols; c += 16) tmem_wait(*reinterpret_cast<float (*)[16]>(acc + c));
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive_cluster(free_bar + 8 * buf);              // the next tile's sums may start
+                sums_taken();
             }
-            if (++buf == S::kBufs) { buf = 0; buf_phase ^= 1; }
+#pragma unroll 1
+            for (int b = k0 + kChunk; kChunked && b < k1; b += kChunk) {
+                if (!sums_ready()) break;
+                float v[2][16];
+                tmem_load16(mine + buf * NT, v[0]);
+#pragma unroll
+                for (int c = 0; c < S::kCols; c += 16) {
+                    float (&x)[16] = v[(c >> 4) & 1];
+                    tmem_wait(x);
+                    if (c + 16 < S::kCols) tmem_load16(mine + buf * NT + c + 16, v[((c >> 4) & 1) ^ 1]);
+                    else sums_taken();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c + i] += x[i];
+                }
+            }
             if (!ok) {
 #pragma unroll
                 for (int i = 0; i < S::kCols; ++i) acc[i] = __uint_as_float(0x7FC00000u);

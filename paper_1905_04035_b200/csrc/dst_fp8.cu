@@ -458,11 +458,12 @@ k_matmul_fp8(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ 
     using S = TileShape<CG, NT, FUSED>;
     // Blocks summed in tensor memory before that sum is added to the one in registers.  Additions there do not round to
     // nearest: where one block outweighs the ones after it, each of them takes up to a unit off.  On the gradients of 8111
-    // tokens by 33,708 words (K 33,708 and 8111) the error is 3.3e-5 and 4.8e-6 with no limit, 1.9e-6 and 1.2e-6 with 16
-    // blocks, 9e-7 and 6e-7 with 8, 4.8e-7 and 3.2e-7 with 4 (fp32 products: 3.8e-6 and 1.2e-6), for 520, 542, 556 and 593 us.
-    // A bf16 result has 2e-3 from its own rounding, and no limit.
+    // tokens by 33,708 words (fp32 dx and dweight, K 33,708 and 8111) the errors are 3.3e-5 and 4.8e-6 with no limit, 1.9e-6
+    // and 1.2e-6 with 16 blocks, 9e-7 and 6e-7 with 8, 7e-7 and 4.5e-7 with 6, 4.8e-7 and 3.2e-7 with 4 (products in fp32:
+    // 3.8e-6 and 1.2e-6), for 520, 542, 556, 561 and 593 us together.  A bf16 result has 2e-3 from its own rounding, and
+    // no limit.
     constexpr bool kChunked = sizeof(OT) == 4;
-    constexpr int kChunk = 8;
+    constexpr int kChunk = 6;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const resident = smem + S::kStages * S::kStageBytes;              // FUSED: Q, a block after the other
     unsigned char* const scale_ring = resident + S::kResident;

@@ -277,11 +277,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     }
     if (tid == 0) { s.candidates = 0; s.top_key = top_key; s.bound = edge; }
     sync();
-    unsigned bound = 0xFFFFFFFFu;
-    top_key = 0;
-    for (int c = 0; c < ctas; ++c) {
-        top_key = max(top_key, *cluster.map_shared_rank(&s.top_key, c));
-        bound = min(bound, *cluster.map_shared_rank(&s.bound, c));
+    unsigned bound = edge;
+    if (ctas > 1) {                                             // every warp asks all CTAs at once
+        bound = 0xFFFFFFFFu;
+        if (lane < ctas) { top_key = *cluster.map_shared_rank(&s.top_key, lane); bound = *cluster.map_shared_rank(&s.bound, lane); }
+        top_key = __reduce_max_sync(0xFFFFFFFFu, top_key);
+        bound = __reduce_min_sync(0xFFFFFFFFu, bound);
     }
 
     Weigh g;
@@ -319,7 +320,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         sync();
         const unsigned total = first->candidates;
         list = total <= kListMost;
-        sync();                                                 // (everybody has read it; the lists' memory may become the histograms')
         if (list) {
             if (rank != 0) return;                              // the rest is the first CTA's, with nobody else's memory
             const int count = (int)total;
@@ -445,6 +445,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
 #pragma unroll
             for (int r = 0; r < 2; ++r)
                 if (upto[r] - w[r] <= drawn && drawn < upto[r]) answer(order[r] >> 10, (float)w[r] / (float)sum);
+            if (ctas > 1) cluster.sync();                       // others may still be reading the number of candidates; those that left count as arrived
             return;
         }
     }

@@ -491,14 +491,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
                     const float f = v.get(i), z = g.z(f);
                     // to the nearest whole number of steps, by the bits of a sum with 2^23 (anything where the weight is 0)
                     unsigned b = min(__float_as_uint(__fmaf_rn(z, -kBinsPerZ, 8388608.f)) & 0x7FFFFFu, kBins - 1u);
-                    bool in = true;
-                    if (!coarse) {
+                    if (!coarse) {                                // few are in the bin: no exponential for the others
                         const unsigned key = key_of(f) >> kShift;
-                        in = b == bin && key <= hi && (hi - key) >> shift < kBins;
+                        if (b != bin || key > hi || (hi - key) >> shift >= kBins) continue;
                         b = (hi - key) >> shift;
                     }
                     const unsigned w = Weigh::weight(expf(z));
-                    if (w && in) {
+                    if (w) {
                         if (k) atomicAdd(&s.count[b], 1u);
                         atomicAdd(&s.low[b], w & 0xFFFFu);
                         if (w >> 16) atomicAdd(&s.high[b], w >> 16);

@@ -12,6 +12,10 @@
 // kept in index order.
 //
 // A row belongs to a cluster of 1, 2, 4 or 8 CTAs with a slice of it each, joined through distributed shared memory.
+//
+// Bound by: the list's short dependent phases (one row of 33,708 fp32 logits: 9.7 us; 512 rows of 65,536 in bf16: 40 us, of
+// which their 67 MB need 10); without top-k by the instructions and shared-memory additions an entry costs in every pass over
+// the row (512 x 65,536 bf16: top-p alone 193 us, min-p alone 52, no filter 78).
 #include <cooperative_groups.h>
 
 #include "dst_tied.cuh"

@@ -3,9 +3,10 @@
 Tolerances, with u = 2^-24 (fp32 rounding) and h = 2^-8 (half a bf16 step, relative):
   dropout    out = r + x (k s): three roundings, each at most u of |x k s| or |out|:   4u (|x k s| + |r|) (+ h |out|)
   embed      out = k (w s + p): three roundings:                                       4u k (|w s| + |p|) (+ h |out|)
-  product    terms are exact in fp32 (two 4-bit significands); a block's 128 are summed in fp32, at worst with
-             truncation (2u an addition), then one rounding a block for the scale and one for the running sum, and one
-             a part where the inner dimension is split: (128 + 2 blocks + 16) 2u sum|terms| (+ h |out|)
+  product    terms are exact in fp32 (two 4-bit significands, scales of powers of two); sums of 32 are added up in fp32,
+             at worst with truncation (2u an addition: four a block of 128, and up to 128 within the steps of one), and one
+             rounding for each stretch moved to registers and each part of the inner dimension:
+             (128 + 4 blocks + 16) 2u sum|terms| (+ h |out|)
   quantise   codes and scales are exact
   sample     tokens are exact wherever no decision of the definition is nearer than 2^-18 of the sums to falling
              otherwise (the exponential's error, 2 ulp, is below 2^-21); prob 2^-18
@@ -235,7 +236,7 @@ def product(a, b, block_a, block_b, ot, pad=0, skew=0, workspace=True):
     dst.dst_matmul_fp8(qa, qb, out, ws)
     assert torch.isnan(buf).sum() == buf.numel() - M * N
     A, B = np64(qa.dequantize()), np64(qb.dequantize())
-    tol = (128 + 2 * -(-K // 128) + 16) * 2 * U * (np.abs(A) @ np.abs(B).T)
+    tol = (128 + 4 * -(-K // 128) + 16) * 2 * U * (np.abs(A) @ np.abs(B).T)
     close(out, A @ B.T, tol, ot)
     return out
 
@@ -312,7 +313,7 @@ def test_projection_and_its_gradients(M, V, D, xt, ot):
         rows = lambda v: o.dequantize(*o.quantize(v, 1), 1)  # noqa: E731
         X, DL, XT, DLT = rows(np64(x)), rows(np64(dl)), rows(np64(x).T), rows(np64(dl).T)
         for got, a, b, t in ((logits, X, W.T, ot), (dx, DL, W, xt), (dw, DLT, XT.T, "f32")):
-            close(got, a @ b, (128 + 2 * -(-a.shape[1] // 128) + 16) * 2 * U * (np.abs(a) @ np.abs(b)), t)
+            close(got, a @ b, (128 + 4 * -(-a.shape[1] // 128) + 16) * 2 * U * (np.abs(a) @ np.abs(b)), t)
 
 
 def test_projection_gradient_against_differences():
@@ -474,3 +475,56 @@ def test_work_goes_to_the_stream_that_is_named():
     t2 = torch.empty_like(tokens)
     dst.dst_sample(want, u, t2)
     assert torch.equal(logits, want) and torch.equal(tokens, t2)
+
+
+# ---- offsets beyond 32 bits -----------------------------------------------------------------------------------------
+def test_rows_more_than_two_to_the_31_elements_apart():
+    """Row distances whose byte and element offsets pass 32 bits, in one buffer for inputs and outputs."""
+    ld, d = (1 << 31) + 8, 520
+    buf = torch.empty(2 * ld + 4 * d, dtype=torch.bfloat16, device="cuda")
+    rows = lambda at, n=d: buf[at:at + 2 * ld + n].as_strided((3, n), (ld, 1))  # noqa: E731
+    x, out = rows(0), rows(d)
+    x.copy_(randn((3, d), "bf16", 41))
+    out.zero_()
+    dst.dst_dropout(x, out, 0.25, 3, residual=x)
+    want = np64(x) * (1 + o.drop_factor(3, d, 0.25, 3))
+    close(out, want, 8 * U * np.abs(want), "bf16")
+    q, qt = dst.Fp8Matrix(3, d), dst.Fp8Matrix(d, 3)
+    dst.dst_quantize_fp8(x, q, qt)
+    assert np.array_equal(codes(q), o.quantize(np64(x), 1)[0]) and np.array_equal(codes(qt), o.quantize(np64(x).T, 1)[0])
+    w = dst.Fp8Matrix(d, d, dst.DST_FP8_SQUARE)
+    dst.dst_quantize_fp8(randn((d, d), seed=42), w)
+    ws = torch.empty(max(dst.dst_matmul_fp8_workspace_bytes(3, d, d), 256), dtype=torch.uint8, device="cuda")
+    dst.dst_matmul_fp8(q, w, out, ws)
+    A, B = np64(q.dequantize()), np64(w.dequantize())
+    close(out, A @ B.T, (128 + 4 * 5 + 16) * 2 * U * (np.abs(A) @ np.abs(B).T), "bf16")
+    s = settings(3, 43)
+    check_sample(x, s["u"], s["temperature"], s["top_k"], s["top_p"], s["min_p"])
+
+
+@pytest.mark.parametrize("n,d", [(70000, 32768)])
+def test_matrices_of_more_than_two_to_the_31_elements(n, d):
+    """2.3 billion elements through dropout, both quantisations and a thin product; rows from all over are checked."""
+    x = torch.empty(n, d, dtype=torch.bfloat16, device="cuda")
+    pattern = randn((1000, d), "bf16", 44)
+    for i in range(0, n, 1000):
+        x[i:i + 1000] = pattern
+    out = torch.empty_like(x)
+    dst.dst_dropout(x, out, 0.5, 11)
+    at = [0, 1, 65535, 65536, n - 1]
+    for r in at:
+        k = o.drop_factor(1, d, 0.5, 11, row_offset=r)
+        assert np.array_equal(np64(out[r:r + 1]), np64(x[r:r + 1]) * k)
+    del out
+    q = dst.Fp8Matrix(n, d)
+    dst.dst_quantize_fp8(x, q)
+    want = o.dequantize(*o.quantize(np64(x[at]), 1), 1)
+    got = torch.stack([q.q[r, :d].float() * q.scales()[r].repeat_interleave(128) for r in at])
+    assert np.array_equal(np64(got), want)
+    b = randn((20, d), seed=45)
+    qb = dst.Fp8Matrix(20, d)
+    dst.dst_quantize_fp8(b, qb)
+    y = torch.empty(n, 20, device="cuda")
+    dst.dst_matmul_fp8(q, qb, y, torch.empty(max(dst.dst_matmul_fp8_workspace_bytes(n, 20, d), 256), dtype=torch.uint8, device="cuda"))
+    B = np64(qb.dequantize())
+    close(y[at], want @ B.T, (128 + 4 * (d // 128) + 16) * 2 * U * (np.abs(want) @ np.abs(B).T), "f32")

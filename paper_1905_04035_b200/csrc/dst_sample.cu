@@ -575,7 +575,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     const float cut_e = equal_only ? 1.f : g.e(cut_key), least = cut_key > kLowestKey ? of_key(cut_key) : -INFINITY;
     const unsigned cut_w = cut_key && cut_e >= g.min_p ? Weigh::weight(cut_e) : 0u;
     // nothing below `skip` is kept: the cut, or what min-p leaves at most, taken a little lower than its logarithm can be off
-    const float skip = fmaxf(least, g.min_p > 0.f ? g.top + (logf(g.min_p) - 1e-3f) / g.inv_t * 1.0001f - fabsf(g.top) * 1e-6f : -INFINITY);
+    // (where only the largest count, the cut is the largest, which min-p never takes, and inv_t may be anything)
+    const float skip = equal_only || !(g.min_p > 0.f) ? least : fmaxf(least, g.top + (logf(g.min_p) - 1e-3f) / g.inv_t * 1.0001f - fabsf(g.top) * 1e-6f);
     auto kept = [&](float f) {                                    // weight of an entry above the cut
         const float e = expf(g.z(f));
         return f > least && e >= g.min_p ? Weigh::weight(e) : 0u;

@@ -1,0 +1,36 @@
+"""GPU tests of the operators around the tied weight at the ends of their arguments' ranges, against the 64-bit
+definitions (oracle/tied_oracle.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1905_04035_b200 as dst
+from oracle import tied_oracle as o
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24                                              # half a step of fp32, relative
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def draw_tokens(x, u, **settings):
+    """(tokens, prob) of dst_sample with one value of each setting for all rows."""
+    rows = x.shape[0]
+    full = lambda v, d=torch.float32: torch.full((rows,), v, dtype=d, device="cuda")  # noqa: E731
+    args = {name: full(v, torch.int32 if name == "top_k" else torch.float32) for name, v in settings.items() if v is not None}
+    tokens, prob = full(-7, torch.int64), full(-7.0)
+    dst.dst_sample(x, u if torch.is_tensor(u) else full(u), tokens, prob=prob, **args)
+    return tokens.cpu().numpy(), prob.cpu().numpy()
+
+
+# (rows, vocab): a row in one CTA as a list or not, a row over two, four and eight CTAs, more rows than CTAs at once
+@pytest.mark.parametrize("rows,vocab", [(3, 700), (2, 2000), (40, 4100), (20, 9000), (1, 33708), (400, 3000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top_k,top_p", [(None, None), (40, None), (None, 0.9), (40, 0.9)])
+def test_temperatures_not_above_zero_take_the_largest_logit_whatever_the_filters(rows, vocab, dtype, top_k, top_p):
+    x = (torch.randn(rows, vocab, generator=torch.Generator().manual_seed(vocab)) * 3).to(TYPES[dtype])
+    want = x.float().numpy().argmax(-1)                                          # the first of equal ones
+    x = x.cuda()
+    for t in (-1.0, -0.5, -1e-30, -1e30, float("-inf"), -0.0, 0.0, float("nan")):
+        for min_p in (None, 1e-30, 0.1, 1.0, 2.0):
+            tokens, prob = draw_tokens(x, 0.75, temperature=t, top_k=top_k, top_p=top_p, min_p=min_p)
+            assert np.array_equal(tokens, want) and (prob == 1).all(), (t, min_p)

@@ -55,7 +55,8 @@ int dst_dropout(const void* x, int64_t ldx, int32_t x_type, const void* residual
  * out[i, c] = k[i, c] * (scale * weight[indices[i], c] + (position ? position[i % n_positions, c] : 0))
  * indices [n_rows]; weight [vocab, d] contiguous in weight_type; position [n_positions, d] contiguous fp32 or NULL;
  * out [n_rows, d] contiguous in out_type; drop NULL: k = 1.  A row whose index lies outside [0, vocab) is written as
- * zeros and counted in `result` (optional DEVICE memory, cleared by this call: status and n_out_of_range are set).
+ * zeros and counted in `result` (optional DEVICE memory, cleared by this call: status and n_out_of_range are set); with
+ * vocab = 0 that is every row.
  * The value rows of this lookup's IndexedSlices gradient are dst_dropout(grad, scale, the same drop).
  */
 int dst_embed(const void* indices, int64_t n_rows, int32_t index_type, const void* weight, int64_t vocab, int64_t d,

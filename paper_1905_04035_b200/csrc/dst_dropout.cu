@@ -124,7 +124,9 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_any(const __grid_const
     }
 }
 
-// What a token's index says: where its row lies; an index outside the table is counted once and gives a row of zeros.
+// What a token's index says: where its row lies; an index outside the table is counted once and gives a row of zeros.  The
+// table's first row is read in its place, and not used (a table without rows does not come here): loads that depend
+// on the index's check took 25600 rows of 1024, bf16, from 25.3 to 27.8 us, and of 1021 from 43.0 to 46.4.
 template <typename IT>
 __device__ __forceinline__ bool token_row(const EmbedParams& p, long long row, bool counts, long long& index) {
     index = (long long)static_cast<const IT*>(p.indices)[row];
@@ -266,7 +268,21 @@ static cudaError_t embed_i(const EmbedParams& p, int weight_type, int out_type, 
     return out_type == DST_F32 ? embed_t<IT, __nv_bfloat16, float, POS>(p, sms, stream) : embed_t<IT, __nv_bfloat16, __nv_bfloat16, POS>(p, sms, stream);
 }
 
+// A table without rows: no index lies inside it.  Nothing is read; the zeros of `out` are a memset.
+__global__ void k_embed_none(dst_result_t* result, long long rows) {
+    pdl_trigger();
+    pdl_wait();
+    result->status = DST_ERR_INDEX_OUT_OF_RANGE;
+    result->n_out_of_range = rows;
+}
+static cudaError_t embed_none(const EmbedParams& p, int out_type, cudaStream_t stream) {
+    const cudaError_t e = cudaMemsetAsync(p.out, 0, size_t(p.rows) * size_t(p.d) * (out_type == DST_F32 ? 4 : 2), stream);
+    if (e != cudaSuccess || !p.result) return e;
+    return launch_pdl(k_embed_none, dim3(1), dim3(1), 0, stream, p.result, p.rows);
+}
+
 cudaError_t launch_embed(const EmbedParams& p, int index_type, int weight_type, int out_type, int sms, cudaStream_t stream) {
+    if (p.vocab == 0) return embed_none(p, out_type, stream);
     if (index_type == DST_I64) return p.position ? embed_i<long long, true>(p, weight_type, out_type, sms, stream) : embed_i<long long, false>(p, weight_type, out_type, sms, stream);
     return p.position ? embed_i<int, true>(p, weight_type, out_type, sms, stream) : embed_i<int, false>(p, weight_type, out_type, sms, stream);
 }

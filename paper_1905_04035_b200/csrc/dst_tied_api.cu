@@ -125,7 +125,7 @@ int dst_embed(const void* indices, int64_t n_rows, int32_t index_type, const voi
     p.step = UnitStep{};
     p.indices = indices; p.weight = weight; p.position = position; p.out = out; p.result = result;
     p.rows = n_rows; p.vocab = vocab; p.n_positions = n_positions; p.d = int(d); p.scale = scale;
-    return done(launch_embed(p, index_type, weight_type, out_type, device_sm_count(), stream), 1);
+    return done(launch_embed(p, index_type, weight_type, out_type, device_sm_count(), stream), vocab > 0 || result ? 1 : 0);
 }
 
 int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, int64_t cols, const dst_fp8_t* q,

@@ -34,3 +34,17 @@ def test_temperatures_not_above_zero_take_the_largest_logit_whatever_the_filters
         for min_p in (None, 1e-30, 0.1, 1.0, 2.0):
             tokens, prob = draw_tokens(x, 0.75, temperature=t, top_k=top_k, top_p=top_p, min_p=min_p)
             assert np.array_equal(tokens, want) and (prob == 1).all(), (t, min_p)
+
+
+@pytest.mark.parametrize("n,d", [(1, 8), (37, 64), (300, 512), (5, 61), (70, 1021)])
+@pytest.mark.parametrize("wt,ot,it", [("f32", "f32", torch.int64), ("bf16", "bf16", torch.int32), ("f32", "bf16", torch.int32), ("bf16", "f32", torch.int64)])
+@pytest.mark.parametrize("positions,p", [(0, 0.0), (3, 0.25)])
+def test_a_lookup_in_an_empty_table_gives_zeros_and_counts_every_index(n, d, wt, ot, it, positions, p):
+    weight = torch.empty(0, d, dtype=TYPES[wt], device="cuda")
+    assert weight.data_ptr() == 0                                                # there is nothing to read
+    idx = torch.arange(n, device="cuda").sub_(n // 2).to(it)
+    position = torch.ones(positions, d, device="cuda") if positions else None
+    out = torch.full((n, d), float("nan"), dtype=TYPES[ot], device="cuda")
+    result = torch.full((3,), 7, dtype=torch.int64, device="cuda")
+    dst.dst_embed(idx, weight, out, scale=3.0, position=position, p=p, seed=5, result=result)
+    assert (out == 0).all() and result.tolist() == [4, n, 0]

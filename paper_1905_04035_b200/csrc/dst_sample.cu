@@ -255,7 +255,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
     if (list && !short_row) {
         const unsigned want = (unsigned)((k + ctas - 1) / ctas);
         const float hi = of_key(top_key), lo = of_key(low_key);
-        const float per = hi > lo && hi - lo < INFINITY ? (kSampleThreads - 1) / (hi - lo) : 0.f;
+        float per = hi > lo && hi - lo < INFINITY ? (kSampleThreads - 1) / (hi - lo) : 0.f;
+        if (!(per < INFINITY)) per = 0.f;                       // maxima so close together that the bins have no width: one bin
         if (my_key > kLowestKey) atomicAdd(&s.bins[per > 0.f ? min((unsigned)((hi - mine) * per), (unsigned)kSampleThreads - 1) : 0u], 1u);
         __syncthreads();
         constexpr int kPer = kSampleThreads / 32;

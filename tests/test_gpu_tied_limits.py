@@ -48,3 +48,34 @@ def test_a_lookup_in_an_empty_table_gives_zeros_and_counts_every_index(n, d, wt,
     result = torch.full((3,), 7, dtype=torch.int64, device="cuda")
     dst.dst_embed(idx, weight, out, scale=3.0, position=position, p=p, seed=5, result=result)
     assert (out == 0).all() and result.tolist() == [4, n, 0]
+
+
+def check_draws(X, x, u, temperature, **settings):
+    """Tokens and probs of every row against the definition; rows where a decision hangs on the exponential's last bits
+    (nearer than 2^-18 of the sums) may differ, and are counted."""
+    rows = x.shape[0]
+    tokens, prob = draw_tokens(x, torch.tensor(u, dtype=torch.float32, device="cuda"), temperature=temperature, **settings)
+    unsure = 0
+    for r in range(rows):
+        token, p, margin = o.sample(X[r], float(np.float32(u[r])), float(np.float32(1.0 if temperature is None else temperature)), settings.get("top_k") or 0,
+                                    float(np.float32(settings.get("top_p") or 1.0)), float(np.float32(settings.get("min_p") or 0.0)))
+        if margin < 2.0 ** -18 and token != tokens[r]:
+            unsure += 1
+            continue
+        assert token == tokens[r] and abs(p - prob[r]) <= 2.0 ** -18, (r, token, tokens[r], p, prob[r], settings)
+    assert unsure <= 1 + rows // 50
+
+
+# rows of 1025 to 2048 entries, and many rows of any length, are one CTA's
+@pytest.mark.parametrize("rows,vocab", [(1, 2000), (5, 1100), (1, 4099), (80, 33708)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("most,rest", [(1e-40, 1e-42), (1e-37, 0.0), (1e-40, 0.0), (0.0, -1e-38), (3e-36, 0.0)])
+def test_top_k_of_logits_whose_differences_are_next_to_nothing(rows, vocab, dtype, most, rest):
+    x = torch.full((rows, vocab), rest).to(TYPES[dtype])
+    x[:, 7] = most
+    x[:, 900] = (most + rest) / 2
+    X = x.float().numpy()
+    u = np.random.default_rng(vocab).integers(0, 1 << 24, rows) / 2.0 ** 24
+    for k in (2, 40, 200):
+        check_draws(X, x.cuda(), u, None, top_k=k)
+        check_draws(X, x.cuda(), u, None, top_k=k, top_p=0.5, min_p=0.5)

@@ -477,7 +477,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
         }
     } else if (k || by_mass) {
         constexpr int kShift = sizeof(T) == 2 ? 16 : 0;          // bf16 logits differ in the upper half of the key only
-        const float step = 1.f / (kBinsPerZ * g.inv_t);          // width of a bin in logits
         // One round: a histogram of the whole row over the steps of z (coarse), or of one such bin's entries over the bits
         // of their keys below `hi`; joined; and the bin in which the sum reaches what is still wanted.  First top-k's
         // count is narrowed down to one key, then top-p's mass.
@@ -536,10 +535,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const __grid_const
             find_bin(s, need - (for_k ? (u64)count_above : mass_above), !for_k);
             if (coarse) {
                 bin = s.hit_bin; count_above = s.hit_count_above; mass_above = s.hit_mass_above;
-                // bounds of the bin's logits, a little wider than the roundings of z and of the bin number can move them
-                const float near = bin ? ((float)bin - 0.5f) * step * (1.f - 0x1p-19f) : 0.f, far = ((float)bin + 0.5f) * step * (1.f + 0x1p-19f);
-                floor_of = bin == kBins - 1 ? -INFINITY : __fsub_rd(g.top, far);
-                hi = min(top_key, key_of(__fsub_ru(g.top, near))) >> kShift;
+                // bounds of the bin's logits, a little wider than the roundings of z and of the bin number can move them; in 64
+                // bits, as the width of a bin in logits is no fp32 number for temperatures below 3e-37
+                const double step = 1. / ((double)kBinsPerZ * g.inv_t), near = bin ? (bin - 0.5) * step * (1. - 0x1p-19) : 0.,
+                             far = (bin + 0.5) * step * (1. + 0x1p-19);
+                floor_of = bin == kBins - 1 ? -INFINITY : __double2float_rd(__dsub_rd(g.top, far));
+                hi = min(top_key, key_of(__double2float_ru(__dsub_ru(g.top, near)))) >> kShift;
                 lo = key_of(floor_of) >> kShift;
                 coarse = false;
             } else {

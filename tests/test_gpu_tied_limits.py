@@ -79,3 +79,14 @@ def test_top_k_of_logits_whose_differences_are_next_to_nothing(rows, vocab, dtyp
     for k in (2, 40, 200):
         check_draws(X, x.cuda(), u, None, top_k=k)
         check_draws(X, x.cuda(), u, None, top_k=k, top_p=0.5, min_p=0.5)
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 3000), (100, 1500), (2, 33708)])
+@pytest.mark.parametrize("temperature", [2e-37, 1e-38, 4e-39])
+@pytest.mark.parametrize("settings", [dict(top_p=0.5), dict(top_p=0.95), dict(top_k=1200), dict(top_k=1200, top_p=0.8, min_p=0.01), dict(min_p=0.05)])
+def test_temperatures_whose_steps_are_next_to_nothing(rows, vocab, temperature, settings):
+    """Logits as close together as the temperature is small, so that their weights are ordinary ones."""
+    g = np.random.default_rng(vocab)
+    X = (-np.abs(g.standard_normal((rows, vocab))) * 4 * temperature).astype(np.float32)
+    assert len(np.unique(X)) > 1000
+    check_draws(X, torch.from_numpy(X).cuda(), g.integers(0, 1 << 24, rows) / 2.0 ** 24, temperature, **settings)

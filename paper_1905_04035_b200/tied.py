@@ -34,8 +34,8 @@ def _matrix(t: torch.Tensor, rows: int, cols: int, index: int, name: str):
     if t.get_device() != index:
         raise ValueError("all tensors must live on the same device")
     ld, step = t.stride()
-    if step != 1 or ld < cols:
-        if (step != 1 and cols > 1) or rows > 1:
+    if step != 1 and cols > 1 or ld < cols:                 # (the stride of a single column means nothing)
+        if rows > 1 or step != 1 and cols > 1:
             raise ValueError("%s must have contiguous rows that do not overlap" % name)
         ld = cols
     return t.data_ptr(), ld, kind

@@ -90,3 +90,22 @@ def test_temperatures_whose_steps_are_next_to_nothing(rows, vocab, temperature, 
     X = (-np.abs(g.standard_normal((rows, vocab))) * 4 * temperature).astype(np.float32)
     assert len(np.unique(X)) > 1000
     check_draws(X, torch.from_numpy(X).cuda(), g.integers(0, 1 << 24, rows) / 2.0 ** 24, temperature, **settings)
+
+
+def test_a_single_column_has_no_order_of_its_own():
+    """[n, 1] tensors whose rows are one element apart, whatever stride their single column reports."""
+    n = 300
+    x = torch.randn(1, n, device="cuda").t()
+    assert x.stride() == (1, n)
+    out = torch.empty(1, n, device="cuda").t()
+    dst.dst_dropout(x, out, 0.0, 1, scale=2.0)
+    assert torch.equal(out, x * 2)
+    q = dst.Fp8Matrix(n, 1)
+    dst.dst_quantize_fp8(x, q)
+    assert (q.dequantize() - x).abs().max() <= x.abs().max() / 16
+    idx = torch.arange(n - 1, -1, -1, device="cuda")
+    dst.dst_embed(idx, x, out)
+    assert torch.equal(out, x.flip(0))
+    tokens = torch.full((n,), -7, device="cuda")
+    dst.dst_sample(x, torch.full((n,), 0.5, device="cuda"), tokens)
+    assert (tokens == 0).all()

@@ -210,6 +210,8 @@ def _workspace(t: Optional[torch.Tensor], index: int):
     if t is None:
         return None, 0
     _here(t, index)
+    if not t.is_contiguous():                               # (of an expanded tensor there is less than its elements say)
+        raise ValueError("workspace must be contiguous")
     return t.data_ptr(), t.numel() * t.element_size()
 
 

@@ -20,3 +20,11 @@ def test_a_single_column_or_row_has_no_stride_of_its_own():
     for bad in (torch.zeros(8).expand(5, 8), torch.zeros(1).expand(5, 1), torch.zeros(8, 5).t(), torch.zeros(5, 16)[:, ::2], torch.zeros(8, 1).t()[:, ::2]):
         with pytest.raises(ValueError):
             tied._matrix(bad, *bad.shape, CPU, "x")
+
+
+def test_a_workspace_has_all_the_bytes_that_it_reports():
+    for bad in (torch.empty(1, dtype=torch.uint8).expand(1 << 20), torch.empty(64, 64)[:, ::2]):
+        with pytest.raises(ValueError):
+            tied._workspace(bad, CPU)
+    whole = torch.empty(64, 64)
+    assert tied._workspace(whole, CPU) == (whole.data_ptr(), 64 * 64 * 4) and tied._workspace(None, CPU) == (None, 0)

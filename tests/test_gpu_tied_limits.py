@@ -109,3 +109,35 @@ def test_a_single_column_has_no_order_of_its_own():
     tokens = torch.full((n,), -7, device="cuda")
     dst.dst_sample(x, torch.full((n,), 0.5, device="cuda"), tokens)
     assert (tokens == 0).all()
+
+
+# M, N, K whose tiles fill the GPU, so that the inner dimension is summed in one part: the tile of two CTAs, and the side of at
+# most 16, 32, 64 and 128 rows as a or as b
+@pytest.mark.parametrize("M,N,K", [(4736, 1024, 16384), (5, 19000, 16384), (30, 19000, 9000), (19000, 60, 9000), (19000, 100, 9000)])
+def test_an_fp32_result_does_not_pay_for_an_early_block_that_outweighs_the_rest(M, N, K):
+    """Every element is one product B in the first block, nothing up to column 768, and 2^-6 B spread over what follows.
+
+    The first six blocks sum to B exactly.  Stretches of six blocks after them may lose 2u of their own sum for every one of
+    their 768 additions (additions in tensor memory truncate, at worst), and joining a stretch rounds to nearest, u of the sum:
+        768 2u R + stretches u (B + R)             R the sum of the rest
+    that is 35 u B for K = 9000 and 45 u B for 16384.  Summed on in tensor memory, every 32 elements after the first block lose
+    half of 2u B on average, a truncation at B itself: 257 and 488 u B."""
+    g = torch.Generator(device="cuda").manual_seed(K)
+
+    def matrix(rows, small):
+        x = torch.rand(rows, K, device="cuda", generator=g).to(torch.bfloat16).add_(1).mul_(small)
+        x[:, 0], x[:, 1:768] = 448, 0
+        m = dst.Fp8Matrix(rows, K)
+        dst.dst_quantize_fp8(x, m)
+        return m
+
+    a, b = matrix(M, 0.09 * 15616 / (K - 768)), matrix(N, 1.0)
+    out = torch.full((M, N), float("nan"), device="cuda")
+    dst.dst_matmul_fp8(a, b, out, torch.empty(max(dst.dst_matmul_fp8_workspace_bytes(M, N, K), 256), dtype=torch.uint8, device="cuda"))
+    rows, cols = torch.arange(0, M, max(1, M // 40), device="cuda"), torch.arange(0, N, max(1, N // 40), device="cuda")
+    A, B = a.dequantize()[rows].double(), b.dequantize()[cols].double()
+    first, rest = A[:, :1] @ B[:, :1].T, A[:, 768:] @ B[:, 768:].T
+    stretches = -(-(K - 768) // 768)
+    bound = 768 * 2 * U * rest + stretches * U * (first + rest)
+    error = (out[rows][:, cols].double() - (first + rest)).abs()
+    assert (error <= bound).all(), (float((error / (U * first)).max()), float((bound / (U * first)).max()))

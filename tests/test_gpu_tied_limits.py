@@ -141,3 +141,13 @@ def test_an_fp32_result_does_not_pay_for_an_early_block_that_outweighs_the_rest(
     bound = 768 * 2 * U * rest + stretches * U * (first + rest)
     error = (out[rows][:, cols].double() - (first + rest)).abs()
     assert (error <= bound).all(), (float((error / (U * first)).max()), float((bound / (U * first)).max()))
+
+
+def test_weights_next_to_a_power_of_two():
+    """Rows [0, z] with z around every -k ln 2, where the weight is next to 2^(31 - k): the second entry is never lost.  Its
+    weight is at least 2^11, and a uniform number of 1 - 2^-24 takes the last 2^-24 of the sum, 2^8 at most."""
+    z = np.concatenate([np.float32(-k * np.log(2)) + np.arange(-300, 301, dtype=np.float32) * np.spacing(np.float32(k * np.log(2))) for k in range(1, 20)]).astype(np.float32)
+    x = torch.from_numpy(np.stack([np.zeros_like(z), z], -1)).cuda()
+    tokens, prob = draw_tokens(x, 1 - 2.0 ** -24)
+    e = np.exp(z.astype(np.float64))
+    assert (tokens == 1).all() and np.abs(prob / (e / (1 + e)) - 1).max() <= 2.0 ** -11

@@ -95,7 +95,10 @@ int dst_quantize_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
 /*
  * out[m, n] = sum over column blocks b of a.scale(m, b) * b.scale(n, b) * sum_{k in b} a.q[m, k] * b.q[n, k]
  * a [M, K], b [N, K], out [M, N] in out_type (fp32 or bf16, rounded once).  All sums are fp32 in an order fixed by the
- * shapes and out_type.  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes (may be 0), 256-byte aligned;
+ * shapes and out_type.  The tensor cores' own additions truncate; an fp32 result leaves them every six blocks of 128 and is
+ * added up to nearest from there, a bf16 result (whose own rounding is 2^-9) only at the end of the inner dimension, or of the
+ * parts that it is cut into where the tiles are few: before its rounding it may be off by the order of 2^-23 of the largest
+ * partial sum for every 32 elements (6.3e-5 where one block outweighs the 15,616 elements after it).  K = 0 gives zeros.  workspace: dst_matmul_fp8_workspace_bytes(M, N, K) bytes (may be 0), 256-byte aligned;
  * as much is enough for every smaller M, N and K too.  A device-side wait that gives up leaves NaN in the part of `out`
  * that was still to be written.
  */

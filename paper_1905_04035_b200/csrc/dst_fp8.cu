@@ -816,8 +816,11 @@ cudaError_t launch_matmul_fp8(const Fp8View& a, const Fp8View& b, void* out, lon
 
 // A few rows of x against a whole weight, quantised by every CTA for itself while the weight's first tiles are on their way:
 // where they fit next to the ring of stages, the inner dimension stays whole, and the blocks are few enough for the four
-// epilogue warps (against the two-kernel form, 1024 columns: 1 row 7.9 and 10.3 us, 4 rows 9.1 and 10.3, 6 rows 10.8 and 10.7,
-// 16 rows 15.0 and 11.0).
+// epilogue warps (against the two-kernel form, 33,708 x 1024: 1 row 7.9 and 10.3 us, 4 rows 9.1 and 10.3, 6 rows 10.8 and 10.7,
+// 16 rows 15.0 and 11.0).  The work before the first tile is the same whatever the vocabulary, and the limit holds for small
+// ones and for few columns too: at the most rows it takes, 6.2 and 6.3 us for 16 rows of 33,708 x 256, 5.2 and 6.0 of x 128, 15.6 and
+// 17.2 for 2 rows of x 2048; 4.7 and 5.9 for 16 rows of 1000 x 64, 5.9 and 6.6 for 8 of x 512, 7.3 and 8.1 for 4 of x 1024;
+// 4.4 and 5.4 for 16 of 200 x 128.
 bool linear_fp8_fused(long long M, long long N, long long K) {
     const MatmulPlan L = plan_matmul(M, N, K);
     return L.swap && L.nt == 16 && L.splits == 1 && L.blocks * L.nt * kBlockK <= TileShape<1, 16, true>::kResident && M * L.blocks <= 40;

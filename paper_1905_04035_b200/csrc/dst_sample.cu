@@ -13,9 +13,10 @@
 //
 // A row belongs to a cluster of 1, 2, 4 or 8 CTAs with a slice of it each, joined through distributed shared memory.
 //
-// Bound by: the list's short dependent phases (one row of 33,708 fp32 logits: 9.7 us; 512 rows of 65,536 in bf16: 40 us, of
-// which their 67 MB need 10); without top-k by the instructions and shared-memory additions an entry costs in every pass over
-// the row (512 x 65,536 bf16: top-p alone 193 us, min-p alone 52, no filter 78).
+// Bound by: the list's short dependent phases (one row of 33,708 fp32 logits: 9.2 us, of 327,680: 13; 512 rows of 65,536 in bf16:
+// 39 us, of which their 67 MB need 10); without top-k by the instructions and shared-memory additions an entry costs in every pass
+// over the row (512 x 65,536 bf16: top-p alone 182 to 195 us, as the logits fall, min-p alone 49 to 53, no filter 78; 64 x 327,680
+// bf16: top-p alone 149, no filter 63).
 #include <cooperative_groups.h>
 
 #include "dst_tied.cuh"

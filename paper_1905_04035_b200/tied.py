@@ -273,7 +273,10 @@ class TiedProjection:
 
     ``update(weight)`` quantises the weight (after every optimizer step), ``logits(x, out)`` is x W^T, and with
     ``training`` ``backward(dlogits, x, dx, dweight)`` gives both gradients; ``dweight`` is the dense partner that
-    ``dst_densify`` adds to the embedding's gradient."""
+    ``dst_densify`` adds to the embedding's gradient.
+
+    The calls of one object share its workspace and its quantised weight and gradients: they must be ordered among each other, by
+    going to one stream or by events between streams.  Calls that may overlap on the GPU take an object each."""
 
     def __init__(self, vocab: int, d: int, max_tokens: int, *, training: bool = True, device="cuda"):
         self.vocab, self.d, self.max_tokens, self.training = vocab, d, max_tokens, training

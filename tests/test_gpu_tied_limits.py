@@ -120,8 +120,8 @@ def test_an_fp32_result_does_not_pay_for_an_early_block_that_outweighs_the_rest(
     The first six blocks sum to B exactly.  Stretches of six blocks after them may lose 2u of their own sum for every one of
     their 768 additions (additions in tensor memory truncate, at worst), and joining a stretch rounds to nearest, u of the sum:
         768 2u R + stretches u (B + R)             R the sum of the rest
-    that is 35 u B for K = 9000 and 45 u B for 16384.  Summed on in tensor memory, every 32 elements after the first block lose
-    half of 2u B on average, a truncation at B itself: 257 and 488 u B."""
+    that is 35 u B for K = 9000 and 45 u B for 16384.  Summed on in tensor memory, every 32 elements after the first block are
+    truncated at B itself, which is off by 285 and 1065 u B."""
     g = torch.Generator(device="cuda").manual_seed(K)
 
     def matrix(rows, small):

@@ -108,7 +108,7 @@ def prepare(case, seed):
         s["dlogprob"] = torch.full((n,), -1.0 / n, device="cuda") if case["mode"] == "loss" else torch.randn(n, device="cuda", generator=g) / n
         s["dentropy"] = (0.01 / n) * (1 + torch.rand(n, device="cuda", generator=g)) * ~padding
         new = lambda *shape: torch.empty(*shape, device="cuda")  # noqa: E731
-        s["logprob"], s["lse"], s["entropy"] = new(n), new(n), new(n)
+        s["logprob"], s["stats"], s["entropy"] = new(n), new(n, 2), new(n)
         if case["top"]:
             s["top_tokens"], s["top_logprob"] = torch.empty(n, case["top"], device="cuda", dtype=torch.int64), new(n, case["top"])
         if case["mode"] != "score":
@@ -269,8 +269,8 @@ def run(s):
             if c["mode"] == "loss":
                 dst.dst_logprob_loss(x, t, s["dlogprob"], s["logprob"], s["dlogits"], scale=scale, entropy=s["entropy"])
             else:
-                dst.dst_logprob(x, t, s["logprob"], scale=scale, lse=s["lse"], entropy=s["entropy"])
-                dst.dst_logprob_backward(x, t, s["logprob"], s["lse"], s["dlogprob"], s["dlogits"], scale=scale, entropy=s["entropy"], dentropy=s["dentropy"])
+                dst.dst_logprob(x, t, s["logprob"], scale=scale, stats=s["stats"], entropy=s["entropy"])
+                dst.dst_logprob_backward(x, t, s["stats"], s["dlogprob"], s["dlogits"], scale=scale, entropy=s["entropy"], dentropy=s["dentropy"])
             return r | {"dlogits": s["dlogits"]}
         if op == "norm":
             added = {} if s["residual"] is None else {"residual": s["residual"], "sum_out": s["sum"]}

@@ -37,6 +37,20 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .step import (  # noqa: F401
+    DST_LOGPROB_MAX_TOP,
+    DST_RMSNORM_MAX_D,
+    TensorList,
+    dst_clip,
+    dst_grad_norm,
+    dst_grad_norm_workspace_bytes,
+    dst_logprob,
+    dst_logprob_backward,
+    dst_logprob_loss,
+    dst_rmsnorm,
+    dst_rmsnorm_backward,
+    dst_rmsnorm_backward_workspace_bytes,
+)
 from .tied import (  # noqa: F401
     DST_FP8_ROW,
     DST_FP8_SQUARE,

@@ -80,6 +80,10 @@ class _Fp8(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 RESULT_BYTES = ctypes.sizeof(_Result)
 DST_GRAD_DENSE, DST_GRAD_SLICES = 0, 1
 DST_ACC_STOCK, DST_ACC_PROPOSED, DST_ACC_SPARSE_AS_DENSE = 0, 1, 2
@@ -128,6 +132,21 @@ SYMBOLS = {
     "dst_linear_fp8_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "dst_linear_fp8": (ctypes.c_int, [_vp, _i64, _i32, _i64, ctypes.POINTER(_Fp8), _vp, _i64, _i32, _vp, _sz, _vp]),
     "dst_sample": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    # include/dst_step.h
+    "dst_logprob": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp,
+                                   _vp]),
+    "dst_logprob_loss": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                        _i32, _vp, _vp]),
+    "dst_logprob_backward": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _i64,
+                                            _i32, _vp]),
+    "dst_rmsnorm": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i64, _vp, _i64, _i32, _vp, ctypes.c_float, _vp, _i64, _i32,
+                                   ctypes.POINTER(_Fp8), _vp, _i64, _i64, _vp]),
+    "dst_rmsnorm_backward_workspace_bytes": (_sz, [_i64, _i64]),
+    "dst_rmsnorm_backward": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64,
+                                            _i64, _vp, _sz, _vp]),
+    "dst_grad_norm_workspace_bytes": (_sz, [ctypes.POINTER(_Tensor), _i64]),
+    "dst_grad_norm": (ctypes.c_int, [ctypes.POINTER(_Tensor), _i64, ctypes.c_double, _vp, _vp, _sz, _vp]),
+    "dst_clip": (ctypes.c_int, [ctypes.POINTER(_Tensor), ctypes.POINTER(_Tensor), _i64, _vp, _vp]),
 }
 
 

@@ -1,0 +1,504 @@
+// Log probabilities of given tokens, entropy and the most likely tokens of rows of logits, and the gradient through them.
+//
+// With m the largest logit of some part of a row, a part is described by three numbers: m, r = sum exp(z) - 1 (the largest
+// logit's own 1 apart, so that what the others add is not rounded against it) and t = sum exp(z) z, z = scale (x - m) <= 0.
+// Two parts join by multiplying the one with the smaller m by exp(scale (m - M)) and moving its z's by the same
+// difference; a thread's logits, the lanes of a warp, the warps of a CTA and the CTAs of a row join in that way, and each
+// is read once.  Then log p = z - log1p(r) and the entropy is log1p(r) - t / (1 + r): a sum of two terms of one sign.
+//
+// A row belongs to a cluster of 1, 2, 4 or 8 CTAs, joined through distributed shared memory.  Where a CTA's part fits into its
+// threads' registers (eight vectors of 16 bytes each) it stays there for the gradient and the alternatives.
+//
+// Alternatives: the n-th largest of the maxima of some hundred groups of logits is a bound that n logits reach at least and
+// few more than n do; those are collected and ranked by counting.  Where too many reach it (equal logits), n
+// rounds look for the next largest instead.
+#include <cooperative_groups.h>
+
+#include "dst_step.cuh"
+
+namespace dst {
+namespace cg = cooperative_groups;
+
+typedef unsigned long long u64;
+constexpr int kLpThreads = 512;              // of a CTA, at most
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpVecs = 8;                   // vectors a thread holds
+constexpr int kLpCtas = 8;                   // of a row, at most
+constexpr int kLpGroups = 160;               // whose maxima bound the alternatives, at most
+constexpr int kLpList = 512;                 // candidates that are ranked
+constexpr unsigned kKeyLowest = 0x007FFFFFu; // key of -infinity
+constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
+constexpr float kLeastZ = -1000.f;           // in place of z = -infinity (and of anything below): its exponential is zero, and zero times it too
+
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+__device__ __forceinline__ float warp_max(float x) { float y; asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x)); return y; }
+
+// order-preserving bits of a float; the two zeros have the same, NaN counts as -infinity
+__device__ __forceinline__ unsigned order_key(float x) {
+    x = x == x ? x + 0.f : -INFINITY;
+    const unsigned b = __float_as_uint(x);
+    return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float of_order_key(unsigned k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+
+template <typename T> struct Logits8;        // a vector of 16 bytes
+template <> struct Logits8<float> {
+    static constexpr int kN = 4;
+    uint4 v;
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
+    __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))); }
+    static __device__ __forceinline__ Logits8 nothing() { return Logits8{make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u)}; }
+};
+template <> struct Logits8<__nv_bfloat16> {
+    static constexpr int kN = 8;
+    uint4 v;
+    __device__ __forceinline__ float get(int i) const {
+        const unsigned w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+        return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    __device__ __forceinline__ float largest() const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ Logits8 nothing() { return Logits8{make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u)}; }
+};
+
+// A row in vectors that start at multiples of 16 bytes: vector v holds entries v kN - skew and on.  The first and the last may
+// lie partly outside the row and are read entry by entry.
+template <typename T> struct RowView {
+    static constexpr int kN = Logits8<T>::kN;
+    const T* row;
+    int skew, vocab;
+    __device__ __forceinline__ RowView(const T* r, int n) : row(r), skew((int)((reinterpret_cast<uintptr_t>(r) & 15u) / sizeof(T))), vocab(n) {}
+    __device__ __forceinline__ int first(int v) const { return v * kN - skew; }
+    __device__ __forceinline__ Logits8<T> load(int v) const {
+        const int at = first(v);
+        Logits8<T> x;
+        if (at >= 0 && at + kN <= vocab) { x.v = *reinterpret_cast<const uint4*>(row + at); return x; }
+        T e[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) e[i] = at + i >= 0 && at + i < vocab ? row[at + i] : from_float<T>(-INFINITY);
+        x.v = *reinterpret_cast<const uint4*>(e);
+        return x;
+    }
+};
+
+// eight or four results to entries `at` and on of a row of the output; ALIGNED: the vector's place is aligned to its size or 16
+template <typename OT, int N>
+__device__ __forceinline__ void store_vec(OT* row, int at, int vocab, const float (&g)[N], bool aligned) {
+    if (aligned && at >= 0 && at + N <= vocab) {
+        if (sizeof(OT) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) __stcs(reinterpret_cast<float4*>(row + at + i), make_float4(g[i], g[i + 1], g[i + 2], g[i + 3]));
+        } else if (N == 4) {
+            __stcs(reinterpret_cast<uint2*>(row + at), make_uint2(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3])));
+        } else {
+            __stcs(reinterpret_cast<uint4*>(row + at), make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[N - 4], g[N - 3]), pack_bf16(g[N - 2], g[N - 1])));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) if (at + i >= 0 && at + i < vocab) row[at + i] = from_float<OT>(g[i]);
+}
+template <typename OT, int N>
+__device__ __forceinline__ bool vec_aligned(const OT* row, int skew) {
+    constexpr unsigned kTo = N * sizeof(OT) < 16 ? N * sizeof(OT) : 16;
+    return ((reinterpret_cast<uintptr_t>(row) - (uintptr_t)skew * sizeof(OT)) & (kTo - 1)) == 0;
+}
+
+struct Part { float m, r, t; };              // t with z in units of log 2
+__device__ __forceinline__ Part no_part() { return Part{-INFINITY, -1.f, 0.f}; }
+
+// The parts of a warp's lanes as one; `owner` is the first lane with the largest logit, whose 1 stays apart.
+__device__ __forceinline__ Part join_lanes(Part p, float scale2, int& owner) {
+    const float top = warp_max(p.m);
+    owner = __ffs(__ballot_sync(0xFFFFFFFFu, p.m == top)) - 1;
+    float r = 0.f, t = 0.f;
+    if (p.m != -INFINITY) {
+        const float d = max_nan((p.m - top) * scale2, kLeastZ), f = exp2_fast(d), s = 1.f + p.r;
+        r = s * f; t = f * fmaf(d, s, p.t);
+        if (lane_id() == owner) { r = p.r; t = p.t; }
+        if (top == INFINITY) r = t = NAN;
+    } else if (lane_id() == owner) r = -1.f;     // (all are -infinity)
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) { r += __shfl_xor_sync(0xFFFFFFFFu, r, d); t += __shfl_xor_sync(0xFFFFFFFFu, t, d); }
+    return Part{top, r, t};
+}
+
+struct LpShared {
+    Part warp[kLpWarps], cta;                // `cta`: read by the other CTAs of the row
+    int owner[kLpWarps];
+    float correction;
+    unsigned group[kLpGroups];
+    unsigned bound, count;
+    u64 round[kLpWarps];
+    u64 list[kLpList];
+    u64 top[DST_LOGPROB_MAX_TOP];            // the CTA's alternatives: key, then the index' complement (a larger number comes first)
+};
+
+// The gradient by a row's logits: scale (dlogprob ([here the target] - p) - dentropy p (log p + H)).
+struct RowGrad {
+    float top, scale, scale2, log_total, entropy, dlogprob, dentropy;
+    float base, slope;                       // p's factor is base + slope z2, z2 = log2(p sum); 1 / sum is in both
+    bool zero;                               // nothing reaches the row, or it has no probabilities
+    long long target;
+    __device__ __forceinline__ RowGrad(const LogprobParams& p, long long row, long long given, float largest, float log_sum, float h)
+        : top(largest), scale(p.scale), scale2(p.scale2), log_total(log_sum), entropy(h), target(given) {
+        dlogprob = target >= 0 && p.dlogprob ? p.dlogprob[row] : 0.f;
+        dentropy = p.dentropy ? p.dentropy[row] : 0.f;
+        zero = (dlogprob == 0.f && dentropy == 0.f) || top == -INFINITY;
+        const float unit = -scale * exp2_fast(-log_total * kLog2e);
+        base = unit * (dentropy == 0.f ? dlogprob : fmaf(dentropy, entropy - log_total, dlogprob));
+        slope = unit * dentropy * kLn2;
+    }
+    // of a vector whose first entry is number `at`
+    template <typename T> __device__ __forceinline__ void of(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
+        constexpr int kN = Logits8<T>::kN;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            const float z2 = max_nan((v.get(j) - top) * scale2, kLeastZ);
+            g[j] = zero ? 0.f : exp2_fast(z2) * fmaf(slope, z2, base);
+        }
+        if (zero || target < at || target >= at + kN) return;
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+            if (at + j == target) {          // 1 - p without a difference
+                const float log_p = fmaf(v.get(j) - top, scale, -log_total), p = exp2_fast(max_nan(log_p * kLog2e, kLeastZ));
+                const float by_entropy = dentropy == 0.f ? 0.f : __fmul_rn(dentropy * p, max_nan(log_p, kLeastZ) + entropy);
+                g[j] = scale * fmaf(dlogprob, -expm1f(log_p), -by_entropy);   // (spelt out: two kernels give the same bits)
+            }
+    }
+};
+
+template <typename T, bool KEEP> struct RowPart {
+    static constexpr int kN = Logits8<T>::kN;
+    RowView<T> row;
+    int begin, end;                          // the CTA's vectors
+    Logits8<T> kept[kLpVecs];
+    __device__ __forceinline__ RowPart(const T* r, int vocab, int b, int e) : row(r, vocab), begin(b), end(e) {}
+    __device__ __forceinline__ void fetch(Logits8<T> (&x)[kLpVecs], int v0) const {
+#pragma unroll
+        for (int i = 0; i < kLpVecs; ++i) {
+            const int v = v0 + i * blockDim.x;
+            if (v < end) x[i] = row.load(v); else x[i] = Logits8<T>::nothing();
+        }
+    }
+    // f(eight vectors, the first one's number; the others are blockDim.x on); past the end they hold -infinity
+    template <typename F> __device__ __forceinline__ void tiles(F f) {
+        if constexpr (KEEP) f(kept, begin + (int)threadIdx.x);
+        else for (int v0 = begin + threadIdx.x; v0 < end; v0 += kLpVecs * blockDim.x) {
+            Logits8<T> x[kLpVecs];
+            fetch(x, v0);
+            f(x, v0);
+        }
+    }
+};
+
+template <typename T, bool KEEP>
+__device__ __forceinline__ Part thread_part(RowPart<T, KEEP>& mine, float scale2) {
+    constexpr int kN = Logits8<T>::kN;
+    Part p = no_part();
+    mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int) {
+        float top = p.m;
+#pragma unroll
+        for (int i = 0; i < kLpVecs; ++i) top = fmaxf(top, x[i].largest());
+        float s = 0.f, t = 0.f;
+        if (p.m != -INFINITY) {                              // what was summed before, seen from the larger maximum
+            const float d = max_nan((p.m - top) * scale2, kLeastZ), f = exp2_fast(d);
+            s = f * (1.f + p.r); t = f * fmaf(d, 1.f + p.r, p.t);
+        }
+        p.m = top;
+        const float from = top == -INFINITY ? 0.f : top;     // (nothing but -infinity: z is -infinity all the same; a NaN stays)
+        float s2[2] = {s, 0.f}, t2[2] = {t, 0.f};
+#pragma unroll
+        for (int i = 0; i < kLpVecs; ++i)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                const float z = max_nan((x[i].get(j) - from) * scale2, kLeastZ), e = exp2_fast(z);
+                s2[j & 1] += e;
+                t2[j & 1] = fmaf(e, z, t2[j & 1]);
+            }
+        p.r = (s2[0] + s2[1]) - 1.f;
+        p.t = t2[0] + t2[1];
+    });
+    return p;
+}
+
+// The sum of a thread's exponentials without the first of those that equal `top`.
+template <typename T, bool KEEP>
+__device__ __forceinline__ float others_of(RowPart<T, KEEP>& mine, float top, float scale2) {
+    constexpr int kN = Logits8<T>::kN;
+    float s = 0.f;
+    int ties = 0;
+    mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int) {
+#pragma unroll
+        for (int i = 0; i < kLpVecs; ++i)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                const float v = x[i].get(j);
+                if (v == top) ++ties; else s += exp2_fast(max_nan((v - top) * scale2, kLeastZ));
+            }
+    });
+    return s + (float)(ties - 1);
+}
+
+__device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, int n) {
+    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+        const u64 k = list[i];
+        int before = 0;
+        for (int j = 0; j < count; ++j) before += list[j] > k;
+        if (k != 0 && before < n) out[before] = k;           // (0: an empty place)
+    }
+}
+
+// The CTA's n largest logits into s.top (0: none left).
+template <typename T, bool KEEP>
+__device__ __forceinline__ void find_top(RowPart<T, KEEP>& mine, float thread_max, int n, LpShared& s) {
+    constexpr int kN = Logits8<T>::kN;
+    const int threads = blockDim.x;
+    const int per = threads > 320 ? 4 : threads > 160 ? 2 : 1, groups = threads / per;
+    unsigned key = order_key(thread_max), most = key;
+    for (int d = 1; d < per; d *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+    if (threadIdx.x % per == 0) s.group[threadIdx.x / per] = most;
+    if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
+    if (threadIdx.x == 0) { s.count = 0; s.bound = kKeyLowest; }
+    __syncthreads();
+    if ((int)threadIdx.x < groups) {
+        const unsigned k = s.group[threadIdx.x];
+        int before = 0;
+        for (int j = 0; j < groups; ++j) { const unsigned o = s.group[j]; before += o > k || (o == k && j < (int)threadIdx.x); }
+        if (before == n - 1) s.bound = k;
+    }
+    __syncthreads();
+    const unsigned bound = max(s.bound, kKeyLowest + 1);     // (-infinity is never listed)
+    if (key >= bound)
+        mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int v0) {
+#pragma unroll
+            for (int i = 0; i < kLpVecs; ++i) {
+                if (order_key(x[i].largest()) < bound) continue;
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    const unsigned k = order_key(x[i].get(j));
+                    if (k < bound) continue;
+                    const unsigned at = atomicAdd(&s.count, 1u);
+                    if (at < kLpList) s.list[at] = (u64)k << 32 | (unsigned)~(mine.row.first(v0 + i * threads) + j);
+                }
+            }
+        });
+    __syncthreads();
+    const int count = (int)s.count;
+    if (count <= kLpList) {
+        rank_into(s.list, count, s.top, n);
+        __syncthreads();
+        return;
+    }
+    u64 last = ~0ull;
+    for (int place = 0; place < n; ++place) {
+        u64 best = 0;
+        if (key >= bound)
+            mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int v0) {
+#pragma unroll
+                for (int i = 0; i < kLpVecs; ++i)
+#pragma unroll
+                    for (int j = 0; j < kN; ++j) {
+                        const unsigned k = order_key(x[i].get(j));
+                        const u64 full = (u64)k << 32 | (unsigned)~(mine.row.first(v0 + i * threads) + j);
+                        if (k >= bound && full < last && full > best) best = full;
+                    }
+            });
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) { const u64 o = __shfl_xor_sync(0xFFFFFFFFu, best, d); if (o > best) best = o; }
+        if (lane_id() == 0) s.round[warp_id()] = best;
+        __syncthreads();
+        for (int w = 0; w < threads / 32; ++w) if (s.round[w] > best) best = s.round[w];
+        if (threadIdx.x == 0) s.top[place] = best;
+        __syncthreads();
+        if (best == 0) break;
+        last = best;
+    }
+}
+
+__device__ __forceinline__ long long target_of(const LogprobParams& p, long long row) {
+    if (!p.targets) return -1;
+    return p.wide ? static_cast<const long long*>(p.targets)[row] : static_cast<const int*>(p.targets)[row];
+}
+
+template <typename T, typename OT, bool KEEP, bool GRAD>
+__global__ void __launch_bounds__(kLpThreads) k_logprob(const __grid_constant__ LogprobParams p) {
+    constexpr int kN = Logits8<T>::kN;
+    __shared__ LpShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const long long row = blockIdx.x / ctas;
+    pdl_trigger();
+    pdl_wait();
+    const T* const x = static_cast<const T*>(p.logits) + row * p.ld;
+    RowPart<T, KEEP> mine(x, p.vocab, rank * p.vectors, 0);
+    mine.end = min(mine.begin + p.vectors, (p.vocab + mine.row.skew + kN - 1) / kN);
+    if (KEEP) mine.fetch(mine.kept, mine.begin + threadIdx.x);
+
+    // (thread 0 of the first CTA alone uses the given token's logit; it is read before anything is written)
+    long long target = target_of(p, row);
+    if (target >= p.vocab) {
+        if (p.result && rank == 0 && threadIdx.x == 0) {
+            atomicAdd(reinterpret_cast<u64*>(&p.result->n_out_of_range), 1ull);
+            p.result->status = DST_ERR_INDEX_OUT_OF_RANGE;
+        }
+        target = -1;
+    }
+    const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x[target]) : 0.f;
+
+    const Part thread = thread_part(mine, p.scale2);
+    int owner, owner_warp;
+    // (a thread with nothing but NaN and -infinity has no largest logit, but its NaN counts)
+    Part all = join_lanes(thread.m == -INFINITY && thread.r != thread.r ? Part{0.f, thread.r, thread.r} : thread, p.scale2, owner);
+    if (lane_id() == 0) { s.warp[warp_id()] = all; s.owner[warp_id()] = owner; }
+    if (threadIdx.x == 0) s.correction = 0.f;
+    __syncthreads();
+    all = join_lanes(lane_id() < (int)blockDim.x / 32 ? s.warp[lane_id()] : no_part(), p.scale2, owner_warp);
+    if (all.r < 0.25f && all.m != -INFINITY) {               // nearly all on one token: what the thread that holds it rounded against 1, anew
+        if (warp_id() == owner_warp && lane_id() == s.owner[owner_warp]) s.correction = others_of(mine, all.m, p.scale2) - thread.r;
+        __syncthreads();
+        all.r += s.correction;
+    }
+    if (!GRAD && p.top_n > 0) find_top(mine, thread.m, p.top_n, s);
+    if (ctas > 1) {
+        if (threadIdx.x == 0) s.cta = all;
+        cluster.sync();
+        int first;
+        all = join_lanes(lane_id() < ctas ? *cluster.map_shared_rank(&s.cta, lane_id()) : no_part(), p.scale2, first);
+    }
+    if (all.m == INFINITY) all.r = all.t = NAN;
+    const float total = 1.f + all.r, log_total = log1pf(all.r), entropy = all.m == -INFINITY ? 0.f : log_total - all.t * kLn2 / total;
+    if (rank == 0 && threadIdx.x == 0) {
+        // (log1p(-1) is -infinity, for a row of nothing but that)
+        if (p.logprob) p.logprob[row] = target < 0 ? 0.f : all.m == -INFINITY ? -INFINITY : fmaf(given - all.m, p.scale, -log_total);
+        if (p.lse) p.lse[row] = all.m == -INFINITY ? -INFINITY : fmaf(all.m, p.scale, log_total);
+        if (p.entropy) p.entropy[row] = entropy;
+        if (p.stats) { p.stats[2 * row] = all.m; p.stats[2 * row + 1] = log_total; }
+    }
+    if (GRAD) {
+        const RowGrad grad(p, row, target, all.m, log_total, entropy);
+        OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
+        const bool aligned = vec_aligned<OT, kN>(d, mine.row.skew);
+        mine.tiles([&](const Logits8<T> (&v)[kLpVecs], int v0) {
+#pragma unroll
+            for (int i = 0; i < kLpVecs; ++i) {
+                if (v0 + i * (int)blockDim.x >= mine.end) break;
+                const int at = mine.row.first(v0 + i * blockDim.x);
+                float g[kN];
+                grad.of(v[i], at, g);
+                store_vec<OT, kN>(d, at, p.vocab, g, aligned);
+            }
+        });
+    } else if (p.top_n > 0 && rank == 0) {
+        const int n = p.top_n;
+        if (ctas > 1) {
+            for (int i = threadIdx.x; i < ctas * n; i += blockDim.x) s.list[i] = cluster.map_shared_rank(s.top, i / n)[i % n];
+            __syncthreads();
+            if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
+            __syncthreads();
+            rank_into(s.list, ctas * n, s.top, n);
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const u64 k = s.top[i];
+            if (p.top_tokens) {
+                const int token = k == 0 ? -1 : (int)~(unsigned)k;
+                if (p.wide) static_cast<long long*>(p.top_tokens)[row * n + i] = token;
+                else static_cast<int*>(p.top_tokens)[row * n + i] = token;
+            }
+            if (p.top_logprob) p.top_logprob[row * n + i] = k == 0 ? -INFINITY : fmaf(of_order_key((unsigned)(k >> 32)) - all.m, p.scale, -log_total);
+        }
+    }
+    if (ctas > 1) cluster.sync();                            // (what others read of this CTA stays until then)
+}
+
+// The gradient from what the forward call gave: the same arithmetic.
+template <typename T, typename OT>
+__global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant__ LogprobParams p) {
+    constexpr int kN = Logits8<T>::kN;
+    const int parts = ((p.vocab + 2 * kN - 2) / kN + p.vectors - 1) / p.vectors;
+    const long long row = blockIdx.x / parts;
+    const int part = (int)(blockIdx.x - row * parts);
+    pdl_trigger();
+    pdl_wait();
+    const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
+    const int begin = part * p.vectors + threadIdx.x, end = min((part + 1) * p.vectors, (p.vocab + x.skew + kN - 1) / kN);
+    Logits8<T> v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (begin + i * 256 < end) v[i] = x.load(begin + i * 256);
+    const long long target = target_of(p, row);
+    const RowGrad grad(p, row, target < p.vocab ? target : -1, p.saved_stats[2 * row], p.saved_stats[2 * row + 1], p.saved_entropy ? p.saved_entropy[row] : 0.f);
+    OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
+    const bool aligned = vec_aligned<OT, kN>(d, x.skew);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (begin + i * 256 >= end) break;
+        const int at = x.first(begin + i * 256);
+        float g[kN];
+        grad.of(v[i], at, g);
+        store_vec<OT, kN>(d, at, p.vocab, g, aligned);
+    }
+}
+
+// How a row is cut.  A CTA's part is what its threads can hold (eight vectors each, up to 320 threads so that others fit
+// beside it); where there are fewer CTAs than twice the SMs, rows are cut further and threads hold less, so that the loads of a
+// row are spread over the device.
+struct LogprobShape { int ctas, threads, vectors, keep; };
+static LogprobShape logprob_shape(long long rows, long long vocab, int per_vector, int sms) {
+    const long long all = (vocab + 2 * per_vector - 2) / per_vector;     // whatever the row's place within 16 bytes
+    LogprobShape L{1, 0, 0, 1};
+    auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
+    while (L.ctas < kLpCtas && per() > kLpVecs * 320) L.ctas *= 2;
+    while (L.ctas < kLpCtas && rows * L.ctas < 2 * sms && per() > 256) L.ctas *= 2;
+    const long long each = rows * L.ctas < 2 * sms ? 2 : kLpVecs;
+    long long t = (per() + each - 1) / each;
+    t = (t + 31) / 32 * 32;
+    L.threads = int(t < kLpThreads ? t : kLpThreads);
+    L.vectors = int(per());
+    L.keep = per() <= (long long)kLpVecs * L.threads;
+    return L;
+}
+
+template <typename T, typename OT, bool KEEP, bool GRAD>
+static cudaError_t logprob_run(const LogprobParams& p, const LogprobShape& L, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.rows * L.ctas)); cfg.blockDim = dim3(L.threads); cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = L.ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k_logprob<T, OT, KEEP, GRAD>, p);
+}
+template <typename T, typename OT, bool GRAD>
+static cudaError_t logprob_t(LogprobParams p, int sms, cudaStream_t stream) {
+    const LogprobShape L = logprob_shape(p.rows, p.vocab, Logits8<T>::kN, sms);
+    p.vectors = L.vectors;
+    return L.keep ? logprob_run<T, OT, true, GRAD>(p, L, stream) : logprob_run<T, OT, false, GRAD>(p, L, stream);
+}
+cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream_t stream) {
+    return type == DST_F32 ? logprob_t<float, float, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false>(p, sms, stream);
+}
+cudaError_t launch_logprob_loss(const LogprobParams& p, int type, int d_type, int sms, cudaStream_t stream) {
+    if (type == DST_F32) return d_type == DST_F32 ? logprob_t<float, float, true>(p, sms, stream) : logprob_t<float, __nv_bfloat16, true>(p, sms, stream);
+    return d_type == DST_F32 ? logprob_t<__nv_bfloat16, float, true>(p, sms, stream) : logprob_t<__nv_bfloat16, __nv_bfloat16, true>(p, sms, stream);
+}
+
+template <typename T, typename OT>
+static cudaError_t logprob_backward_t(LogprobParams p, cudaStream_t stream) {
+    constexpr int kN = Logits8<T>::kN;
+    p.vectors = 4 * 256;
+    const long long parts = ((p.vocab + 2 * kN - 2) / kN + p.vectors - 1) / p.vectors;
+    return launch_pdl(k_logprob_backward<T, OT>, dim3((unsigned)(p.rows * parts)), dim3(256), 0, stream, p);
+}
+cudaError_t launch_logprob_backward(const LogprobParams& p, int type, int d_type, cudaStream_t stream) {
+    if (type == DST_F32) return d_type == DST_F32 ? logprob_backward_t<float, float>(p, stream) : logprob_backward_t<float, __nv_bfloat16>(p, stream);
+    return d_type == DST_F32 ? logprob_backward_t<__nv_bfloat16, float>(p, stream) : logprob_backward_t<__nv_bfloat16, __nv_bfloat16>(p, stream);
+}
+
+}  // namespace dst

@@ -55,6 +55,7 @@ struct Fp8View {                            // dst_fp8_t
     long long rows, cols, ld, ld_scale;
     int square;
 };
+int fp8_view(const dst_fp8_t* m, Fp8View& v); // of a matrix whose description is valid (dst_tied_api.cu); a dst_status_t
 constexpr int kScaleTile = 512;             // bytes of scales for 128 rows by 4 column blocks
 struct QuantParams {
     const void* x;

@@ -39,7 +39,7 @@ static bool drop_params(const dst_dropout_t* d, int64_t rows, DropParams& p) {
 }
 
 // 0: fine; the view of a matrix in 8 bits whose buffers are there
-static int fp8_view(const dst_fp8_t* m, Fp8View& v) {
+int fp8_view(const dst_fp8_t* m, Fp8View& v) {
     if (!m || m->rows < 0 || m->cols < 0 || m->ld < m->cols) return DST_ERR_INVALID_ARG;
     if (m->block != DST_FP8_ROW && m->block != DST_FP8_SQUARE) return DST_ERR_INVALID_ARG;
     if (m->rows > kMaxCols || m->cols > kMaxCols) return DST_ERR_UNSUPPORTED;

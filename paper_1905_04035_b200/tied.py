@@ -300,7 +300,11 @@ class TiedProjection:
         if tokens > self.max_tokens:
             raise ValueError("at most %d tokens a call, got %d" % (self.max_tokens, tokens))
 
-    def logits(self, x: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
+    def logits(self, x, out: torch.Tensor, stream=None) -> torch.Tensor:
+        """out [tokens, vocab] = x W^T; x is a tensor [tokens, d] or already in 8 bits (an ``Fp8Matrix``, as ``dst_rmsnorm`` writes it)."""
+        if isinstance(x, Fp8Matrix):
+            self._check(x.rows)
+            return dst_matmul_fp8(x, self.weight, out, self.workspace, stream=stream)
         self._check(x.shape[0])
         return dst_linear_fp8(x, self.weight, out, self.workspace, stream=stream)
 

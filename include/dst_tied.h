@@ -6,6 +6,8 @@
  *   dst_quantize_fp8, dst_matmul_fp8,
  *   dst_linear_fp8                   the projection and its gradients in 8-bit floating point; the weight's gradient
  *                                    is the dense partner dst_densify takes
+ *   dst_quantize_fp4, dst_matmul_fp4,
+ *   dst_linear_fp4                   the projection in 4 bits, for answers and scoring
  *   dst_sample                       a token per row of logits
  *
  * Conventions are those of dst.h: device pointers, caller-owned buffers, nothing allocated or synchronised, all work
@@ -112,6 +114,41 @@ int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ld
  */
 size_t dst_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const dst_fp8_t* w, void* out, int64_t ldo,
+                   int32_t out_type, void* workspace, size_t workspace_bytes, dst_stream_t stream);
+
+/*
+ * A matrix [rows, cols] in 4-bit floating point (2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) with one scale, a power of two, for each block of 32 consecutive columns of a row (the last one smaller).
+ *   q      [rows, ld], 16-byte aligned, ld in BYTES, a multiple of 16, at least (cols + 1) / 2; column c is in byte c / 2,
+ *          the lower half for even ones.  An odd last column's other half, and the rest of its 4-byte word, are written as zeros
+ *   scale  as in dst_fp8_t with blocks of 32: the byte of row r and block b in tile (r / 128) * ld_scale + b / 4, so that
+ *          ld_scale is at least cols / 128, rounded up.  dst_quantize_fp4 writes whole groups of four blocks
+ */
+typedef struct {
+    void* q;
+    void* scale;
+    int64_t rows, cols, ld, ld_scale;
+} dst_fp4_t;
+
+/*
+ * Quantise x [rows, cols] (fp32 or bf16).  The scale of a block is the smallest power of two 2^e with max|x| <= 6 * 2^e
+ * (max|x| taken as at least 2^-100): nothing saturates, the scaling is exact, and the one rounding is the one to 4 bits, to
+ * nearest even.  A block that holds an infinity or a NaN gets the scale NaN.
+ */
+int dst_quantize_fp4(const void* x, int64_t ldx, int32_t x_type, int64_t rows, int64_t cols, const dst_fp4_t* q,
+                     dst_stream_t stream);
+
+/*
+ * out = a b^T and out = quantised(x) w^T as dst_matmul_fp8 and dst_linear_fp8 have them, their workspaces likewise.  Sums are
+ * fp32 in an order fixed by the shapes and out_type; an fp32 result leaves the tensor cores every 1024 columns.  The 8-bit
+ * and the 4-bit form of a matrix do not mix.  dst_linear_fp4 takes up to 20 blocks of 256 elements, of up to 2048
+ * columns, in one kernel.
+ */
+size_t dst_matmul_fp4_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int dst_matmul_fp4(const dst_fp4_t* a, const dst_fp4_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,
+                   size_t workspace_bytes, dst_stream_t stream);
+size_t dst_linear_fp4_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int dst_linear_fp4(const void* x, int64_t ldx, int32_t x_type, int64_t M, const dst_fp4_t* w, void* out, int64_t ldo,
                    int32_t out_type, void* workspace, size_t workspace_bytes, dst_stream_t stream);
 
 /*

@@ -54,14 +54,20 @@ from .step import (  # noqa: F401
 from .tied import (  # noqa: F401
     DST_FP8_ROW,
     DST_FP8_SQUARE,
+    Fp4Matrix,
     Fp8Matrix,
     TiedProjection,
     dst_dropout,
     dst_embed,
+    dst_linear_fp4,
+    dst_linear_fp4_workspace_bytes,
     dst_linear_fp8,
     dst_linear_fp8_workspace_bytes,
+    dst_matmul_fp4,
+    dst_matmul_fp4_workspace_bytes,
     dst_matmul_fp8,
     dst_matmul_fp8_workspace_bytes,
+    dst_quantize_fp4,
     dst_quantize_fp8,
     dst_sample,
 )

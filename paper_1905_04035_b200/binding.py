@@ -80,6 +80,11 @@ class _Fp8(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class _Fp4(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ld_scale", ctypes.c_int64)]
+
+
 class _Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
@@ -131,6 +136,11 @@ SYMBOLS = {
     "dst_matmul_fp8": (ctypes.c_int, [ctypes.POINTER(_Fp8), ctypes.POINTER(_Fp8), _vp, _i64, _i32, _vp, _sz, _vp]),
     "dst_linear_fp8_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "dst_linear_fp8": (ctypes.c_int, [_vp, _i64, _i32, _i64, ctypes.POINTER(_Fp8), _vp, _i64, _i32, _vp, _sz, _vp]),
+    "dst_quantize_fp4": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, ctypes.POINTER(_Fp4), _vp]),
+    "dst_matmul_fp4_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "dst_matmul_fp4": (ctypes.c_int, [ctypes.POINTER(_Fp4), ctypes.POINTER(_Fp4), _vp, _i64, _i32, _vp, _sz, _vp]),
+    "dst_linear_fp4_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "dst_linear_fp4": (ctypes.c_int, [_vp, _i64, _i32, _i64, ctypes.POINTER(_Fp4), _vp, _i64, _i32, _vp, _sz, _vp]),
     "dst_sample": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
     # include/dst_step.h
     "dst_logprob": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp,

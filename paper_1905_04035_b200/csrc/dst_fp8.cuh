@@ -32,4 +32,42 @@ __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d
     return lo | hi << 16;
 }
 
+// Four neighbouring elements as they are stored; the largest magnitudes of four rows' elements in each of the columns.
+template <typename T> struct Four;
+template <> struct Four<float> {
+    float4 v;
+    __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void set(int j, float x) { (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) = x; }
+    __device__ __forceinline__ float get(int j) const { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+    __device__ __forceinline__ unsigned abs(int j) const { return __float_as_uint(get(j)) & 0x7FFFFFFFu; }
+    __device__ __forceinline__ unsigned amax() const { return max(max(abs(0), abs(1)), max(abs(2), abs(3))); }
+    __device__ static __forceinline__ void column_amax(const Four (&w)[4], unsigned (&top)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = max(max(w[0].abs(i), w[1].abs(i)), max(w[2].abs(i), w[3].abs(i)));
+    }
+};
+template <> struct Four<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void clear() { v = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
+        unsigned& w = j < 2 ? v.x : v.y;
+        const unsigned b = __bfloat16_as_ushort(x);
+        w = j & 1 ? (w & 0xFFFFu) | b << 16 : (w & 0xFFFF0000u) | b;
+    }
+    __device__ __forceinline__ float get(int j) const {
+        const unsigned w = j < 2 ? v.x : v.y;
+        return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    __device__ __forceinline__ unsigned amax() const {
+        const unsigned m = __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu);
+        return max(m << 16, m & 0xFFFF0000u);
+    }
+    __device__ static __forceinline__ void column_amax(const Four (&w)[4], unsigned (&top)[4]) {
+        const unsigned k = 0x7FFF7FFFu;
+        const unsigned a = __vmaxu2(__vmaxu2(w[0].v.x & k, w[1].v.x & k), __vmaxu2(w[2].v.x & k, w[3].v.x & k));
+        const unsigned b = __vmaxu2(__vmaxu2(w[0].v.y & k, w[1].v.y & k), __vmaxu2(w[2].v.y & k, w[3].v.y & k));
+        top[0] = a << 16; top[1] = a & 0xFFFF0000u; top[2] = b << 16; top[3] = b & 0xFFFF0000u;
+    }
+};
+
 }  // namespace dst

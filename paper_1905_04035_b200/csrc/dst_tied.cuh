@@ -72,6 +72,17 @@ bool linear_fp8_fused(long long M, long long N, long long K);               // x
 cudaError_t launch_linear_fp8_fused(const void* x, long long ldx, int x_type, long long M, const Fp8View& w, void* out, long long ldo,
                                     int out_type, int sms, cudaStream_t stream);
 
+// ---- 4-bit floating point (dst_fp4.cu) --------------------------------------------
+// (an Fp8View with ld in bytes and `square` unused)
+cudaError_t launch_quantize_fp4(const QuantParams& p, int x_type, cudaStream_t stream);
+size_t matmul_fp4_workspace(long long M, long long N, long long K);
+size_t matmul_fp4_workspace_bound(long long M, long long N, long long K);
+cudaError_t launch_matmul_fp4(const Fp8View& a, const Fp8View& b, void* out, long long ldo, int out_type, void* workspace,
+                              int sms, cudaStream_t stream);
+bool linear_fp4_fused(long long M, long long N, long long K);
+cudaError_t launch_linear_fp4_fused(const void* x, long long ldx, int x_type, long long M, const Fp8View& w, void* out, long long ldo,
+                                    int out_type, int sms, cudaStream_t stream);
+
 // ---- sampling (dst_sample.cu) -----------------------------------------------------
 struct SampleParams {
     const void* logits;

@@ -54,34 +54,85 @@ static bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int
     return rows >= 0 && cols >= 0 && ld >= cols && !misaligned(p, type_size(type)) && (p || rows == 0 || cols == 0);
 }
 
-static int matmul_impl(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,
-                       size_t workspace_bytes, cudaStream_t stream) {
-    if (!dtype_ok(out_type)) return DST_ERR_UNSUPPORTED;
-    Fp8View va, vb;
-    int rc = fp8_view(a, va);
-    if (rc == DST_OK) rc = fp8_view(b, vb);
-    if (rc != DST_OK) return rc;
+static int fp4_view(const dst_fp4_t* m, Fp8View& v) {
+    if (!m || m->rows < 0 || m->cols < 0 || m->ld < (m->cols + 1) / 2) return DST_ERR_INVALID_ARG;
+    if (m->rows > kMaxCols || m->cols > kMaxCols) return DST_ERR_UNSUPPORTED;
+    if (m->ld % 16 != 0 || m->ld_scale < (m->cols + 127) / 128) return DST_ERR_INVALID_ARG;
+    if (m->rows > 0 && m->cols > 0 && (!m->q || !m->scale || misaligned(m->q, 16) || misaligned(m->scale, 16))) return DST_ERR_INVALID_ARG;
+    v = Fp8View{static_cast<uint8_t*>(m->q), static_cast<uint8_t*>(m->scale), (long long)m->rows, (long long)m->cols, (long long)m->ld,
+                (long long)m->ld_scale, 0};
+    return DST_OK;
+}
+
+// What the two kinds of matrix differ in, for the host.
+struct Eight {
+    static constexpr int64_t kScaleCols = 512;               // columns whose scales are one tile
+    static int64_t row_bytes(int64_t cols) { return (cols + 15) / 16 * 16; }
+    static size_t workspace(long long M, long long N, long long K) { return matmul_fp8_workspace(M, N, K); }
+    static size_t bound(long long M, long long N, long long K) { return matmul_fp8_workspace_bound(M, N, K); }
+    static constexpr auto matmul = launch_matmul_fp8;
+    static constexpr auto quantize = launch_quantize;
+    static constexpr auto fused = linear_fp8_fused;
+    static constexpr auto linear = launch_linear_fp8_fused;
+};
+struct Four {
+    static constexpr int64_t kScaleCols = 128;
+    static int64_t row_bytes(int64_t cols) { return (cols + 31) / 32 * 16; }
+    static size_t workspace(long long M, long long N, long long K) { return matmul_fp4_workspace(M, N, K); }
+    static size_t bound(long long M, long long N, long long K) { return matmul_fp4_workspace_bound(M, N, K); }
+    static constexpr auto matmul = launch_matmul_fp4;
+    static constexpr auto quantize = launch_quantize_fp4;
+    static constexpr auto fused = linear_fp4_fused;
+    static constexpr auto linear = launch_linear_fp4_fused;
+};
+
+template <typename KIND>
+static int matmul_impl(const Fp8View& va, const Fp8View& vb, void* out, int64_t ldo, int32_t out_type, void* workspace, size_t workspace_bytes,
+                       cudaStream_t stream) {
     if (va.cols != vb.cols || !matrix_ok(out, ldo, va.rows, vb.rows, out_type)) return DST_ERR_INVALID_ARG;
     if (va.rows == 0 || vb.rows == 0) return DST_OK;
     if (va.cols == 0)   // an empty sum
         return cudaMemset2DAsync(out, size_t(ldo) * type_size(out_type), 0, size_t(vb.rows) * type_size(out_type), size_t(va.rows), stream) == cudaSuccess
                    ? DST_OK : DST_ERR_CUDA;
-    const size_t need = matmul_fp8_workspace(va.rows, vb.rows, va.cols);
+    const size_t need = KIND::workspace(va.rows, vb.rows, va.cols);
     if (need > 0 && (!workspace || misaligned(workspace, 256))) return DST_ERR_INVALID_ARG;
     if (workspace_bytes < need) return DST_ERR_WORKSPACE_TOO_SMALL;
-    return done(launch_matmul_fp8(va, vb, out, ldo, out_type, workspace, device_sm_count(), stream), need > 0 ? 2 : 1);
+    return done(KIND::matmul(va, vb, out, ldo, out_type, workspace, device_sm_count(), stream), need > 0 ? 2 : 1);
 }
 
-// the quantised left operand of dst_linear_fp8 in its workspace: q, scales, then the product's own workspace
+// the quantised left operand of a linear call in its workspace: q, scales, then the product's own workspace
 struct LinearLayout { int64_t ld, ld_scale; size_t off_scale, off_matmul, total; };
-static LinearLayout linear_layout(int64_t M, int64_t N, int64_t K) {
+template <typename KIND> static LinearLayout linear_layout(int64_t M, int64_t N, int64_t K) {
     LinearLayout L{};
-    L.ld = (K + 15) / 16 * 16;
-    L.ld_scale = (K + 511) / 512;
+    L.ld = KIND::row_bytes(K);
+    L.ld_scale = (K + KIND::kScaleCols - 1) / KIND::kScaleCols;
     L.off_scale = align_up(size_t(M) * size_t(L.ld), 256);
     L.off_matmul = L.off_scale + size_t((M + 127) / 128) * size_t(L.ld_scale) * kScaleTile;
-    L.total = L.off_matmul + matmul_fp8_workspace_bound(M, N, K);
+    L.total = L.off_matmul + KIND::bound(M, N, K);
     return L;
+}
+
+template <typename KIND>
+static int linear_impl(const void* x, int64_t ldx, int32_t x_type, int64_t M, const Fp8View& w, void* out, int64_t ldo, int32_t out_type,
+                       void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    if (M > kMaxCols) return DST_ERR_UNSUPPORTED;
+    if (!matrix_ok(x, ldx, M, w.cols, x_type) || !matrix_ok(out, ldo, M, w.rows, out_type)) return DST_ERR_INVALID_ARG;
+    if (M == 0 || w.rows == 0) return DST_OK;
+    const LinearLayout L = linear_layout<KIND>(M, w.rows, w.cols);
+    Fp8View a{nullptr, nullptr, (long long)M, w.cols, (long long)L.ld, (long long)L.ld_scale, 0};
+    if (w.cols > 0) {
+        if (!workspace || misaligned(workspace, 256)) return DST_ERR_INVALID_ARG;
+        if (workspace_bytes < L.off_matmul + KIND::workspace(M, w.rows, w.cols)) return DST_ERR_WORKSPACE_TOO_SMALL;
+        if (KIND::fused(M, w.rows, w.cols))
+            return done(KIND::linear(x, ldx, x_type, M, w, out, ldo, out_type, device_sm_count(), stream), 1);
+        a.q = static_cast<uint8_t*>(workspace);
+        a.scale = static_cast<uint8_t*>(workspace) + L.off_scale;
+        const QuantParams p{x, (long long)ldx, (long long)M, w.cols, a, {}};
+        const int rc = done(KIND::quantize(p, x_type, stream), 1);
+        if (rc != DST_OK) return rc;
+    }
+    return matmul_impl<KIND>(a, w, out, ldo, out_type, workspace ? static_cast<char*>(workspace) + L.off_matmul : nullptr,
+                             w.cols > 0 ? workspace_bytes - L.off_matmul : 0, stream);
 }
 
 }  // namespace dst
@@ -154,12 +205,16 @@ size_t dst_matmul_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 
 int dst_matmul_fp8(const dst_fp8_t* a, const dst_fp8_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,
                    size_t workspace_bytes, dst_stream_t stream) {
-    return matmul_impl(a, b, out, ldo, out_type, workspace, workspace_bytes, stream);
+    if (!dtype_ok(out_type)) return DST_ERR_UNSUPPORTED;
+    Fp8View va, vb;
+    int rc = fp8_view(a, va);
+    if (rc == DST_OK) rc = fp8_view(b, vb);
+    return rc != DST_OK ? rc : matmul_impl<Eight>(va, vb, out, ldo, out_type, workspace, workspace_bytes, stream);
 }
 
 size_t dst_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || N <= 0 || K <= 0 || M > kMaxCols || N > kMaxCols || K > kMaxCols) return 0;
-    return linear_layout(M, N, K).total;
+    return linear_layout<Eight>(M, N, K).total;
 }
 
 int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const dst_fp8_t* w, void* out, int64_t ldo,
@@ -167,24 +222,45 @@ int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const 
     if (!dtype_ok(x_type) || !dtype_ok(out_type)) return DST_ERR_UNSUPPORTED;
     Fp8View v;
     const int rc = fp8_view(w, v);
+    return rc != DST_OK ? rc : linear_impl<Eight>(x, ldx, x_type, M, v, out, ldo, out_type, workspace, workspace_bytes, stream);
+}
+
+int dst_quantize_fp4(const void* x, int64_t ldx, int32_t x_type, int64_t rows, int64_t cols, const dst_fp4_t* q, dst_stream_t stream) {
+    if (!dtype_ok(x_type)) return DST_ERR_UNSUPPORTED;
+    if (!matrix_ok(x, ldx, rows, cols, x_type)) return DST_ERR_INVALID_ARG;
+    QuantParams p{x, (long long)ldx, (long long)rows, (long long)cols, {}, {}};
+    const int rc = fp4_view(q, p.q);
     if (rc != DST_OK) return rc;
-    if (M > kMaxCols) return DST_ERR_UNSUPPORTED;
-    if (!matrix_ok(x, ldx, M, w->cols, x_type) || !matrix_ok(out, ldo, M, w->rows, out_type)) return DST_ERR_INVALID_ARG;
-    if (M == 0 || w->rows == 0) return DST_OK;
-    const LinearLayout L = linear_layout(M, w->rows, w->cols);
-    dst_fp8_t a{nullptr, nullptr, M, w->cols, L.ld, L.ld_scale, DST_FP8_ROW, 0};
-    if (w->cols > 0) {
-        if (!workspace || misaligned(workspace, 256)) return DST_ERR_INVALID_ARG;
-        if (workspace_bytes < L.off_matmul + matmul_fp8_workspace(M, w->rows, w->cols)) return DST_ERR_WORKSPACE_TOO_SMALL;
-        if (linear_fp8_fused(M, w->rows, w->cols))
-            return done(launch_linear_fp8_fused(x, ldx, x_type, M, v, out, ldo, out_type, device_sm_count(), stream), 1);
-        a.q = workspace;
-        a.scale = static_cast<char*>(workspace) + L.off_scale;
-        const int rq = dst_quantize_fp8(x, ldx, x_type, M, w->cols, &a, nullptr, stream);
-        if (rq != DST_OK) return rq;
-    }
-    return matmul_impl(&a, w, out, ldo, out_type, workspace ? static_cast<char*>(workspace) + L.off_matmul : nullptr,
-                       w->cols > 0 ? workspace_bytes - L.off_matmul : 0, stream);
+    if (q->rows != rows || q->cols != cols) return DST_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return DST_OK;
+    return done(launch_quantize_fp4(p, x_type, stream), 1);
+}
+
+size_t dst_matmul_fp4_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0 || M > kMaxCols || N > kMaxCols || K > kMaxCols) return 0;
+    return matmul_fp4_workspace_bound(M, N, K);
+}
+
+int dst_matmul_fp4(const dst_fp4_t* a, const dst_fp4_t* b, void* out, int64_t ldo, int32_t out_type, void* workspace,
+                   size_t workspace_bytes, dst_stream_t stream) {
+    if (!dtype_ok(out_type)) return DST_ERR_UNSUPPORTED;
+    Fp8View va, vb;
+    int rc = fp4_view(a, va);
+    if (rc == DST_OK) rc = fp4_view(b, vb);
+    return rc != DST_OK ? rc : matmul_impl<Four>(va, vb, out, ldo, out_type, workspace, workspace_bytes, stream);
+}
+
+size_t dst_linear_fp4_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0 || M > kMaxCols || N > kMaxCols || K > kMaxCols) return 0;
+    return linear_layout<Four>(M, N, K).total;
+}
+
+int dst_linear_fp4(const void* x, int64_t ldx, int32_t x_type, int64_t M, const dst_fp4_t* w, void* out, int64_t ldo,
+                   int32_t out_type, void* workspace, size_t workspace_bytes, dst_stream_t stream) {
+    if (!dtype_ok(x_type) || !dtype_ok(out_type)) return DST_ERR_UNSUPPORTED;
+    Fp8View v;
+    const int rc = fp4_view(w, v);
+    return rc != DST_OK ? rc : linear_impl<Four>(x, ldx, x_type, M, v, out, ldo, out_type, workspace, workspace_bytes, stream);
 }
 
 int dst_sample(const void* logits, int64_t ld, int32_t type, int64_t rows, int64_t vocab, const float* uniform,

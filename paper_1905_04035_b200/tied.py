@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _Fp8, load_library
+from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _Fp4, _Fp8, load_library
 
 DST_FP8_ROW, DST_FP8_SQUARE = 0, 1
 _TYPES = {torch.float32: DST_F32, torch.bfloat16: DST_BF16}
@@ -183,6 +183,45 @@ class Fp8Matrix:
         return self.q[:, :self.cols].float() * self.scales().repeat_interleave(128, 1)[:, :self.cols]
 
 
+class Fp4Matrix:
+    """Owns a matrix [rows, cols] in 4-bit floating point (``dst_fp4_t``): ``q`` [rows, bytes padded to 16], two columns a byte, and a
+    scale (a power of two, as its exponent + 127) for each block of 32 columns of a row, in ``scale`` [rows / 128, blocks / 4, 512]."""
+
+    def __init__(self, rows: int, cols: int, *, device="cuda"):
+        if rows < 0 or cols < 0:
+            raise ValueError("rows and cols must not be negative")
+        self.rows, self.cols = rows, cols
+        self.q = torch.empty(rows, -(-cols // 32) * 16, dtype=torch.uint8, device=device)
+        self.scale = torch.empty(-(-rows // 128), -(-cols // 128), 512, dtype=torch.uint8, device=device)
+        self.device = self.q.device
+        self._c = _Fp4(self.q.data_ptr(), self.scale.data_ptr(), rows, cols, self.q.shape[1], self.scale.shape[1])
+
+    def part(self, rows: int, cols: int) -> "Fp4Matrix":
+        """The same buffers seen as a smaller matrix (leading dimensions stay)."""
+        if not (0 <= rows <= self.rows and 0 <= cols <= self.cols):
+            raise ValueError("a part is at most [%d, %d]" % (self.rows, self.cols))
+        m = object.__new__(Fp4Matrix)
+        m.rows, m.cols, m.q, m.scale, m.device = rows, cols, self.q[:rows], self.scale, self.device
+        m._c = _Fp4(self._c.q, self._c.scale, rows, cols, self._c.ld, self._c.ld_scale)
+        return m
+
+    def scales(self) -> torch.Tensor:
+        """The scale of every row and block, fp32 [rows, blocks]."""
+        tiles, groups = self.scale.shape[:2]
+        e = self.scale.view(tiles, groups, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(tiles * 128, groups * 4)
+        e = e[:self.rows, :-(-self.cols // 32)].int()
+        return torch.where(e == 255, torch.nan, torch.ldexp(torch.ones_like(e, dtype=torch.float32), e - 127))
+
+    def codes(self) -> torch.Tensor:
+        """The elements before scaling, fp32 [rows, cols]."""
+        value = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], device=self.device)
+        return value[torch.stack([self.q & 15, self.q >> 4], -1).reshape(self.rows, -1)[:, :self.cols].long()]
+
+    def dequantize(self) -> torch.Tensor:
+        """The fp32 matrix that the 4-bit one stands for."""
+        return self.codes() * self.scales().repeat_interleave(32, 1)[:, :self.cols]
+
+
 def dst_quantize_fp8(x: torch.Tensor, q: Optional[Fp8Matrix], qt: Optional[Fp8Matrix] = None, *, stream=None) -> None:
     """Enqueue ``dst_quantize_fp8``: x into ``q`` and its transpose into ``qt`` (either may be None)."""
     if q is None and qt is None:
@@ -242,6 +281,52 @@ def dst_linear_fp8(x: torch.Tensor, w: Fp8Matrix, out: torch.Tensor, workspace: 
     return out
 
 
+def dst_quantize_fp4(x: torch.Tensor, q: Fp4Matrix, *, stream=None) -> None:
+    """Enqueue ``dst_quantize_fp4``: x into ``q``."""
+    index = _device(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    px, ldx, tx = _matrix(x, rows, cols, index, "x")
+    _here(q.q, index)
+    _enqueue("dst_quantize_fp4", index, stream, px, ldx, tx, rows, cols, q._c)
+
+
+def dst_matmul_fp4_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load_library().dst_matmul_fp4_workspace_bytes(M, N, K))
+
+
+def dst_linear_fp4_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load_library().dst_linear_fp4_workspace_bytes(M, N, K))
+
+
+def dst_matmul_fp4(a: Fp4Matrix, b: Fp4Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
+                   stream=None) -> torch.Tensor:
+    """Enqueue ``dst_matmul_fp4``: out [a.rows, b.rows] = a b^T."""
+    index = _device(out)
+    _here(a.q, index)
+    _here(b.q, index)
+    po, ldo, to = _matrix(out, a.rows, b.rows, index, "out")
+    ws, ws_bytes = _workspace(workspace, index)
+    _enqueue("dst_matmul_fp4", index, stream, a._c, b._c, po, ldo, to, ws, ws_bytes)
+    return out
+
+
+def dst_linear_fp4(x: torch.Tensor, w: Fp4Matrix, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, *,
+                   stream=None) -> torch.Tensor:
+    """Enqueue ``dst_linear_fp4``: out [x.rows, w.rows] = quantised(x) w^T."""
+    index = _device(out)
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    m = x.shape[0]
+    px, ldx, tx = _matrix(x, m, w.cols, index, "x")
+    po, ldo, to = _matrix(out, m, w.rows, index, "out")
+    _here(w.q, index)
+    ws, ws_bytes = _workspace(workspace, index)
+    _enqueue("dst_linear_fp4", index, stream, px, ldx, tx, m, w._c, po, ldo, to, ws, ws_bytes)
+    return out
+
+
 def dst_sample(logits: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, *,
                temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
                top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
@@ -271,6 +356,9 @@ class TiedProjection:
     """The pre-softmax projection through the tied weight [vocab, d] in 8-bit floating point, for up to ``max_tokens``
     rows a call: owns the quantised weight and the workspaces, the arithmetic stays in the library.
 
+    With ``bits=4`` the weight and the rows are in 4 bits instead, half the bytes, for answers and scoring (``training=False``): there is
+    no gradient through it.
+
     ``update(weight)`` quantises the weight (after every optimizer step), ``logits(x, out)`` is x W^T, and with
     ``training`` ``backward(dlogits, x, dx, dweight)`` gives both gradients; ``dweight`` is the dense partner that
     ``dst_densify`` adds to the embedding's gradient.
@@ -278,11 +366,15 @@ class TiedProjection:
     The calls of one object share its workspace and its quantised weight and gradients: they must be ordered among each other, by
     going to one stream or by events between streams.  Calls that may overlap on the GPU take an object each."""
 
-    def __init__(self, vocab: int, d: int, max_tokens: int, *, training: bool = True, device="cuda"):
-        self.vocab, self.d, self.max_tokens, self.training = vocab, d, max_tokens, training
-        self.weight = Fp8Matrix(vocab, d, DST_FP8_SQUARE, device=device)
+    def __init__(self, vocab: int, d: int, max_tokens: int, *, training: bool = True, bits: int = 8, device="cuda"):
+        if bits not in (4, 8):
+            raise ValueError("bits must be 8 or 4")
+        if bits == 4 and training:
+            raise ValueError("a projection in 4 bits has no gradient: training=False")
+        self.vocab, self.d, self.max_tokens, self.training, self.bits = vocab, d, max_tokens, training, bits
+        self.weight = Fp4Matrix(vocab, d, device=device) if bits == 4 else Fp8Matrix(vocab, d, DST_FP8_SQUARE, device=device)
         self.device = self.weight.device
-        need = dst_linear_fp8_workspace_bytes(max_tokens, vocab, d)
+        need = (dst_linear_fp4_workspace_bytes if bits == 4 else dst_linear_fp8_workspace_bytes)(max_tokens, vocab, d)
         if training:
             # everything backward needs is there from the start: nothing is allocated, or freed, under a caller's stream
             self.weight_t = Fp8Matrix(d, vocab, DST_FP8_SQUARE, device=device)
@@ -294,6 +386,8 @@ class TiedProjection:
         self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
 
     def update(self, weight: torch.Tensor, stream=None) -> None:
+        if self.bits == 4:
+            return dst_quantize_fp4(weight, self.weight, stream=stream)
         dst_quantize_fp8(weight, self.weight, self.weight_t if self.training else None, stream=stream)
 
     def _check(self, tokens: int) -> None:
@@ -301,11 +395,16 @@ class TiedProjection:
             raise ValueError("at most %d tokens a call, got %d" % (self.max_tokens, tokens))
 
     def logits(self, x, out: torch.Tensor, stream=None) -> torch.Tensor:
-        """out [tokens, vocab] = x W^T; x is a tensor [tokens, d] or already in 8 bits (an ``Fp8Matrix``, as ``dst_rmsnorm`` writes it)."""
-        if isinstance(x, Fp8Matrix):
+        """out [tokens, vocab] = x W^T; x is a tensor [tokens, d] or already quantised: an ``Fp8Matrix``, as ``dst_rmsnorm`` writes it, or
+        with ``bits=4`` an ``Fp4Matrix``."""
+        if isinstance(x, (Fp8Matrix, Fp4Matrix)):
+            if isinstance(x, Fp4Matrix) != (self.bits == 4):
+                raise TypeError("x must be quantised as the weight is, to %d bits" % self.bits)
             self._check(x.rows)
-            return dst_matmul_fp8(x, self.weight, out, self.workspace, stream=stream)
+            return (dst_matmul_fp4 if self.bits == 4 else dst_matmul_fp8)(x, self.weight, out, self.workspace, stream=stream)
         self._check(x.shape[0])
+        if self.bits == 4:
+            return dst_linear_fp4(x, self.weight, out, self.workspace, stream=stream)
         return dst_linear_fp8(x, self.weight, out, self.workspace, stream=stream)
 
     def backward(self, dlogits: torch.Tensor, x: torch.Tensor, dx: torch.Tensor, dweight: torch.Tensor, stream=None) -> None:

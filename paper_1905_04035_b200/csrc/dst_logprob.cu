@@ -22,7 +22,7 @@ namespace cg = cooperative_groups;
 typedef unsigned long long u64;
 constexpr int kLpThreads = 512;              // of a CTA, at most
 constexpr int kLpWarps = kLpThreads / 32;
-constexpr int kLpVecs = 8;                   // vectors a thread holds
+constexpr int kLpVecs = 4;                   // vectors a thread takes at a time
 constexpr int kLpCtas = 8;                   // of a row, at most
 constexpr int kLpGroups = 160;               // whose maxima bound the alternatives, at most
 constexpr int kLpList = 512;                 // candidates that are ranked
@@ -179,19 +179,31 @@ template <typename T, bool KEEP> struct RowPart {
     Logits8<T> kept[kLpVecs];
     __device__ __forceinline__ RowPart(const T* r, int vocab, int b, int e) : row(r, vocab), begin(b), end(e) {}
     __device__ __forceinline__ void fetch(Logits8<T> (&x)[kLpVecs], int v0) const {
+        const int step = blockDim.x, last = v0 + (kLpVecs - 1) * step;
+        if (row.first(v0) >= 0 && last < end && row.first(last) + kN <= row.vocab) {
+            const T* const from = row.row + row.first(v0);
 #pragma unroll
-        for (int i = 0; i < kLpVecs; ++i) {
-            const int v = v0 + i * blockDim.x;
-            if (v < end) x[i] = row.load(v); else x[i] = Logits8<T>::nothing();
+            for (int i = 0; i < kLpVecs; ++i) x[i].v = *reinterpret_cast<const uint4*>(from + i * step * kN);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLpVecs; ++i) if (v0 + i * step < end) x[i] = row.load(v0 + i * step); else x[i] = Logits8<T>::nothing();
         }
     }
-    // f(eight vectors, the first one's number; the others are blockDim.x on); past the end they hold -infinity
+    // f(four vectors, the first one's number) for all of the thread's; the others are blockDim.x on, and past the end they hold
+    // -infinity.  The next four are on their way meanwhile.
     template <typename F> __device__ __forceinline__ void tiles(F f) {
         if constexpr (KEEP) f(kept, begin + (int)threadIdx.x);
-        else for (int v0 = begin + threadIdx.x; v0 < end; v0 += kLpVecs * blockDim.x) {
-            Logits8<T> x[kLpVecs];
+        else {
+            int v0 = begin + threadIdx.x;
+            Logits8<T> x[kLpVecs], next[kLpVecs];
             fetch(x, v0);
-            f(x, v0);
+#pragma unroll 1
+            for (; v0 < end; v0 += kLpVecs * blockDim.x) {
+                if (v0 + kLpVecs * (int)blockDim.x < end) fetch(next, v0 + kLpVecs * blockDim.x);
+                f(x, v0);
+#pragma unroll
+                for (int i = 0; i < kLpVecs; ++i) x[i] = next[i];
+            }
         }
     }
 };
@@ -444,20 +456,18 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant_
     }
 }
 
-// How a row is cut.  A CTA's part is what its threads can hold (eight vectors each, up to 320 threads so that others fit
-// beside it); where there are fewer CTAs than twice the SMs, rows are cut further and threads hold less, so that the loads of a
-// row are spread over the device.
+// How a row is cut.  Many rows: a CTA of 256 threads each, four on an SM, which read them four vectors a thread at a time.  Fewer rows than fill
+// the device so: several CTAs a row, and as many threads as hold their part at four vectors each.
 struct LogprobShape { int ctas, threads, vectors, keep; };
 static LogprobShape logprob_shape(long long rows, long long vocab, int per_vector, int sms) {
     const long long all = (vocab + 2 * per_vector - 2) / per_vector;     // whatever the row's place within 16 bytes
     LogprobShape L{1, 0, 0, 1};
     auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
-    while (L.ctas < kLpCtas && per() > kLpVecs * 320) L.ctas *= 2;
-    while (L.ctas < kLpCtas && rows * L.ctas < 2 * sms && per() > 256) L.ctas *= 2;
-    const long long each = rows * L.ctas < 2 * sms ? 2 : kLpVecs;
-    long long t = (per() + each - 1) / each;
+    while (L.ctas < kLpCtas && rows * L.ctas < 3 * sms && per() > 256) L.ctas *= 2;
+    const long long most = rows * L.ctas < 2 * sms ? kLpThreads : 256;
+    long long t = (per() + 1) / 2;                                       // two vectors a thread at least
     t = (t + 31) / 32 * 32;
-    L.threads = int(t < kLpThreads ? t : kLpThreads);
+    L.threads = int(t < most ? t : most);
     L.vectors = int(per());
     L.keep = per() <= (long long)kLpVecs * L.threads;
     return L;

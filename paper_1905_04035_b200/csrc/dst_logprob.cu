@@ -21,6 +21,7 @@ namespace cg = cooperative_groups;
 
 typedef unsigned long long u64;
 constexpr int kLpThreads = 512;              // of a CTA, at most
+constexpr int kLpStream = 256;               // ... where it streams its part
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpVecs = 4;                   // vectors a thread takes at a time
 constexpr int kLpCtas = 8;                   // of a row, at most
@@ -33,6 +34,14 @@ constexpr float kLeastZ = -1000.f;           // in place of z = -infinity (and o
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 __device__ __forceinline__ float warp_max(float x) { float y; asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x)); return y; }
+
+// two floats at a time
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float x, float y) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ void apart(Two a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a)); }
+__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Two mul2(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 
 // order-preserving bits of a float; the two zeros have the same, NaN counts as -infinity
 __device__ __forceinline__ unsigned order_key(float x) {
@@ -156,12 +165,28 @@ struct RowGrad {
     // of a vector whose first entry is number `at`
     template <typename T> __device__ __forceinline__ void of(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
         constexpr int kN = Logits8<T>::kN;
+        for (int j = 0; j < kN; ++j) g[j] = 0.f;
+        if (zero) return;
+        const Two minus = two(-top, -top), factor = two(scale2, scale2), b2 = two(base, base);
+        if (slope == 0.f) {                  // (no factor that could be infinite where the exponential is zero)
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            const float z2 = max_nan((v.get(j) - top) * scale2, kLeastZ);
-            g[j] = zero ? 0.f : exp2_fast(z2) * fmaf(slope, z2, base);
+            for (int j = 0; j < kN; j += 2) {
+                float z0, z1;
+                apart(mul2(add2(two(v.get(j), v.get(j + 1)), minus), factor), z0, z1);
+                apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), b2), g[j], g[j + 1]);
+            }
+        } else {
+            const Two s2 = two(slope, slope);
+#pragma unroll
+            for (int j = 0; j < kN; j += 2) {
+                float z0, z1;
+                apart(mul2(add2(two(v.get(j), v.get(j + 1)), minus), factor), z0, z1);
+                z0 = max_nan(z0, kLeastZ);
+                z1 = max_nan(z1, kLeastZ);
+                apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), fma2(s2, two(z0, z1), b2)), g[j], g[j + 1]);
+            }
         }
-        if (zero || target < at || target >= at + kN) return;
+        if (target < at || target >= at + kN) return;
 #pragma unroll
         for (int j = 0; j < kN; ++j)
             if (at + j == target) {          // 1 - p without a difference
@@ -176,7 +201,7 @@ template <typename T, bool KEEP> struct RowPart {
     static constexpr int kN = Logits8<T>::kN;
     RowView<T> row;
     int begin, end;                          // the CTA's vectors
-    Logits8<T> kept[kLpVecs];
+    Logits8<T> kept[KEEP ? kLpVecs : 1];
     __device__ __forceinline__ RowPart(const T* r, int vocab, int b, int e) : row(r, vocab), begin(b), end(e) {}
     __device__ __forceinline__ void fetch(Logits8<T> (&x)[kLpVecs], int v0) const {
         const int step = blockDim.x, last = v0 + (kLpVecs - 1) * step;
@@ -223,17 +248,25 @@ __device__ __forceinline__ Part thread_part(RowPart<T, KEEP>& mine, float scale2
         }
         p.m = top;
         const float from = top == -INFINITY ? 0.f : top;     // (nothing but -infinity: z is -infinity all the same; a NaN stays)
-        float s2[2] = {s, 0.f}, t2[2] = {t, 0.f};
+        const Two minus = two(-from, -from), factor = two(scale2, scale2);
+        Two s2 = two(s, 0.f), t2 = two(t, 0.f);
 #pragma unroll
         for (int i = 0; i < kLpVecs; ++i)
 #pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const float z = max_nan((x[i].get(j) - from) * scale2, kLeastZ), e = exp2_fast(z);
-                s2[j & 1] += e;
-                t2[j & 1] = fmaf(e, z, t2[j & 1]);
+            for (int j = 0; j < kN; j += 2) {
+                float z0, z1;
+                apart(mul2(add2(two(x[i].get(j), x[i].get(j + 1)), minus), factor), z0, z1);
+                z0 = max_nan(z0, kLeastZ);
+                z1 = max_nan(z1, kLeastZ);
+                const Two e = two(exp2_fast(z0), exp2_fast(z1));
+                s2 = add2(s2, e);
+                t2 = fma2(e, two(z0, z1), t2);
             }
-        p.r = (s2[0] + s2[1]) - 1.f;
-        p.t = t2[0] + t2[1];
+        float s1, t1;
+        apart(s2, s, s1);
+        apart(t2, t, t1);
+        p.r = (s + s1) - 1.f;
+        p.t = t + t1;
     });
     return p;
 }
@@ -338,7 +371,7 @@ __device__ __forceinline__ long long target_of(const LogprobParams& p, long long
 }
 
 template <typename T, typename OT, bool KEEP, bool GRAD>
-__global__ void __launch_bounds__(kLpThreads) k_logprob(const __grid_constant__ LogprobParams p) {
+__global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, KEEP ? 1 : 4) k_logprob(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
     __shared__ LpShared s;
     cg::cluster_group cluster = cg::this_cluster();
@@ -349,7 +382,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(const __grid_constant__ 
     const T* const x = static_cast<const T*>(p.logits) + row * p.ld;
     RowPart<T, KEEP> mine(x, p.vocab, rank * p.vectors, 0);
     mine.end = min(mine.begin + p.vectors, (p.vocab + mine.row.skew + kN - 1) / kN);
-    if (KEEP) mine.fetch(mine.kept, mine.begin + threadIdx.x);
+    if constexpr (KEEP) mine.fetch(mine.kept, mine.begin + threadIdx.x);
 
     // (thread 0 of the first CTA alone uses the given token's logit; it is read before anything is written)
     long long target = target_of(p, row);
@@ -464,7 +497,7 @@ static LogprobShape logprob_shape(long long rows, long long vocab, int per_vecto
     LogprobShape L{1, 0, 0, 1};
     auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
     while (L.ctas < kLpCtas && rows * L.ctas < 3 * sms && per() > 256) L.ctas *= 2;
-    const long long most = rows * L.ctas < 2 * sms ? kLpThreads : 256;
+    const long long most = rows * L.ctas < 2 * sms && per() <= kLpVecs * kLpThreads ? kLpThreads : kLpStream;
     long long t = (per() + 1) / 2;                                       // two vectors a thread at least
     t = (t + 31) / 32 * 32;
     L.threads = int(t < most ? t : most);

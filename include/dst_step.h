@@ -55,7 +55,7 @@ int dst_logprob(const void* logits, int64_t ld, int32_t type, int64_t rows, int6
  *
  * dst_logprob_loss is dst_logprob (without alternatives) and the gradient in one pass, for derivatives that are known
  * before (cross entropy: dlogprob = -1 / tokens).  dst_logprob_backward takes what dst_logprob gave: stats, and entropy with
- * dentropy.  Both give the same bits.
+ * dentropy.  (The calls may split a row's sums in other ways, which the number of rows decides too; they agree to rounding.)
  */
 int dst_logprob_loss(const void* logits, int64_t ld, int32_t type, int64_t rows, int64_t vocab, const void* targets,
                      int32_t index_type, float scale, const float* dlogprob, const float* dentropy, float* logprob,

@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(HERE, "libdst_b200.so")
 SOURCES = ["dst_api.cu", "dst_index_kernels.cu", "dst_front_cluster.cu", "dst_reduce_kernels.cu",
            "dst_accumulate_kernels.cu", "dst_dropout.cu", "dst_fp8.cu", "dst_fp4.cu", "dst_sample.cu", "dst_tied_api.cu",
            "dst_logprob.cu", "dst_norm.cu", "dst_clip.cu", "dst_step_api.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("dst_common.cuh", "dst_tied.cuh", "dst_fp8.cuh", "dst_fp4.cuh", "dst_block_matmul.cuh", "dst_step.cuh")] + [
+HEADERS = [os.path.join(CSRC, h) for h in ("dst_common.cuh", "dst_tied.cuh", "dst_async.cuh", "dst_fp8.cuh", "dst_fp4.cuh", "dst_block_matmul.cuh", "dst_step.cuh")] + [
     os.path.join(INCLUDE, h) for h in ("dst.h", "dst_tied.h", "dst_step.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", INCLUDE]

@@ -5,6 +5,7 @@
 
 #include <type_traits>
 
+#include "dst_async.cuh"
 #include "dst_fp4.cuh"
 #include "dst_fp8.cuh"
 
@@ -78,25 +79,9 @@ struct MatmulParams {
     int x_type, x_vec;                                    // rows aligned to four elements
 };
 
-__device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
 // (what is handed over here is tensor memory, ordered by the tcgen05 fences around it; a release at cluster scope would
 // wait for all of the thread's memory traffic)
 __device__ __forceinline__ void bar_arrive_cluster(unsigned bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
-    unsigned done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
-    if (bar_try(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (!bar_try(bar, parity))
-        if (clock64() - t0 > kWaitCycles) return false;
-    return true;
-}
 __device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {   // the same place in another CTA of the cluster
     unsigned r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));

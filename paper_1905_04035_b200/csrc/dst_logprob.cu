@@ -14,6 +14,7 @@
 // rounds look for the next largest instead.
 #include <cooperative_groups.h>
 
+#include "dst_async.cuh"
 #include "dst_step.cuh"
 
 namespace dst {
@@ -57,6 +58,12 @@ template <> struct Logits8<float> {
     uint4 v;
     __device__ __forceinline__ float get(int i) const { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
     __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))); }
+    static __device__ __forceinline__ float largest(const Logits8 (&x)[kLpVecs]) {
+        float m = x[0].largest();
+#pragma unroll
+        for (int i = 1; i < kLpVecs; ++i) m = fmaxf(m, x[i].largest());
+        return m;
+    }
     static __device__ __forceinline__ Logits8 nothing() { return Logits8{make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u)}; }
 };
 template <> struct Logits8<__nv_bfloat16> {
@@ -69,6 +76,14 @@ template <> struct Logits8<__nv_bfloat16> {
     __device__ __forceinline__ float largest() const {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
         const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ float largest(const Logits8 (&x)[kLpVecs]) {
+        __nv_bfloat162 m = reinterpret_cast<const __nv_bfloat162*>(&x[0].v)[0];
+#pragma unroll
+        for (int i = 0; i < kLpVecs; ++i)
+#pragma unroll
+            for (int j = i ? 0 : 1; j < 4; ++j) m = __hmax2(m, reinterpret_cast<const __nv_bfloat162*>(&x[i].v)[j]);
         return fmaxf(__low2float(m), __high2float(m));
     }
     static __device__ __forceinline__ Logits8 nothing() { return Logits8{make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u)}; }
@@ -138,8 +153,6 @@ __device__ __forceinline__ Part join_lanes(Part p, float scale2, int& owner) {
 
 struct LpShared {
     Part warp[kLpWarps], cta;                // `cta`: read by the other CTAs of the row
-    int owner[kLpWarps];
-    float correction;
     unsigned group[kLpGroups];
     unsigned bound, count;
     u64 round[kLpWarps];
@@ -197,7 +210,8 @@ struct RowGrad {
     }
 };
 
-template <typename T, bool KEEP> struct RowPart {
+// A CTA's part of a row.  KEEP: four vectors a thread, that stay in registers.
+template <typename T, bool KEEP, bool GRAD> struct RowPart {
     static constexpr int kN = Logits8<T>::kN;
     RowView<T> row;
     int begin, end;                          // the CTA's vectors
@@ -219,74 +233,86 @@ template <typename T, bool KEEP> struct RowPart {
     template <typename F> __device__ __forceinline__ void tiles(F f) {
         if constexpr (KEEP) f(kept, begin + (int)threadIdx.x);
         else {
-            int v0 = begin + threadIdx.x;
-            Logits8<T> x[kLpVecs], next[kLpVecs];
-            fetch(x, v0);
+            const int step = kLpVecs * blockDim.x;
+            Logits8<T> x[kLpVecs], y[kLpVecs];
+            fetch(x, begin + threadIdx.x);
+            if constexpr (GRAD) {                            // (one copy of f: two of them do not fit the registers)
 #pragma unroll 1
-            for (; v0 < end; v0 += kLpVecs * blockDim.x) {
-                if (v0 + kLpVecs * (int)blockDim.x < end) fetch(next, v0 + kLpVecs * blockDim.x);
-                f(x, v0);
+                for (int v0 = begin + threadIdx.x; v0 < end; v0 += step) {
+                    if (v0 + step < end) fetch(y, v0 + step);
+                    f(x, v0);
 #pragma unroll
-                for (int i = 0; i < kLpVecs; ++i) x[i] = next[i];
+                    for (int i = 0; i < kLpVecs; ++i) x[i] = y[i];
+                }
+            } else {
+#pragma unroll 1
+                for (int v0 = begin + threadIdx.x; v0 < end; v0 += 2 * step) {
+                    if (v0 + step < end) fetch(y, v0 + step);
+                    f(x, v0);
+                    if (v0 + step >= end) break;
+                    if (v0 + 2 * step < end) fetch(x, v0 + 2 * step);
+                    f(y, v0 + step);
+                }
             }
         }
     }
 };
 
-template <typename T, bool KEEP>
-__device__ __forceinline__ Part thread_part(RowPart<T, KEEP>& mine, float scale2) {
+// four more vectors of a thread's
+template <typename T>
+__device__ __forceinline__ void add_logits(Part& p, const Logits8<T> (&x)[kLpVecs], float scale2) {
     constexpr int kN = Logits8<T>::kN;
-    Part p = no_part();
-    mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int) {
-        float top = p.m;
-#pragma unroll
-        for (int i = 0; i < kLpVecs; ++i) top = fmaxf(top, x[i].largest());
-        float s = 0.f, t = 0.f;
-        if (p.m != -INFINITY) {                              // what was summed before, seen from the larger maximum
-            const float d = max_nan((p.m - top) * scale2, kLeastZ), f = exp2_fast(d);
-            s = f * (1.f + p.r); t = f * fmaf(d, 1.f + p.r, p.t);
-        }
+    const float top = fmaxf(p.m, Logits8<T>::largest(x));
+    float s = 1.f + p.r, t = p.t;
+    if (top != p.m) {                                    // what was summed before, seen from the larger maximum
+        const float d = max_nan((p.m - top) * scale2, kLeastZ), f = exp2_fast(d);
+        t = f * fmaf(d, s, t); s *= f;
         p.m = top;
-        const float from = top == -INFINITY ? 0.f : top;     // (nothing but -infinity: z is -infinity all the same; a NaN stays)
-        const Two minus = two(-from, -from), factor = two(scale2, scale2);
-        Two s2 = two(s, 0.f), t2 = two(t, 0.f);
+    }
+    const float from = top == -INFINITY ? 0.f : top;     // (nothing but -infinity: z is -infinity all the same; a NaN stays)
+    const Two minus = two(-from, -from), factor = two(scale2, scale2);
+    Two s2 = two(s, 0.f), t2 = two(t, 0.f);
 #pragma unroll
-        for (int i = 0; i < kLpVecs; ++i)
+    for (int i = 0; i < kLpVecs; ++i)
 #pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                float z0, z1;
-                apart(mul2(add2(two(x[i].get(j), x[i].get(j + 1)), minus), factor), z0, z1);
-                z0 = max_nan(z0, kLeastZ);
-                z1 = max_nan(z1, kLeastZ);
-                const Two e = two(exp2_fast(z0), exp2_fast(z1));
-                s2 = add2(s2, e);
-                t2 = fma2(e, two(z0, z1), t2);
-            }
-        float s1, t1;
-        apart(s2, s, s1);
-        apart(t2, t, t1);
-        p.r = (s + s1) - 1.f;
-        p.t = t + t1;
-    });
+        for (int j = 0; j < kN; j += 2) {
+            float z0, z1;
+            apart(mul2(add2(two(x[i].get(j), x[i].get(j + 1)), minus), factor), z0, z1);
+            z0 = max_nan(z0, kLeastZ);
+            z1 = max_nan(z1, kLeastZ);
+            const Two e = two(exp2_fast(z0), exp2_fast(z1));
+            s2 = add2(s2, e);
+            t2 = fma2(e, two(z0, z1), t2);
+        }
+    float s1, t1;
+    apart(s2, s, s1);
+    apart(t2, t, t1);
+    p.r = (s + s1) - 1.f;
+    p.t = t + t1;
+}
+template <typename T, bool KEEP, bool GRAD>
+__device__ __forceinline__ Part thread_part(RowPart<T, KEEP, GRAD>& mine, float scale2) {
+    Part p = no_part();
+    mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int) { add_logits<T>(p, x, scale2); });
     return p;
 }
 
-// The sum of a thread's exponentials without the first of those that equal `top`.
-template <typename T, bool KEEP>
-__device__ __forceinline__ float others_of(RowPart<T, KEEP>& mine, float top, float scale2) {
-    constexpr int kN = Logits8<T>::kN;
+// The sum of a thread's exponentials without the first of those that equal `top`, by its warp: vector(i) are the thread's n.
+template <typename T, typename F>
+__device__ __forceinline__ float others_of(int n, float top, float scale2, F vector) {
     float s = 0.f;
     int ties = 0;
-    mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int) {
+    for (int i = lane_id(); i < n; i += 32) {
+        const Logits8<T> x = vector(i);
 #pragma unroll
-        for (int i = 0; i < kLpVecs; ++i)
+        for (int j = 0; j < Logits8<T>::kN; ++j) {
+            const float v = x.get(j);
+            if (v == top) ++ties; else s += exp2_fast(max_nan((v - top) * scale2, kLeastZ));
+        }
+    }
 #pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const float v = x[i].get(j);
-                if (v == top) ++ties; else s += exp2_fast(max_nan((v - top) * scale2, kLeastZ));
-            }
-    });
-    return s + (float)(ties - 1);
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    return s + (float)((int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)ties) - 1);
 }
 
 __device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, int n) {
@@ -299,8 +325,8 @@ __device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, 
 }
 
 // The CTA's n largest logits into s.top (0: none left).
-template <typename T, bool KEEP>
-__device__ __forceinline__ void find_top(RowPart<T, KEEP>& mine, float thread_max, int n, LpShared& s) {
+template <typename T, bool KEEP, bool GRAD>
+__device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thread_max, int n, LpShared& s) {
     constexpr int kN = Logits8<T>::kN;
     const int threads = blockDim.x;
     const int per = threads > 320 ? 4 : threads > 160 ? 2 : 1, groups = threads / per;
@@ -370,44 +396,65 @@ __device__ __forceinline__ long long target_of(const LogprobParams& p, long long
     return p.wide ? static_cast<const long long*>(p.targets)[row] : static_cast<const int*>(p.targets)[row];
 }
 
+// the given token of a row, -1 for none; one that is out of range is counted by one thread
+__device__ __forceinline__ long long checked_target(const LogprobParams& p, long long row, bool counts) {
+    const long long target = target_of(p, row);
+    if (target < p.vocab) return target;
+    if (p.result && counts) {
+        atomicAdd(reinterpret_cast<u64*>(&p.result->n_out_of_range), 1ull);
+        p.result->status = DST_ERR_INDEX_OUT_OF_RANGE;
+    }
+    return -1;
+}
+
+// A whole row's numbers.
+struct RowSums {
+    float top, log_total, entropy;
+    __device__ __forceinline__ RowSums(Part all) : top(all.m) {
+        if (all.m == INFINITY) all.r = all.t = NAN;
+        log_total = log1pf(all.r);                            // (log1p(-1) is -infinity, for a row of nothing but that)
+        entropy = all.m == -INFINITY ? 0.f : log_total - all.t * kLn2 / (1.f + all.r);
+    }
+    __device__ __forceinline__ void write(const LogprobParams& p, long long row, long long target, float given) const {
+        const bool empty = top == -INFINITY;
+        if (p.logprob) p.logprob[row] = target < 0 ? 0.f : empty ? -INFINITY : fmaf(given - top, p.scale, -log_total);
+        if (p.lse) p.lse[row] = empty ? -INFINITY : fmaf(top, p.scale, log_total);
+        if (p.entropy) p.entropy[row] = entropy;
+        if (p.stats) { p.stats[2 * row] = top; p.stats[2 * row + 1] = log_total; }
+    }
+};
+
 template <typename T, typename OT, bool KEEP, bool GRAD>
 __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, KEEP ? 1 : 4) k_logprob(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
     __shared__ LpShared s;
     cg::cluster_group cluster = cg::this_cluster();
-    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const long long row = blockIdx.x / ctas;
+    const int ctas = 1 << p.cut, rank = blockIdx.x & (ctas - 1);
+    const long long row = blockIdx.x >> p.cut;
     pdl_trigger();
     pdl_wait();
     const T* const x = static_cast<const T*>(p.logits) + row * p.ld;
-    RowPart<T, KEEP> mine(x, p.vocab, rank * p.vectors, 0);
+    RowPart<T, KEEP, GRAD> mine(x, p.vocab, rank * p.vectors, 0);
     mine.end = min(mine.begin + p.vectors, (p.vocab + mine.row.skew + kN - 1) / kN);
     if constexpr (KEEP) mine.fetch(mine.kept, mine.begin + threadIdx.x);
 
     // (thread 0 of the first CTA alone uses the given token's logit; it is read before anything is written)
-    long long target = target_of(p, row);
-    if (target >= p.vocab) {
-        if (p.result && rank == 0 && threadIdx.x == 0) {
-            atomicAdd(reinterpret_cast<u64*>(&p.result->n_out_of_range), 1ull);
-            p.result->status = DST_ERR_INDEX_OUT_OF_RANGE;
-        }
-        target = -1;
-    }
+    const long long target = checked_target(p, row, rank == 0 && threadIdx.x == 0);
     const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x[target]) : 0.f;
 
     const Part thread = thread_part(mine, p.scale2);
-    int owner, owner_warp;
     // (a thread with nothing but NaN and -infinity has no largest logit, but its NaN counts)
+    int owner;
     Part all = join_lanes(thread.m == -INFINITY && thread.r != thread.r ? Part{0.f, thread.r, thread.r} : thread, p.scale2, owner);
-    if (lane_id() == 0) { s.warp[warp_id()] = all; s.owner[warp_id()] = owner; }
-    if (threadIdx.x == 0) s.correction = 0.f;
-    __syncthreads();
-    all = join_lanes(lane_id() < (int)blockDim.x / 32 ? s.warp[lane_id()] : no_part(), p.scale2, owner_warp);
     if (all.r < 0.25f && all.m != -INFINITY) {               // nearly all on one token: what the thread that holds it rounded against 1, anew
-        if (warp_id() == owner_warp && lane_id() == s.owner[owner_warp]) s.correction = others_of(mine, all.m, p.scale2) - thread.r;
-        __syncthreads();
-        all.r += s.correction;
+        const int first = mine.begin + warp_id() * 32 + owner, step = blockDim.x;
+        const float exact = others_of<T>((mine.end - first + step - 1) / step, all.m, p.scale2, [&](int i) { return mine.row.load(first + i * step); });
+        all.r += exact - __shfl_sync(0xFFFFFFFFu, thread.r, owner);
     }
+    if (lane_id() == 0) s.warp[warp_id()] = all;
+    __syncthreads();
+    if (GRAD || p.top_n > 0 || ctas > 1 || warp_id() == 0) all = join_lanes(lane_id() < (int)blockDim.x / 32 ? s.warp[lane_id()] : no_part(), p.scale2, owner);
+    else return;
     if (!GRAD && p.top_n > 0) find_top(mine, thread.m, p.top_n, s);
     if (ctas > 1) {
         if (threadIdx.x == 0) s.cta = all;
@@ -415,17 +462,10 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, KEEP ? 1 : 4) k
         int first;
         all = join_lanes(lane_id() < ctas ? *cluster.map_shared_rank(&s.cta, lane_id()) : no_part(), p.scale2, first);
     }
-    if (all.m == INFINITY) all.r = all.t = NAN;
-    const float total = 1.f + all.r, log_total = log1pf(all.r), entropy = all.m == -INFINITY ? 0.f : log_total - all.t * kLn2 / total;
-    if (rank == 0 && threadIdx.x == 0) {
-        // (log1p(-1) is -infinity, for a row of nothing but that)
-        if (p.logprob) p.logprob[row] = target < 0 ? 0.f : all.m == -INFINITY ? -INFINITY : fmaf(given - all.m, p.scale, -log_total);
-        if (p.lse) p.lse[row] = all.m == -INFINITY ? -INFINITY : fmaf(all.m, p.scale, log_total);
-        if (p.entropy) p.entropy[row] = entropy;
-        if (p.stats) { p.stats[2 * row] = all.m; p.stats[2 * row + 1] = log_total; }
-    }
+    const RowSums sums(all);
+    if (rank == 0 && threadIdx.x == 0) sums.write(p, row, target, given);
     if (GRAD) {
-        const RowGrad grad(p, row, target, all.m, log_total, entropy);
+        const RowGrad grad(p, row, target, all.m, sums.log_total, sums.entropy);
         OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
         const bool aligned = vec_aligned<OT, kN>(d, mine.row.skew);
         mine.tiles([&](const Logits8<T> (&v)[kLpVecs], int v0) {
@@ -455,7 +495,7 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, KEEP ? 1 : 4) k
                 if (p.wide) static_cast<long long*>(p.top_tokens)[row * n + i] = token;
                 else static_cast<int*>(p.top_tokens)[row * n + i] = token;
             }
-            if (p.top_logprob) p.top_logprob[row * n + i] = k == 0 ? -INFINITY : fmaf(of_order_key((unsigned)(k >> 32)) - all.m, p.scale, -log_total);
+            if (p.top_logprob) p.top_logprob[row * n + i] = k == 0 ? -INFINITY : fmaf(of_order_key((unsigned)(k >> 32)) - all.m, p.scale, -sums.log_total);
         }
     }
     if (ctas > 1) cluster.sync();                            // (what others read of this CTA stays until then)
@@ -486,6 +526,130 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant_
         float g[kN];
         grad.of(v[i], at, g);
         store_vec<OT, kN>(d, at, p.vocab, g, aligned);
+    }
+}
+
+// The loss and its gradient of many rows that fit into shared memory: a CTA takes every gridDim.x-th row.  One warp brings the rows in by
+// bulk copies, chunk after chunk into a ring; the others read a row twice there, for its sums and for the gradient, and give the
+// chunks back on the second time.  Every logit crosses from memory once, and what is free of the ring holds the next row's first
+// chunks while a row's sums are joined.  The pieces of a row before and after its whole vectors are read from memory.
+template <int N> struct RingShape {                         // N threads that work
+    static constexpr int kChunk = 2 * N;                    // vectors
+    static constexpr int kCtas = N <= 256 ? 2 : 1;          // on an SM
+    static constexpr int kSlots = (kCtas == 2 ? 113 : 225) * 1024 / (kChunk * 16) < 32 ? (kCtas == 2 ? 113 : 225) * 1024 / (kChunk * 16) : 32;
+    static constexpr int kSmem = kSlots * kChunk * 16;
+};
+template <typename T, typename OT, int N>
+__global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(const __grid_constant__ LogprobParams p) {
+    using S = RingShape<N>;
+    constexpr int kN = Logits8<T>::kN, kWarps = N / 32;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ Part parts[2][kWarps];
+    __shared__ __align__(8) unsigned long long bars[2 * S::kSlots];
+    const unsigned full = smem_addr(bars), empty = full + 8 * S::kSlots;
+    pdl_trigger();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kSlots; ++i) { bar_init(full + 8 * i, 1); bar_init(empty + 8 * i, kWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    pdl_wait();
+    bool ok = true;
+    if (warp_id() == kWarps) {                               // ---- copies ----
+        if (lane_id() == 0) {
+            int slot = 0;
+            unsigned phase = 1;                              // every slot is free at first
+            for (long long row = blockIdx.x; row < p.rows && ok; row += gridDim.x) {
+                const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
+                const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
+                for (int v = 0; v < end; v += S::kChunk) {
+                    ok = bar_wait(empty + 8 * slot, phase);
+                    if (!ok) break;
+                    const int from = max(v, whole0), to = min(v + S::kChunk, whole1);
+                    if (from < to) {
+                        bar_expect(full + 8 * slot, (to - from) * 16);
+                        copy_bytes(smem_addr(ring) + (slot * S::kChunk + from - v) * 16, x.row + x.first(from), (to - from) * 16, full + 8 * slot);
+                    } else bar_arrive(full + 8 * slot);
+                    if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
+                }
+            }
+        }
+    } else {
+        int slot = 0, turn = 0;
+        unsigned phase = 0;
+        for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+            const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
+            const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
+            // the thread's vectors of the chunk at v in the slot k; a chunk that never came is NaN
+            auto take = [&](Logits8<T>& to, int v, int at, int k) {
+                if (!ok) to.v = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
+                else if (at >= whole0 && at < whole1) to.v = *reinterpret_cast<const uint4*>(ring + (k * S::kChunk + at - v) * 16);
+                else if (at < end) to = x.load(at);
+                else to = Logits8<T>::nothing();
+            };
+            const long long target = checked_target(p, row, threadIdx.x == 0);
+            const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x.row[target]) : 0.f;
+            Part mine = no_part();
+            const int slot0 = slot;
+            for (int v = 0; v < end; v += 2 * S::kChunk) {
+                Logits8<T> y[kLpVecs];
+                static_assert(kLpVecs == 4, "two chunks of two vectors");
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = v + h * S::kChunk;
+                    if (c < end) {
+                        if (ok) ok = bar_wait(full + 8 * slot, phase);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                    }
+                    take(y[2 * h], c, c + threadIdx.x, slot);
+                    take(y[2 * h + 1], c, c + N + threadIdx.x, slot);
+                    if (c < end && ++slot == S::kSlots) { slot = 0; phase ^= 1; }
+                }
+                add_logits<T>(mine, y, p.scale2);
+            }
+            int owner;
+            Part all = join_lanes(mine.m == -INFINITY && mine.r != mine.r ? Part{0.f, mine.r, mine.r} : mine, p.scale2, owner);
+            if (all.r < 0.25f && all.m != -INFINITY) {       // (as in k_logprob)
+                const float exact = others_of<T>((end + N - 1) / N, all.m, p.scale2, [&](int i) {
+                    const int v = i / 2 * S::kChunk;
+                    Logits8<T> y;
+                    take(y, v, i * N + warp_id() * 32 + owner, (slot0 + i / 2) % S::kSlots);
+                    return y;
+                });
+                all.r += exact - __shfl_sync(0xFFFFFFFFu, mine.r, owner);
+            }
+            if (lane_id() == 0) parts[turn][warp_id()] = all;
+            asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+            all = join_lanes(lane_id() < kWarps ? parts[turn][lane_id()] : no_part(), p.scale2, owner);
+            const RowSums sums(all);
+            if (threadIdx.x == 0) sums.write(p, row, target, given);
+            const RowGrad grad(p, row, target, all.m, sums.log_total, sums.entropy);
+            OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
+            const bool aligned = vec_aligned<OT, kN>(d, x.skew);
+            int k = slot0;
+            for (int v = 0; v < end; v += S::kChunk) {
+                Logits8<T> y[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) take(y[h], v, v + h * N + threadIdx.x, k);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int at = v + h * N + threadIdx.x;
+                    if (at >= end) continue;
+                    float g[kN];
+                    grad.of(y[h], x.first(at), g);
+                    store_vec<OT, kN>(d, x.first(at), p.vocab, g, aligned);
+                }
+                // The chunk goes back once every lane has worked with what it read: a read that was only issued may still be on its
+                // way when the next copy lands.
+                __syncwarp();
+                if (lane_id() == 0) bar_arrive(empty + 8 * k);
+                if (++k == S::kSlots) k = 0;
+            }
+        }
+    }
+    if (!ok) {                                               // let copies in flight land
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1LL << 24)) {}
     }
 }
 
@@ -522,14 +686,37 @@ template <typename T, typename OT, bool GRAD>
 static cudaError_t logprob_t(LogprobParams p, int sms, cudaStream_t stream) {
     const LogprobShape L = logprob_shape(p.rows, p.vocab, Logits8<T>::kN, sms);
     p.vectors = L.vectors;
+    p.cut = L.ctas == 1 ? 0 : L.ctas == 2 ? 1 : L.ctas == 4 ? 2 : 3;
     return L.keep ? logprob_run<T, OT, true, GRAD>(p, L, stream) : logprob_run<T, OT, false, GRAD>(p, L, stream);
 }
 cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream_t stream) {
     return type == DST_F32 ? logprob_t<float, float, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false>(p, sms, stream);
 }
+
+// The ring takes rows that leave it room for two more chunks, enough of them for every CTA, and long enough for its threads.
+template <int N> static bool ring_fits(const LogprobParams& p, int per_vector, int sms) {
+    using S = RingShape<N>;
+    const long long vectors = (p.vocab + 2 * per_vector - 2) / per_vector, chunks = (vectors + S::kChunk - 1) / S::kChunk;
+    return chunks + 2 <= S::kSlots && vectors > 1024 && p.rows >= (long long)sms * S::kCtas;
+}
+template <typename T, typename OT, int N>
+static cudaError_t ring_run(const LogprobParams& p, int sms, cudaStream_t stream) {
+    using S = RingShape<N>;
+    static SmemOptIn opt;
+    const cudaError_t e = ensure_dynamic_smem(k_logprob_ring<T, OT, N>, S::kSmem, opt);
+    if (e != cudaSuccess) return e;
+    const long long ctas = (long long)sms * S::kCtas;
+    return launch_pdl(k_logprob_ring<T, OT, N>, dim3((unsigned)(p.rows < ctas ? p.rows : ctas)), dim3(N + 32), S::kSmem, stream, p);
+}
+template <typename T, typename OT>
+static cudaError_t loss_t(const LogprobParams& p, int sms, cudaStream_t stream) {
+    if (ring_fits<256>(p, Logits8<T>::kN, sms)) return ring_run<T, OT, 256>(p, sms, stream);
+    if (ring_fits<512>(p, Logits8<T>::kN, sms)) return ring_run<T, OT, 512>(p, sms, stream);
+    return logprob_t<T, OT, true>(p, sms, stream);
+}
 cudaError_t launch_logprob_loss(const LogprobParams& p, int type, int d_type, int sms, cudaStream_t stream) {
-    if (type == DST_F32) return d_type == DST_F32 ? logprob_t<float, float, true>(p, sms, stream) : logprob_t<float, __nv_bfloat16, true>(p, sms, stream);
-    return d_type == DST_F32 ? logprob_t<__nv_bfloat16, float, true>(p, sms, stream) : logprob_t<__nv_bfloat16, __nv_bfloat16, true>(p, sms, stream);
+    if (type == DST_F32) return d_type == DST_F32 ? loss_t<float, float>(p, sms, stream) : loss_t<float, __nv_bfloat16>(p, sms, stream);
+    return d_type == DST_F32 ? loss_t<__nv_bfloat16, float>(p, sms, stream) : loss_t<__nv_bfloat16, __nv_bfloat16>(p, sms, stream);
 }
 
 template <typename T, typename OT>

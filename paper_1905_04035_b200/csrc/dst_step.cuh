@@ -27,6 +27,7 @@ struct LogprobParams {
     int top_n;
     float scale, scale2;                    // scale2 = scale * log2(e)
     int vectors;                            // of 16 bytes that a CTA of the row's cluster takes
+    int cut;                                // a row has 2^cut CTAs
 };
 cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream_t stream);
 cudaError_t launch_logprob_loss(const LogprobParams& p, int type, int d_type, int sms, cudaStream_t stream);

@@ -14,6 +14,8 @@
 // rounds look for the next largest instead.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "dst_async.cuh"
 #include "dst_step.cuh"
 
@@ -109,18 +111,22 @@ template <typename T> struct RowView {
     }
 };
 
+template <typename OT, int N>
+__device__ __forceinline__ void store_whole(OT* to, const float (&g)[N]) {
+    if (sizeof(OT) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) __stcs(reinterpret_cast<float4*>(to + i), make_float4(g[i], g[i + 1], g[i + 2], g[i + 3]));
+    } else if (N == 4) {
+        __stcs(reinterpret_cast<uint2*>(to), make_uint2(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3])));
+    } else {
+        __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[N - 4], g[N - 3]), pack_bf16(g[N - 2], g[N - 1])));
+    }
+}
 // eight or four results to entries `at` and on of a row of the output; ALIGNED: the vector's place is aligned to its size or 16
 template <typename OT, int N>
 __device__ __forceinline__ void store_vec(OT* row, int at, int vocab, const float (&g)[N], bool aligned) {
     if (aligned && at >= 0 && at + N <= vocab) {
-        if (sizeof(OT) == 4) {
-#pragma unroll
-            for (int i = 0; i < N; i += 4) __stcs(reinterpret_cast<float4*>(row + at + i), make_float4(g[i], g[i + 1], g[i + 2], g[i + 3]));
-        } else if (N == 4) {
-            __stcs(reinterpret_cast<uint2*>(row + at), make_uint2(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3])));
-        } else {
-            __stcs(reinterpret_cast<uint4*>(row + at), make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[N - 4], g[N - 3]), pack_bf16(g[N - 2], g[N - 1])));
-        }
+        store_whole<OT, N>(row + at, g);
         return;
     }
 #pragma unroll
@@ -175,38 +181,37 @@ struct RowGrad {
         base = unit * (dentropy == 0.f ? dlogprob : fmaf(dentropy, entropy - log_total, dlogprob));
         slope = unit * dentropy * kLn2;
     }
-    // of a vector whose first entry is number `at`
-    template <typename T> __device__ __forceinline__ void of(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
-        constexpr int kN = Logits8<T>::kN;
-        for (int j = 0; j < kN; ++j) g[j] = 0.f;
-        if (zero) return;
-        const Two minus = two(-top, -top), factor = two(scale2, scale2), b2 = two(base, base);
-        if (slope == 0.f) {                  // (no factor that could be infinite where the exponential is zero)
+    // of a vector without the target; SLOPE: the entropy counts, and its factor grows where the exponential goes to zero
+    template <typename T, bool SLOPE> __device__ __forceinline__ void plain(const Logits8<T>& v, float (&g)[Logits8<T>::kN]) const {
+        const Two minus = two(-top, -top), factor = two(scale2, scale2), b2 = two(base, base), s2 = two(slope, slope);
 #pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                float z0, z1;
-                apart(mul2(add2(two(v.get(j), v.get(j + 1)), minus), factor), z0, z1);
-                apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), b2), g[j], g[j + 1]);
-            }
-        } else {
-            const Two s2 = two(slope, slope);
-#pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                float z0, z1;
-                apart(mul2(add2(two(v.get(j), v.get(j + 1)), minus), factor), z0, z1);
+        for (int j = 0; j < Logits8<T>::kN; j += 2) {
+            float z0, z1;
+            apart(mul2(add2(two(v.get(j), v.get(j + 1)), minus), factor), z0, z1);
+            if (SLOPE) {
                 z0 = max_nan(z0, kLeastZ);
                 z1 = max_nan(z1, kLeastZ);
                 apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), fma2(s2, two(z0, z1), b2)), g[j], g[j + 1]);
-            }
+            } else apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), b2), g[j], g[j + 1]);
         }
-        if (target < at || target >= at + kN) return;
+    }
+    // the target's place, where the vector at entry `at` has it
+    template <typename T> __device__ __forceinline__ void given(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
+        if (target < at || target >= at + Logits8<T>::kN) return;
 #pragma unroll
-        for (int j = 0; j < kN; ++j)
+        for (int j = 0; j < Logits8<T>::kN; ++j)
             if (at + j == target) {          // 1 - p without a difference
                 const float log_p = fmaf(v.get(j) - top, scale, -log_total), p = exp2_fast(max_nan(log_p * kLog2e, kLeastZ));
-                const float by_entropy = dentropy == 0.f ? 0.f : __fmul_rn(dentropy * p, max_nan(log_p, kLeastZ) + entropy);
-                g[j] = scale * fmaf(dlogprob, -expm1f(log_p), -by_entropy);   // (spelt out: two kernels give the same bits)
+                g[j] = scale * fmaf(dlogprob, -expm1f(log_p), dentropy == 0.f ? 0.f : -dentropy * p * (max_nan(log_p, kLeastZ) + entropy));
             }
+    }
+    // of a vector whose first entry is number `at`
+    template <typename T> __device__ __forceinline__ void of(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
+#pragma unroll
+        for (int j = 0; j < Logits8<T>::kN; ++j) g[j] = 0.f;
+        if (zero) return;
+        if (slope == 0.f) plain<T, false>(v, g); else plain<T, true>(v, g);
+        given(v, at, g);
     }
 };
 
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant_
 // The loss and its gradient of many rows that fit into shared memory: a CTA takes every gridDim.x-th row.  One warp brings the rows in by
 // bulk copies, chunk after chunk into a ring; the others read a row twice there, for its sums and for the gradient, and give the
 // chunks back on the second time.  Every logit crosses from memory once, and what is free of the ring holds the next row's first
-// chunks while a row's sums are joined.  The pieces of a row before and after its whole vectors are read from memory.
+// chunks while a row's sums are joined.  The pieces of a row before and after its whole vectors come by the copying warp's own loads.
 template <int N> struct RingShape {                         // N threads that work
     static constexpr int kChunk = 2 * N;                    // vectors
     static constexpr int kCtas = N <= 256 ? 2 : 1;          // on an SM
@@ -556,22 +561,31 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
     pdl_wait();
     bool ok = true;
     if (warp_id() == kWarps) {                               // ---- copies ----
-        if (lane_id() == 0) {
-            int slot = 0;
-            unsigned phase = 1;                              // every slot is free at first
-            for (long long row = blockIdx.x; row < p.rows && ok; row += gridDim.x) {
-                const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
-                const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
-                for (int v = 0; v < end; v += S::kChunk) {
-                    ok = bar_wait(empty + 8 * slot, phase);
-                    if (!ok) break;
-                    const int from = max(v, whole0), to = min(v + S::kChunk, whole1);
+        int slot = 0;
+        unsigned phase = 1;                                  // every slot is free at first
+        for (long long row = blockIdx.x; row < p.rows && ok; row += gridDim.x) {
+            const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
+            const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
+            // an entry of the first or the last vector, where they lie partly outside the row
+            const int piece = lane_id() / kN == 0 && whole0 ? 0 : lane_id() / kN == 1 && whole1 < end ? whole1 : -1, entry = x.first(piece) + lane_id() % kN;
+            T value = from_float<T>(-INFINITY);
+            if (piece >= 0 && entry >= 0 && entry < p.vocab) value = x.row[entry];
+            for (int v = 0; v < end; v += S::kChunk) {
+                ok = bar_wait(empty + 8 * slot, phase);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                unsigned char* const at = ring + slot * S::kChunk * 16;
+                const int from = max(v, whole0), to = min(v + S::kChunk, whole1);
+                if (piece >= v && piece < v + S::kChunk) reinterpret_cast<T*>(at)[(piece - v) * kN + lane_id() % kN] = value;
+                __syncwarp();
+                if (lane_id() == 0) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the pieces' places belong to a copy again next time)
                     if (from < to) {
                         bar_expect(full + 8 * slot, (to - from) * 16);
-                        copy_bytes(smem_addr(ring) + (slot * S::kChunk + from - v) * 16, x.row + x.first(from), (to - from) * 16, full + 8 * slot);
+                        copy_bytes(smem_addr(at) + (from - v) * 16, x.row + x.first(from), (to - from) * 16, full + 8 * slot);
                     } else bar_arrive(full + 8 * slot);
-                    if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
                 }
+                if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
             }
         }
     } else {
@@ -580,30 +594,35 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
         for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
             const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
             const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
-            // the thread's vectors of the chunk at v in the slot k; a chunk that never came is NaN
+            // vector `at` of the chunk at v, which is in slot k; a chunk that never came is NaN
             auto take = [&](Logits8<T>& to, int v, int at, int k) {
                 if (!ok) to.v = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
-                else if (at >= whole0 && at < whole1) to.v = *reinterpret_cast<const uint4*>(ring + (k * S::kChunk + at - v) * 16);
-                else if (at < end) to = x.load(at);
+                else if (at < end) to.v = *reinterpret_cast<const uint4*>(ring + (k * S::kChunk + at - v) * 16);
                 else to = Logits8<T>::nothing();
             };
+            const uint4* const mine_of_slot0 = reinterpret_cast<const uint4*>(ring) + threadIdx.x;
             const long long target = checked_target(p, row, threadIdx.x == 0);
             const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x.row[target]) : 0.f;
             Part mine = no_part();
             const int slot0 = slot;
             for (int v = 0; v < end; v += 2 * S::kChunk) {
-                Logits8<T> y[kLpVecs];
                 static_assert(kLpVecs == 4, "two chunks of two vectors");
+                Logits8<T> y[kLpVecs];
+                const bool both = v + S::kChunk < end;
+                ok = ok && bar_wait(full + 8 * slot, phase);
+                const int a = slot;
+                if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
+                const int b = slot;
+                if (both) {
+                    ok = ok && bar_wait(full + 8 * slot, phase);
+                    if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
+                }
+                if (ok && v + 2 * S::kChunk <= end) {
+                    y[0].v = mine_of_slot0[a * S::kChunk]; y[1].v = mine_of_slot0[a * S::kChunk + N];
+                    y[2].v = mine_of_slot0[b * S::kChunk]; y[3].v = mine_of_slot0[b * S::kChunk + N];
+                } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int c = v + h * S::kChunk;
-                    if (c < end) {
-                        if (ok) ok = bar_wait(full + 8 * slot, phase);
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                    }
-                    take(y[2 * h], c, c + threadIdx.x, slot);
-                    take(y[2 * h + 1], c, c + N + threadIdx.x, slot);
-                    if (c < end && ++slot == S::kSlots) { slot = 0; phase ^= 1; }
+                    for (int i = 0; i < kLpVecs; ++i) take(y[i], v + i / 2 * S::kChunk, v + i * N + threadIdx.x, i < 2 ? a : b);
                 }
                 add_logits<T>(mine, y, p.scale2);
             }
@@ -611,9 +630,8 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
             Part all = join_lanes(mine.m == -INFINITY && mine.r != mine.r ? Part{0.f, mine.r, mine.r} : mine, p.scale2, owner);
             if (all.r < 0.25f && all.m != -INFINITY) {       // (as in k_logprob)
                 const float exact = others_of<T>((end + N - 1) / N, all.m, p.scale2, [&](int i) {
-                    const int v = i / 2 * S::kChunk;
                     Logits8<T> y;
-                    take(y, v, i * N + warp_id() * 32 + owner, (slot0 + i / 2) % S::kSlots);
+                    take(y, i / 2 * S::kChunk, i * N + warp_id() * 32 + owner, (slot0 + i / 2) % S::kSlots);
                     return y;
                 });
                 all.r += exact - __shfl_sync(0xFFFFFFFFu, mine.r, owner);
@@ -626,25 +644,53 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
             const RowGrad grad(p, row, target, all.m, sums.log_total, sums.entropy);
             OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
             const bool aligned = vec_aligned<OT, kN>(d, x.skew);
-            int k = slot0;
-            for (int v = 0; v < end; v += S::kChunk) {
-                Logits8<T> y[2];
+            auto gradients = [&](auto slope) {
+                constexpr bool kSlope = decltype(slope)::value;
+                int k = slot0;
+                for (int v = 0; v < end; v += S::kChunk) {
+                    if (ok && aligned && v >= whole0 && v + S::kChunk <= whole1) {
+                        const bool here = target >= x.first(v) && target < x.first(v + S::kChunk);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) take(y[h], v, v + h * N + threadIdx.x, k);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int at = v + h * N + threadIdx.x;
-                    if (at >= end) continue;
-                    float g[kN];
-                    grad.of(y[h], x.first(at), g);
-                    store_vec<OT, kN>(d, x.first(at), p.vocab, g, aligned);
+                        for (int h = 0; h < 2; ++h) {
+                            const int at = x.first(v + h * N + threadIdx.x);
+                            Logits8<T> y;
+                            y.v = mine_of_slot0[k * S::kChunk + h * N];
+                            float g[kN];
+                            grad.template plain<T, kSlope>(y, g);
+                            if (here) grad.given(y, at, g);
+                            store_whole<OT, kN>(d + at, g);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            const int i = v + h * N + threadIdx.x, at = x.first(i);
+                            if (i >= end) break;
+                            Logits8<T> y;
+                            take(y, v, i, k);
+                            float g[kN];
+                            grad.template plain<T, kSlope>(y, g);
+                            grad.given(y, at, g);
+                            store_vec<OT, kN>(d, at, p.vocab, g, aligned);
+                        }
+                    }
+                    // The chunk goes back once every lane has worked with what it read: a read that was only issued may still be on
+                    // its way when the next copy lands.
+                    __syncwarp();
+                    if (lane_id() == 0) bar_arrive(empty + 8 * k);
+                    if (++k == S::kSlots) k = 0;
                 }
-                // The chunk goes back once every lane has worked with what it read: a read that was only issued may still be on its
-                // way when the next copy lands.
-                __syncwarp();
-                if (lane_id() == 0) bar_arrive(empty + 8 * k);
-                if (++k == S::kSlots) k = 0;
-            }
+            };
+            if (grad.zero) {
+                const float none[kN] = {};
+                int k = slot0;
+                for (int v = 0; v < end; v += S::kChunk) {
+                    for (int i = v + threadIdx.x; i < min(v + S::kChunk, end); i += N) store_vec<OT, kN>(d, x.first(i), p.vocab, none, aligned);
+                    __syncwarp();
+                    if (lane_id() == 0) bar_arrive(empty + 8 * k);
+                    if (++k == S::kSlots) k = 0;
+                }
+            } else if (grad.slope == 0.f) gradients(std::false_type{});
+            else gradients(std::true_type{});
         }
     }
     if (!ok) {                                               // let copies in flight land

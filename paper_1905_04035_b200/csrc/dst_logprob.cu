@@ -195,15 +195,14 @@ struct RowGrad {
             } else apart(mul2(two(exp2_fast(z0), exp2_fast(z1)), b2), g[j], g[j + 1]);
         }
     }
-    // the target's place, where the vector at entry `at` has it
-    template <typename T> __device__ __forceinline__ void given(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
-        if (target < at || target >= at + Logits8<T>::kN) return;
-#pragma unroll
-        for (int j = 0; j < Logits8<T>::kN; ++j)
-            if (at + j == target) {          // 1 - p without a difference
-                const float log_p = fmaf(v.get(j) - top, scale, -log_total), p = exp2_fast(max_nan(log_p * kLog2e, kLeastZ));
-                g[j] = scale * fmaf(dlogprob, -expm1f(log_p), dentropy == 0.f ? 0.f : -dentropy * p * (max_nan(log_p, kLeastZ) + entropy));
-            }
+    // of one logit: any, and the target's, with 1 - p not as a difference
+    __device__ __forceinline__ float at(float x) const {
+        const float z = max_nan((x - top) * scale2, kLeastZ);
+        return exp2_fast(z) * fmaf(slope, z, base);
+    }
+    __device__ __forceinline__ float target_at(float x) const {
+        const float log_p = fmaf(x - top, scale, -log_total), p = exp2_fast(max_nan(log_p * kLog2e, kLeastZ));
+        return scale * fmaf(dlogprob, -expm1f(log_p), dentropy == 0.f ? 0.f : -dentropy * p * (max_nan(log_p, kLeastZ) + entropy));
     }
     // of a vector whose first entry is number `at`
     template <typename T> __device__ __forceinline__ void of(const Logits8<T>& v, int at, float (&g)[Logits8<T>::kN]) const {
@@ -211,7 +210,9 @@ struct RowGrad {
         for (int j = 0; j < Logits8<T>::kN; ++j) g[j] = 0.f;
         if (zero) return;
         if (slope == 0.f) plain<T, false>(v, g); else plain<T, true>(v, g);
-        given(v, at, g);
+        if (target >= at && target < at + Logits8<T>::kN)
+#pragma unroll
+            for (int j = 0; j < Logits8<T>::kN; ++j) if (at + j == target) g[j] = target_at(v.get(j));
     }
 };
 
@@ -538,16 +539,17 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant_
 // bulk copies, chunk after chunk into a ring; the others read a row twice there, for its sums and for the gradient, and give the
 // chunks back on the second time.  Every logit crosses from memory once, and what is free of the ring holds the next row's first
 // chunks while a row's sums are joined.  The pieces of a row before and after its whole vectors come by the copying warp's own loads.
-template <int N> struct RingShape {                         // N threads that work
+template <int N> struct Ring {                              // N threads that work; one more warp copies
+    static constexpr int kCtas = N <= 384 ? 2 : 1;          // on an SM
     static constexpr int kChunk = 2 * N;                    // vectors
-    static constexpr int kCtas = N <= 256 ? 2 : 1;          // on an SM
-    static constexpr int kSlots = (kCtas == 2 ? 113 : 225) * 1024 / (kChunk * 16) < 32 ? (kCtas == 2 ? 113 : 225) * 1024 / (kChunk * 16) : 32;
+    static constexpr int kSlots = (kCtas == 2 ? 112 : 224) * 1024 / (kChunk * 16);
     static constexpr int kSmem = kSlots * kChunk * 16;
 };
 template <typename T, typename OT, int N>
-__global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(const __grid_constant__ LogprobParams p) {
-    using S = RingShape<N>;
+__global__ void __launch_bounds__(N + 32, Ring<N>::kCtas) k_logprob_ring(const __grid_constant__ LogprobParams p) {
+    using S = Ring<N>;
     constexpr int kN = Logits8<T>::kN, kWarps = N / 32;
+    static_assert(kLpVecs == 4, "two chunks of two vectors");
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ Part parts[2][kWarps];
     __shared__ __align__(8) unsigned long long bars[2 * S::kSlots];
@@ -589,50 +591,49 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
             }
         }
     } else {
+        const uint4* const slots = reinterpret_cast<const uint4*>(ring);
         int slot = 0, turn = 0;
         unsigned phase = 0;
         for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
             const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);
-            const int whole0 = x.skew ? 1 : 0, whole1 = (p.vocab + x.skew) / kN, end = (p.vocab + x.skew + kN - 1) / kN;
-            // vector `at` of the chunk at v, which is in slot k; a chunk that never came is NaN
-            auto take = [&](Logits8<T>& to, int v, int at, int k) {
-                if (!ok) to.v = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
-                else if (at < end) to.v = *reinterpret_cast<const uint4*>(ring + (k * S::kChunk + at - v) * 16);
-                else to = Logits8<T>::nothing();
-            };
-            const uint4* const mine_of_slot0 = reinterpret_cast<const uint4*>(ring) + threadIdx.x;
+            const int end = (p.vocab + x.skew + kN - 1) / kN, chunks = (end + S::kChunk - 1) / S::kChunk;
             const long long target = checked_target(p, row, threadIdx.x == 0);
-            const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x.row[target]) : 0.f;
+            const float given = target >= 0 ? to_float<T>(x.row[target]) : 0.f;   // (read before anything is written, which may be in place)
             Part mine = no_part();
             const int slot0 = slot;
-            for (int v = 0; v < end; v += 2 * S::kChunk) {
-                static_assert(kLpVecs == 4, "two chunks of two vectors");
-                Logits8<T> y[kLpVecs];
-                const bool both = v + S::kChunk < end;
+            auto next_chunk = [&] {
                 ok = ok && bar_wait(full + 8 * slot, phase);
-                const int a = slot;
+                const uint4* const at = slots + slot * S::kChunk + threadIdx.x;
                 if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
-                const int b = slot;
-                if (both) {
-                    ok = ok && bar_wait(full + 8 * slot, phase);
-                    if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
-                }
-                if (ok && v + 2 * S::kChunk <= end) {
-                    y[0].v = mine_of_slot0[a * S::kChunk]; y[1].v = mine_of_slot0[a * S::kChunk + N];
-                    y[2].v = mine_of_slot0[b * S::kChunk]; y[3].v = mine_of_slot0[b * S::kChunk + N];
+                return at;
+            };
+#pragma unroll 1
+            for (int c = 0; c < chunks; c += 2) {
+                Logits8<T> v[kLpVecs];
+                const uint4* from = next_chunk();
+                if ((c + 2) * S::kChunk <= end) {
+                    v[0].v = from[0]; v[1].v = from[N];
+                    from = next_chunk();
+                    v[2].v = from[0]; v[3].v = from[N];
                 } else {
+                    const uint4* const more = c + 1 < chunks ? next_chunk() : from;
 #pragma unroll
-                    for (int i = 0; i < kLpVecs; ++i) take(y[i], v + i / 2 * S::kChunk, v + i * N + threadIdx.x, i < 2 ? a : b);
+                    for (int i = 0; i < kLpVecs; ++i) {
+                        v[i] = Logits8<T>::nothing();
+                        if (c * S::kChunk + i * N + (int)threadIdx.x < end) v[i].v = (i < 2 ? from : more)[(i & 1) * N];
+                    }
                 }
-                add_logits<T>(mine, y, p.scale2);
+                add_logits<T>(mine, v, p.scale2);
             }
+            if (!ok) mine.r = NAN;                           // a copy that never came
             int owner;
             Part all = join_lanes(mine.m == -INFINITY && mine.r != mine.r ? Part{0.f, mine.r, mine.r} : mine, p.scale2, owner);
-            if (all.r < 0.25f && all.m != -INFINITY) {       // (as in k_logprob)
-                const float exact = others_of<T>((end + N - 1) / N, all.m, p.scale2, [&](int i) {
-                    Logits8<T> y;
-                    take(y, i / 2 * S::kChunk, i * N + warp_id() * 32 + owner, (slot0 + i / 2) % S::kSlots);
-                    return y;
+            if (all.r < 0.25f && all.m != -INFINITY) {       // (as in k_logprob; the lane's vectors by memory)
+                const int first = warp_id() * 32 + owner;
+                const float exact = others_of<T>((end - first + N - 1) / N, all.m, p.scale2, [&](int i) {
+                    Logits8<T> v;
+                    v.v = slots[(slot0 + i / 2) % S::kSlots * S::kChunk + (i & 1) * N + first];
+                    return v;
                 });
                 all.r += exact - __shfl_sync(0xFFFFFFFFu, mine.r, owner);
             }
@@ -643,54 +644,57 @@ __global__ void __launch_bounds__(N + 32, RingShape<N>::kCtas) k_logprob_ring(co
             if (threadIdx.x == 0) sums.write(p, row, target, given);
             const RowGrad grad(p, row, target, all.m, sums.log_total, sums.entropy);
             OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
+            const int whole0 = x.skew != 0, whole1 = (p.vocab + x.skew) / kN;
             const bool aligned = vec_aligned<OT, kN>(d, x.skew);
-            auto gradients = [&](auto slope) {
-                constexpr bool kSlope = decltype(slope)::value;
+            // f(chunk, the thread's two vectors of it) for the row's chunks, which go back once every lane has worked with what it read: a
+            // read that was only issued may still be on its way when the next copy lands
+            auto each_chunk = [&](auto f) {
                 int k = slot0;
-                for (int v = 0; v < end; v += S::kChunk) {
-                    if (ok && aligned && v >= whole0 && v + S::kChunk <= whole1) {
-                        const bool here = target >= x.first(v) && target < x.first(v + S::kChunk);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int at = x.first(v + h * N + threadIdx.x);
-                            Logits8<T> y;
-                            y.v = mine_of_slot0[k * S::kChunk + h * N];
-                            float g[kN];
-                            grad.template plain<T, kSlope>(y, g);
-                            if (here) grad.given(y, at, g);
-                            store_whole<OT, kN>(d + at, g);
-                        }
-                    } else {
 #pragma unroll 1
-                        for (int h = 0; h < 2; ++h) {
-                            const int i = v + h * N + threadIdx.x, at = x.first(i);
-                            if (i >= end) break;
-                            Logits8<T> y;
-                            take(y, v, i, k);
-                            float g[kN];
-                            grad.template plain<T, kSlope>(y, g);
-                            grad.given(y, at, g);
-                            store_vec<OT, kN>(d, at, p.vocab, g, aligned);
-                        }
-                    }
-                    // The chunk goes back once every lane has worked with what it read: a read that was only issued may still be on
-                    // its way when the next copy lands.
+                for (int c = 0; c < chunks; ++c) {
+                    f(c, slots + k * S::kChunk + threadIdx.x);
                     __syncwarp();
                     if (lane_id() == 0) bar_arrive(empty + 8 * k);
                     if (++k == S::kSlots) k = 0;
                 }
             };
-            if (grad.zero) {
-                const float none[kN] = {};
-                int k = slot0;
-                for (int v = 0; v < end; v += S::kChunk) {
-                    for (int i = v + threadIdx.x; i < min(v + S::kChunk, end); i += N) store_vec<OT, kN>(d, x.first(i), p.vocab, none, aligned);
-                    __syncwarp();
-                    if (lane_id() == 0) bar_arrive(empty + 8 * k);
-                    if (++k == S::kSlots) k = 0;
-                }
-            } else if (grad.slope == 0.f) gradients(std::false_type{});
+            auto gradients = [&](auto slope) {
+                OT* const mine_out = d + x.first(threadIdx.x);
+                each_chunk([&](int c, const uint4* from) {
+                    OT* const to = mine_out + c * (S::kChunk * kN);
+                    const int at = c * S::kChunk + threadIdx.x;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        Logits8<T> v;
+                        v.v = from[h * N];
+                        float g[kN];
+                        grad.template plain<T, decltype(slope)::value>(v, g);
+                        if (at + h * N >= whole0 && at + h * N < whole1) store_whole<OT, kN>(to + h * N * kN, g);
+                    }
+                });
+            };
+            if (grad.zero || !aligned)
+                each_chunk([&](int c, const uint4* from) {
+#pragma unroll 1
+                    for (int at = c * S::kChunk + threadIdx.x, h = 0; h < 2 && at < end; at += N, ++h) {
+                        Logits8<T> v;
+                        v.v = from[h * N];
+                        float g[kN];
+                        grad.of(v, x.first(at), g);
+                        store_vec<OT, kN>(d, x.first(at), p.vocab, g, aligned);
+                    }
+                });
+            else if (grad.slope == 0.f) gradients(std::false_type{});
             else gradients(std::true_type{});
+            if (grad.zero || !aligned) continue;
+            // the target, by the thread that wrote its vector, and the pieces before and after the whole vectors, an entry a lane
+            const int of = target >= 0 ? (int)((target + x.skew) / kN) : -1;
+            if (of >= whole0 && of < whole1 && of % N == (int)threadIdx.x) d[target] = from_float<OT>(grad.target_at(given));
+            const int pieces = p.vocab - (whole1 - whole0) * kN, entry = lane_id() < x.first(whole0) ? lane_id() : lane_id() + (whole1 - whole0) * kN;
+            if (warp_id() == kWarps - 1 && lane_id() < pieces) {
+                const float v = to_float<T>(x.row[entry]);
+                d[entry] = from_float<OT>(entry == target ? grad.target_at(v) : grad.at(v));
+            }
         }
     }
     if (!ok) {                                               // let copies in flight land
@@ -739,15 +743,10 @@ cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream
     return type == DST_F32 ? logprob_t<float, float, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false>(p, sms, stream);
 }
 
-// The ring takes rows that leave it room for two more chunks, enough of them for every CTA, and long enough for its threads.
-template <int N> static bool ring_fits(const LogprobParams& p, int per_vector, int sms) {
-    using S = RingShape<N>;
-    const long long vectors = (p.vocab + 2 * per_vector - 2) / per_vector, chunks = (vectors + S::kChunk - 1) / S::kChunk;
-    return chunks + 2 <= S::kSlots && vectors > 1024 && p.rows >= (long long)sms * S::kCtas;
-}
+// Enough rows for every SM, longer than what a few warps hold, and short enough for the ring's threads.
 template <typename T, typename OT, int N>
 static cudaError_t ring_run(const LogprobParams& p, int sms, cudaStream_t stream) {
-    using S = RingShape<N>;
+    using S = Ring<N>;
     static SmemOptIn opt;
     const cudaError_t e = ensure_dynamic_smem(k_logprob_ring<T, OT, N>, S::kSmem, opt);
     if (e != cudaSuccess) return e;
@@ -756,8 +755,12 @@ static cudaError_t ring_run(const LogprobParams& p, int sms, cudaStream_t stream
 }
 template <typename T, typename OT>
 static cudaError_t loss_t(const LogprobParams& p, int sms, cudaStream_t stream) {
-    if (ring_fits<256>(p, Logits8<T>::kN, sms)) return ring_run<T, OT, 256>(p, sms, stream);
-    if (ring_fits<512>(p, Logits8<T>::kN, sms)) return ring_run<T, OT, 512>(p, sms, stream);
+    constexpr int kTwo = 384, kOne = 480;
+    const long long vectors = (p.vocab + 2 * Logits8<T>::kN - 2) / Logits8<T>::kN;
+    if (p.rows >= 2 * sms && vectors > 1024) {
+        if (vectors <= (Ring<kTwo>::kSlots - 2) * Ring<kTwo>::kChunk) return ring_run<T, OT, kTwo>(p, sms, stream);
+        if (vectors <= (Ring<kOne>::kSlots - 2) * Ring<kOne>::kChunk) return ring_run<T, OT, kOne>(p, sms, stream);
+    }
     return logprob_t<T, OT, true>(p, sms, stream);
 }
 cudaError_t launch_logprob_loss(const LogprobParams& p, int type, int d_type, int sms, cudaStream_t stream) {

@@ -11,7 +11,8 @@
  * Conventions are those of dst.h and dst_tied.h: device pointers, caller-owned buffers, nothing allocated or
  * synchronised, all work on `stream`, bad arguments refused on the host before anything is enqueued.  A matrix argument
  * has a leading dimension in elements; its rows are contiguous.  Sizes of zero are valid and do nothing unless a comment
- * says otherwise.  Results depend on the inputs and sizes alone: two calls give the same bits.
+ * says otherwise.  Two calls with the same arguments give the same bits; the order of sums follows from the sizes and types, and
+ * from how rows are aligned.
  */
 #ifndef DST_STEP_H_
 #define DST_STEP_H_

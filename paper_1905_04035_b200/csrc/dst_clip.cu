@@ -12,9 +12,10 @@ namespace dst {
 constexpr int kClipEntries = 96;             // tensors of a launch
 constexpr int kClipThreads = 256;
 constexpr int kClipVecs = 8;                 // groups of eight elements that a thread takes of a chunk
-constexpr int kClipBatch = 4;               // of which are in flight at a time
+constexpr int kClipBatch = 2;               // of which are in flight at a time
 constexpr int kClipChunk = kClipThreads * kClipVecs * 8;
-constexpr int kClipCtas = 4 * kSmCount;      // most CTAs of a launch (of a B200, not the device's: they fix the order of sums)
+constexpr int kClipOnSm = 6;                 // CTAs that fit an SM, and
+constexpr int kClipCtas = kClipOnSm * kSmCount;   // most CTAs of a launch (of a B200's SMs, not the device's: they fix the order of sums)
 
 struct ClipEntry {
     const void* in;
@@ -48,12 +49,20 @@ __device__ __forceinline__ double chunk_squares(const T* x, int n) {
     int done = 0;
     if (aligned16(x)) {
         done = n / 8 * 8;
-#pragma unroll 4
-        for (int i = threadIdx.x * 8; i < done; i += kClipThreads * 8) {
-            float v[8];
-            load8<T>(x + i, v);
+#pragma unroll 1
+        for (int from = threadIdx.x * 8; from < done; from += kClipBatch * kClipThreads * 8) {
+            float v[kClipBatch][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j & 1] = fma((double)v[j], (double)v[j], s[j & 1]);
+            for (int i = 0; i < kClipBatch; ++i) {
+                if (from + i * kClipThreads * 8 < done) load8<T>(x + from + i * kClipThreads * 8, v[i]);
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < kClipBatch; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j & 1] = fma((double)v[i][j], (double)v[i][j], s[j & 1]);
         }
     }
     for (int i = done + threadIdx.x; i < n; i += kClipThreads) {
@@ -69,7 +78,7 @@ __device__ __forceinline__ double warp_sum(double x) {
     return x;
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_grad_squares(const __grid_constant__ ClipTable t, double* __restrict__ parts) {
+__global__ void __launch_bounds__(kClipThreads, kClipOnSm) k_grad_squares(const __grid_constant__ ClipTable t, double* __restrict__ parts) {
     __shared__ double sums[kClipThreads / 32];
     pdl_trigger();
     pdl_wait();
@@ -106,46 +115,61 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_norm(const double* __rest
     }
 }
 
-template <typename T, typename OT>
-__device__ __forceinline__ void scale_chunk(const T* x, OT* out, int n, float f) {
+__device__ __forceinline__ float scaled(float x, float f) { return f == 0.f ? 0.f : x * f; }
+__device__ __forceinline__ unsigned scaled_two(unsigned w, float f) {      // two bf16
+    return pack_bf16(scaled(__uint_as_float(w << 16), f), scaled(__uint_as_float(w & 0xFFFF0000u), f));
+}
+// 16 bytes of a tensor whose output has its type
+__device__ __forceinline__ uint4 scaled_piece(uint4 v, float f, const float*) {
+    return make_uint4(__float_as_uint(scaled(__uint_as_float(v.x), f)), __float_as_uint(scaled(__uint_as_float(v.y), f)),
+                      __float_as_uint(scaled(__uint_as_float(v.z), f)), __float_as_uint(scaled(__uint_as_float(v.w), f)));
+}
+__device__ __forceinline__ uint4 scaled_piece(uint4 v, float f, const __nv_bfloat16*) {
+    return make_uint4(scaled_two(v.x, f), scaled_two(v.y, f), scaled_two(v.z, f), scaled_two(v.w, f));
+}
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const T* x, T* out, int n, float f) {
+    constexpr int kPer = 16 / (int)sizeof(T), kBatch = 4;
     int done = 0;
     if (aligned16(x) && aligned16(out)) {
-        done = n / 8 * 8;
+        const int pieces = n / kPer;
+        done = pieces * kPer;
+        const uint4* const from = reinterpret_cast<const uint4*>(x);
+        uint4* const to = reinterpret_cast<uint4*>(out);
 #pragma unroll 1
-        for (int from = threadIdx.x * 8; from < done; from += kClipBatch * kClipThreads * 8) {
-            float v[kClipBatch][8];
+        for (int i = threadIdx.x; i < pieces; i += kBatch * kClipThreads) {
+            uint4 v[kBatch];
 #pragma unroll
-            for (int i = 0; i < kClipBatch; ++i) if (from + i * kClipThreads * 8 < done) load8<T>(x + from + i * kClipThreads * 8, v[i]);
+            for (int j = 0; j < kBatch; ++j) if (i + j * kClipThreads < pieces) v[j] = from[i + j * kClipThreads];
 #pragma unroll
-            for (int i = 0; i < kClipBatch; ++i) {
-                if (from + i * kClipThreads * 8 >= done) break;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = f == 0.f ? 0.f : v[i][j] * f;
-                store8<OT>(out + from + i * kClipThreads * 8, v[i]);
-            }
+            for (int j = 0; j < kBatch; ++j) if (i + j * kClipThreads < pieces) to[i + j * kClipThreads] = scaled_piece(v[j], f, x);
         }
     }
-    for (int i = done + threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<OT>(f == 0.f ? 0.f : to_float<T>(x[i]) * f);
+    for (int i = done + threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(scaled(to_float<T>(x[i]), f));
+}
+template <typename T, typename OT>
+__device__ __forceinline__ void scale_convert(const T* x, OT* out, int n, float f) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<OT>(scaled(to_float<T>(x[i]), f));
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_clip(const __grid_constant__ ClipTable t, const float* __restrict__ clip) {
+__global__ void __launch_bounds__(kClipThreads, 4) k_clip(const __grid_constant__ ClipTable t, const float* __restrict__ clip) {
     pdl_trigger();
     pdl_wait();
     const float f = clip[1];
-    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {   // last first: what the norm read last is still in L2
         long long start;
         int n;
         const ClipEntry& e = tensor_of(t, c, start, n);
         if (f == 1.f && e.in == e.out) continue;             // (in place: nothing to do)
-        if (e.in_type == DST_F32) {
-            const float* const x = static_cast<const float*>(e.in) + start;
-            if (e.out_type == DST_F32) scale_chunk(x, static_cast<float*>(e.out) + start, n, f);
-            else scale_chunk(x, static_cast<__nv_bfloat16*>(e.out) + start, n, f);
-        } else {
-            const __nv_bfloat16* const x = static_cast<const __nv_bfloat16*>(e.in) + start;
-            if (e.out_type == DST_F32) scale_chunk(x, static_cast<float*>(e.out) + start, n, f);
-            else scale_chunk(x, static_cast<__nv_bfloat16*>(e.out) + start, n, f);
-        }
+        const float* const x = static_cast<const float*>(e.in) + start;
+        const __nv_bfloat16* const h = static_cast<const __nv_bfloat16*>(e.in) + start;
+        float* const out = static_cast<float*>(e.out) + start;
+        __nv_bfloat16* const half = static_cast<__nv_bfloat16*>(e.out) + start;
+        if (e.in_type == DST_F32 && e.out_type == DST_F32) scale_chunk(x, out, n, f);
+        else if (e.in_type == DST_BF16 && e.out_type == DST_BF16) scale_chunk(h, half, n, f);
+        else if (e.in_type == DST_F32) scale_convert(x, half, n, f);
+        else scale_convert(h, out, n, f);
     }
 }
 

@@ -22,6 +22,12 @@ __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
         if (clock64() - t0 > kWaitCycles) return false;
     return true;
 }
+// true for one lane of a converged warp; the compiler then knows that one thread goes on, and keeps what it computes in uniform registers
+__device__ __forceinline__ bool elect_one() {
+    unsigned yes;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.b32 %0, 1, 0, p; }" : "=r"(yes));
+    return yes != 0;
+}
 // `bytes` (a multiple of 16) from global to shared memory, both aligned to 16; `bar` counts them
 __device__ __forceinline__ void copy_bytes(unsigned dst, const void* src, unsigned bytes, unsigned bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");

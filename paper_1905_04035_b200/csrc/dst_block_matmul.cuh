@@ -371,7 +371,7 @@ k_block_matmul(const __grid_constant__ CUtensorMap map_p, const __grid_constant_
             }
         }
     } else if (warp == S::kEpiWarps + 1) {                                         // ---- matrix instructions ----
-        if (lane == 0 && rank == 0) {
+        if (elect_one() && rank == 0) {
             // both operands e4m3 (0) or e2m1 (1) with the inner dimension contiguous, N and M of the instruction, scales as exponents
             constexpr unsigned kElement = std::is_same<KIND, Fp4Kind>::value ? 1u << 7 | 1u << 10 : 0u;
             constexpr unsigned idesc = kElement | (unsigned)(NT >> 3) << 17 | 1u << 23 | (unsigned)((kTileP * CG) >> 4) << 24;

@@ -36,6 +36,7 @@ struct Fp8Kind { static constexpr int kStepCols = 128, kScaleSteps = 4, kScaleTi
 struct Fp4Kind { static constexpr int kStepCols = 256, kScaleSteps = 1, kScaleTiles = 2, kChunk = 4, kResident = 16384; };
 constexpr int kTileP = 128;                               // rows of P a CTA
 constexpr int kSmemMost = 232448;
+constexpr int kHalvesPitch = 512 + 16;                    // bytes of shared memory for a row of 256 columns in 16 bits
 
 // FUSED: Q is quantised by the CTA itself from the rows of x, kept whole in shared memory (kResident bytes) and used for
 // every tile; its result leaves swapped.
@@ -215,6 +216,41 @@ __device__ __forceinline__ void store_row(const MatmulParams& p, OT* out, const 
     else if (sizeof(OT) == 4 || (at & 3) == 0) store_row_aligned<OT, COLS, 4>(p, out, acc, buffer, row, col0);
     else store_row_aligned<OT, COLS, 2>(p, out, acc, buffer, row, col0);
 }
+// A row of 256 columns in 16 bits by the two warps that hold its halves: 512 bytes are one copy, and half as many copies are what the
+// unit that makes them is busy with (4096 x 33,708 x 1024 in 4 bits: %WIDE%).  Each of the warps issues every other row's copy.  Rows are
+// aligned to four bytes at least, so that no word has elements of both.
+template <int ALIGN>
+__device__ __forceinline__ void store_row_halves(const MatmulParams& p, __nv_bfloat16* out, const float (&acc)[128], unsigned char* buffer, int row, int col0, int half, int pair) {
+    const bool issues = (lane_id() & 1) == half;
+    if (issues) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+    unsigned char* const at = reinterpret_cast<unsigned char*>(out + (long long)row * p.ldo + col0);
+    const int shift = (int)(reinterpret_cast<uintptr_t>(at) & 15u), total = min(256, p.rows_q - col0) * 2;
+    unsigned char* const base = buffer + shift + half * 256;
+    unsigned v[64];
+#pragma unroll
+    for (int w = 0; w < 64; ++w) v[w] = pack_bf16(acc[2 * w], acc[2 * w + 1]);
+#pragma unroll
+    for (int w = 0; w < 64; w += ALIGN / 4) {
+        if (ALIGN == 16) *reinterpret_cast<uint4*>(base + w * 4) = make_uint4(v[w], v[w + 1], v[w + 2], v[w + 3]);
+        else if (ALIGN == 8) *reinterpret_cast<uint2*>(base + w * 4) = make_uint2(v[w], v[w + 1]);
+        else *reinterpret_cast<unsigned*>(base + w * 4) = v[w];
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+    if (!issues || row >= p.rows_p) return;
+    const int head = min((16 - shift) & 15, total), body = (total - head) & ~15;
+    if (body > 0)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;"
+                     ::"l"(at + head), "r"(smem_addr(buffer + shift + head)), "r"(body) : "memory");
+    auto plain = [&](int from, int n) {
+        const unsigned char* const src = buffer + shift;
+        for (; n >= 4; from += 4, n -= 4) *reinterpret_cast<unsigned*>(at + from) = *reinterpret_cast<const unsigned*>(src + from);
+        if (n > 0) *reinterpret_cast<unsigned short*>(at + from) = *reinterpret_cast<const unsigned short*>(src + from);
+    };
+    if (ALIGN < 16) plain(0, head);
+    plain(head + body, total - head - body);
+}
 // The result is [q, p]: a lane's row is its column there, neighbouring lanes write neighbouring elements.
 template <typename OT, int COLS>
 __device__ __forceinline__ void store_swapped(const MatmulParams& p, OT* out, const float (&acc)[COLS], int row, int col0) {
@@ -334,7 +370,7 @@ k_block_matmul(const __grid_constant__ CUtensorMap map_p, const __grid_constant_
     bool ok = true;
 
     if (warp == S::kEpiWarps) {                                                    // ---- copies ----
-        if (lane == 0) {
+        if (elect_one()) {
             const unsigned stages = smem_addr(smem), ring = smem_addr(scale_ring);
             const unsigned first_full = CG == 2 ? in_cta(full, 0) : full;          // the issuing CTA waits for both CTAs' copies
             int s = 0, used = 0;
@@ -478,7 +514,14 @@ k_block_matmul(const __grid_constant__ CUtensorMap map_p, const __grid_constant_
             }
             OT* const out = static_cast<OT*>(p.out) + part * p.split_stride;
             if (FUSED || p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
-            else store_row<OT, S::kCols>(p, out, acc, buffer, row0 + lane, col0);
+            else if constexpr (CG == 2 && NT == 256 && sizeof(OT) == 2) {
+                const unsigned at = (unsigned)reinterpret_cast<uintptr_t>(out) | (unsigned)(p.ldo * sizeof(OT));
+                unsigned char* const whole = out_rows + (quarter * 32 + lane) * kHalvesPitch;
+                if ((at & 15) == 0) store_row_halves<16>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);
+                else if ((at & 7) == 0) store_row_halves<8>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);
+                else if ((at & 3) == 0) store_row_halves<4>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);
+                else store_row<OT, S::kCols>(p, out, acc, buffer, row0 + lane, col0);
+            } else store_row<OT, S::kCols>(p, out, acc, buffer, row0 + lane, col0);
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }

@@ -36,7 +36,6 @@ struct Fp8Kind { static constexpr int kStepCols = 128, kScaleSteps = 4, kScaleTi
 struct Fp4Kind { static constexpr int kStepCols = 256, kScaleSteps = 1, kScaleTiles = 2, kChunk = 4, kResident = 16384; };
 constexpr int kTileP = 128;                               // rows of P a CTA
 constexpr int kSmemMost = 232448;
-constexpr int kHalvesPitch = 512 + 16;                    // bytes of shared memory for a row of 256 columns in 16 bits
 
 // FUSED: Q is quantised by the CTA itself from the rows of x, kept whole in shared memory (kResident bytes) and used for
 // every tile; its result leaves swapped.
@@ -217,8 +216,8 @@ __device__ __forceinline__ void store_row(const MatmulParams& p, OT* out, const 
     else store_row_aligned<OT, COLS, 2>(p, out, acc, buffer, row, col0);
 }
 // A row of 256 columns in 16 bits by the two warps that hold its halves: 512 bytes are one copy, and half as many copies are what the
-// unit that makes them is busy with (4096 x 33,708 x 1024 in 4 bits: %WIDE%).  Each of the warps issues every other row's copy.  Rows are
-// aligned to four bytes at least, so that no word has elements of both.
+// unit that makes them is busy with (4096 x 33,708 x 512 in 4 bits: 67 us against 82).  Each of the warps issues every other row's copy.
+// Rows are aligned to four bytes at least, so that no word has elements of both; `buffer` is the row's place in shared memory.
 template <int ALIGN>
 __device__ __forceinline__ void store_row_halves(const MatmulParams& p, __nv_bfloat16* out, const float (&acc)[128], unsigned char* buffer, int row, int col0, int half, int pair) {
     const bool issues = (lane_id() & 1) == half;
@@ -226,7 +225,7 @@ __device__ __forceinline__ void store_row_halves(const MatmulParams& p, __nv_bfl
     asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
     unsigned char* const at = reinterpret_cast<unsigned char*>(out + (long long)row * p.ldo + col0);
     const int shift = (int)(reinterpret_cast<uintptr_t>(at) & 15u), total = min(256, p.rows_q - col0) * 2;
-    unsigned char* const base = buffer + shift + half * 256;
+    unsigned char* const base = buffer + half * 256;
     unsigned v[64];
 #pragma unroll
     for (int w = 0; w < 64; ++w) v[w] = pack_bf16(acc[2 * w], acc[2 * w + 1]);
@@ -242,9 +241,9 @@ __device__ __forceinline__ void store_row_halves(const MatmulParams& p, __nv_bfl
     const int head = min((16 - shift) & 15, total), body = (total - head) & ~15;
     if (body > 0)
         asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;"
-                     ::"l"(at + head), "r"(smem_addr(buffer + shift + head)), "r"(body) : "memory");
+                     ::"l"(at + head), "r"(smem_addr(buffer + head)), "r"(body) : "memory");
     auto plain = [&](int from, int n) {
-        const unsigned char* const src = buffer + shift;
+        const unsigned char* const src = buffer;
         for (; n >= 4; from += 4, n -= 4) *reinterpret_cast<unsigned*>(at + from) = *reinterpret_cast<const unsigned*>(src + from);
         if (n > 0) *reinterpret_cast<unsigned short*>(at + from) = *reinterpret_cast<const unsigned short*>(src + from);
     };
@@ -516,7 +515,11 @@ k_block_matmul(const __grid_constant__ CUtensorMap map_p, const __grid_constant_
             if (FUSED || p.swap) store_swapped<OT, S::kCols>(p, out, acc, row0 + lane, col0);
             else if constexpr (CG == 2 && NT == 256 && sizeof(OT) == 2) {
                 const unsigned at = (unsigned)reinterpret_cast<uintptr_t>(out) | (unsigned)(p.ldo * sizeof(OT));
-                unsigned char* const whole = out_rows + (quarter * 32 + lane) * kHalvesPitch;
+                // Rows lie in shared memory as they do in the output, within 16 bytes: by a distance that has the output's remainder.  It
+                // also keeps the lanes' stores, of as many bytes as that remainder allows, out of each other's banks.
+                const int over = (int)(p.ldo * sizeof(OT)) & 15, r = quarter * 32 + lane;
+                const OT* const first = out + (long long)(row0 - quarter * 32) * p.ldo + tq * NT;
+                unsigned char* const whole = out_rows + (reinterpret_cast<uintptr_t>(first) & 15u) + r * (512 + (over ? over : 16));
                 if ((at & 15) == 0) store_row_halves<16>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);
                 else if ((at & 7) == 0) store_row_halves<8>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);
                 else if ((at & 3) == 0) store_row_halves<4>(p, out, acc, whole, row0 + lane, tq * NT, group, 1 + quarter);

@@ -28,7 +28,7 @@ constexpr int kLpStream = 256;               // ... where it streams its part
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpVecs = 4;                   // vectors a thread takes at a time
 constexpr int kLpCtas = 8;                   // of a row, at most
-constexpr int kLpGroups = 160;               // whose maxima bound the alternatives, at most
+constexpr int kLpGroups = 128;               // whose maxima bound the alternatives, at most
 constexpr int kLpList = 512;                 // candidates that are ranked
 constexpr unsigned kKeyLowest = 0x007FFFFFu; // key of -infinity
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
@@ -334,10 +334,11 @@ __device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, 
 template <typename T, bool KEEP, bool GRAD>
 __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thread_max, int n, LpShared& s) {
     constexpr int kN = Logits8<T>::kN;
-    const int threads = blockDim.x;
-    const int per = threads > 320 ? 4 : threads > 160 ? 2 : 1, groups = threads / per;
+    const int threads = blockDim.x, enough = n <= 8 ? 32 : 64;          // groups: some n more logits than n reach the n-th largest of that many maxima
     unsigned key = order_key(thread_max), most = key;
-    for (int d = 1; d < per; d *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+    int per = 1;                                                        // threads of a group
+    for (; threads / (2 * per) >= enough; per *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, per));
+    const int groups = threads / per;
     if (threadIdx.x % per == 0) s.group[threadIdx.x / per] = most;
     if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
     if (threadIdx.x == 0) { s.count = 0; s.bound = kKeyLowest; }
@@ -345,25 +346,32 @@ __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thr
     if ((int)threadIdx.x < groups) {
         const unsigned k = s.group[threadIdx.x];
         int before = 0;
+#pragma unroll 8
         for (int j = 0; j < groups; ++j) { const unsigned o = s.group[j]; before += o > k || (o == k && j < (int)threadIdx.x); }
         if (before == n - 1) s.bound = k;
     }
     __syncthreads();
-    const unsigned bound = max(s.bound, kKeyLowest + 1);     // (-infinity is never listed)
-    if (key >= bound)
-        mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int v0) {
+    const unsigned bound = max(s.bound, kKeyLowest + 1);                // (-infinity is never listed)
+    auto collect = [&](const Logits8<T>& x, int v) {
+        if (order_key(x.largest()) < bound) return;
 #pragma unroll
-            for (int i = 0; i < kLpVecs; ++i) {
-                if (order_key(x[i].largest()) < bound) continue;
+        for (int j = 0; j < kN; ++j) {
+            const unsigned k = order_key(x.get(j));
+            if (k < bound) continue;
+            const unsigned at = atomicAdd(&s.count, 1u);
+            if (at < kLpList) s.list[at] = (u64)k << 32 | (unsigned)~(mine.row.first(v) + j);
+        }
+    };
+    if constexpr (KEEP) {
+        if (key >= bound)
+            mine.tiles([&](const Logits8<T> (&x)[kLpVecs], int v0) {
 #pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    const unsigned k = order_key(x[i].get(j));
-                    if (k < bound) continue;
-                    const unsigned at = atomicAdd(&s.count, 1u);
-                    if (at < kLpList) s.list[at] = (u64)k << 32 | (unsigned)~(mine.row.first(v0 + i * threads) + j);
-                }
-            }
-        });
+                for (int i = 0; i < kLpVecs; ++i) collect(x[i], v0 + i * threads);
+            });
+    } else {                                                            // a thread's vectors again, by its whole warp
+        for (unsigned left = __ballot_sync(0xFFFFFFFFu, key >= bound); left; left &= left - 1)
+            for (int v = mine.begin + (int)(threadIdx.x & ~31u) + __ffs(left) - 1 + lane_id() * threads; v < mine.end; v += 32 * threads) collect(mine.row.load(v), v);
+    }
     __syncthreads();
     const int count = (int)s.count;
     if (count <= kLpList) {
@@ -710,7 +718,7 @@ static LogprobShape logprob_shape(long long rows, long long vocab, int per_vecto
     const long long all = (vocab + 2 * per_vector - 2) / per_vector;     // whatever the row's place within 16 bytes
     LogprobShape L{1, 0, 0, 1};
     auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
-    while (L.ctas < kLpCtas && rows * L.ctas < 3 * sms && per() > 256) L.ctas *= 2;
+    while (L.ctas < kLpCtas && rows * L.ctas * 2 <= sms && per() > 256) L.ctas *= 2;
     const long long most = rows * L.ctas < 2 * sms && per() <= kLpVecs * kLpThreads ? kLpThreads : kLpStream;
     long long t = (per() + 1) / 2;                                       // two vectors a thread at least
     t = (t + 31) / 32 * 32;

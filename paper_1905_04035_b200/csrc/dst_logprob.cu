@@ -439,7 +439,7 @@ struct RowSums {
 };
 
 template <typename T, typename OT, bool KEEP, bool GRAD>
-__global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, KEEP ? 1 : 4) k_logprob(const __grid_constant__ LogprobParams p) {
+__global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRAD ? 2 : 1) k_logprob(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
     __shared__ LpShared s;
     cg::cluster_group cluster = cg::this_cluster();
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(N + 32, Ring<N>::kCtas) k_logprob_ring(const _
 // How a row is cut.  Many rows: a CTA of 256 threads each, four on an SM, which read them four vectors a thread at a time.  Fewer rows than fill
 // the device so: several CTAs a row, and as many threads as hold their part at four vectors each.
 struct LogprobShape { int ctas, threads, vectors, keep; };
-static LogprobShape logprob_shape(long long rows, long long vocab, int per_vector, int sms) {
+static LogprobShape logprob_shape(long long rows, long long vocab, int per_vector, bool grad, int sms) {
     const long long all = (vocab + 2 * per_vector - 2) / per_vector;     // whatever the row's place within 16 bytes
     LogprobShape L{1, 0, 0, 1};
     auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
@@ -724,7 +724,8 @@ static LogprobShape logprob_shape(long long rows, long long vocab, int per_vecto
     t = (t + 31) / 32 * 32;
     L.threads = int(t < most ? t : most);
     L.vectors = int(per());
-    L.keep = per() <= (long long)kLpVecs * L.threads;
+    // (kept in registers: for the gradient, or where rows are few; many rows without one do better with half the registers a thread)
+    L.keep = per() <= (long long)kLpVecs * L.threads && (grad || rows * L.ctas < 2 * sms);
     return L;
 }
 
@@ -742,7 +743,7 @@ static cudaError_t logprob_run(const LogprobParams& p, const LogprobShape& L, cu
 }
 template <typename T, typename OT, bool GRAD>
 static cudaError_t logprob_t(LogprobParams p, int sms, cudaStream_t stream) {
-    const LogprobShape L = logprob_shape(p.rows, p.vocab, Logits8<T>::kN, sms);
+    const LogprobShape L = logprob_shape(p.rows, p.vocab, Logits8<T>::kN, GRAD, sms);
     p.vectors = L.vectors;
     p.cut = L.ctas == 1 ? 0 : L.ctas == 2 ? 1 : L.ctas == 4 ? 2 : 3;
     return L.keep ? logprob_run<T, OT, true, GRAD>(p, L, stream) : logprob_run<T, OT, false, GRAD>(p, L, stream);

@@ -720,7 +720,8 @@ static LogprobShape logprob_shape(long long rows, long long vocab, int per_vecto
     auto per = [&] { return (all + L.ctas - 1) / L.ctas; };
     while (L.ctas < kLpCtas && rows * L.ctas * 2 <= sms && per() > 256) L.ctas *= 2;
     const long long most = rows * L.ctas < 2 * sms && per() <= kLpVecs * kLpThreads ? kLpThreads : kLpStream;
-    long long t = (per() + 1) / 2;                                       // two vectors a thread at least
+    const long long each = rows * L.ctas < 2 * sms ? 2 : grad ? kLpVecs : 2 * kLpVecs;   // vectors a thread, at least
+    long long t = (per() + each - 1) / each;
     t = (t + 31) / 32 * 32;
     L.threads = int(t < most ? t : most);
     L.vectors = int(per());

@@ -11,7 +11,7 @@
  * Conventions are those of dst.h and dst_tied.h: device pointers, caller-owned buffers, nothing allocated or
  * synchronised, all work on `stream`, bad arguments refused on the host before anything is enqueued.  A matrix argument
  * has a leading dimension in elements; its rows are contiguous.  Sizes of zero are valid and do nothing unless a comment
- * says otherwise.  Two calls with the same arguments give the same bits; the order of sums follows from the sizes and types, and
+ * says otherwise.  Calls that share a workspace or an output must be ordered, captured ones too.  Two calls with the same arguments give the same bits; the order of sums follows from the sizes and types, and
  * from how rows are aligned.
  */
 #ifndef DST_STEP_H_
@@ -24,7 +24,7 @@ extern "C" {
 #endif
 
 /*
- * Log probabilities under softmax(scale * x), x the logits of a row as fp32 and scale > 0 (1 / temperature):
+ * Log probabilities under softmax(scale * x), x the logits of a row as fp32 and scale (1 / temperature) above 0 and at most 2e38:
  *     z_i = scale * (x_i - max x),  S = sum exp(z_i),  log p_i = z_i - log S
  *   logprob [rows]        log p of the row's target; 0 for a row without one
  *   lse [rows]            scale * max x + log S (an infinity where that passes fp32's range)
@@ -69,7 +69,8 @@ int dst_logprob_backward(const void* logits, int64_t ld, int32_t type, int64_t r
 /*
  * Root-mean-square norm of the residual stream, d <= DST_RMSNORM_MAX_D:
  *     h = x + residual, rounded to sum_type (h = x where residual and sum_out are NULL)
- *     inv_rms = 1 / sqrt(mean(h^2) + eps),  y = h * inv_rms * weight
+ *     inv_rms = 1 / sqrt(mean(h^2) + eps),  y = h * inv_rms * weight        (sums in fp32: a row whose squares pass its range has
+ *     inv_rms 0)
  *   x [rows, d] in x_type; residual (optional) and sum_out (optional, receives h; may be residual, or x where types
  *   agree) in sum_type; weight [d] fp32 or NULL (ones); inv_rms [rows] fp32, optional, for the backward pass
  *   out [rows, d] in out_type and / or q, its 8-bit form (DST_FP8_ROW blocks, rounded once from fp32, as
@@ -117,7 +118,8 @@ int dst_grad_norm(const dst_tensor_t* tensors, int64_t count, double max_norm, f
 /*
  * outs[i] = clip[1] * tensors[i], rounded once to outs[i]'s type; the two lists have the same lengths.  A factor of 0
  * writes zeros whatever the elements are.  outs may be the same list: in place, where types agree, and a factor of 1
- * then touches nothing.  Otherwise no output may overlap a tensor.
+ * then touches nothing.  Otherwise no output may overlap a tensor, and none another output, in place either (a tensor that is
+ * listed twice would be scaled twice; in the norm it counts twice).
  */
 int dst_clip(const dst_tensor_t* tensors, const dst_tensor_t* outs, int64_t count, const float* clip, dst_stream_t stream);
 

@@ -30,7 +30,7 @@ static int logprob_params(LogprobParams& p, const void* logits, int64_t ld, int3
     if (misaligned(targets, index_type == DST_I64 ? 8 : 4) || (vocab == 0 && rows > 0)) return DST_ERR_INVALID_ARG;
     p.logits = logits; p.targets = targets; p.ld = ld; p.rows = rows; p.vocab = int(vocab); p.wide = index_type == DST_I64;
     p.scale = scale; p.scale2 = float(double(scale) * 1.4426950408889634);
-    return DST_OK;
+    return isfinite(p.scale2) ? DST_OK : DST_ERR_INVALID_ARG;
 }
 static int logprob_grad(LogprobParams& p, int32_t type, const float* dlogprob, const float* dentropy, void* dlogits, int64_t ldd, int32_t d_type) {
     if (!dtype_ok(d_type)) return DST_ERR_UNSUPPORTED;

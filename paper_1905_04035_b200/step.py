@@ -181,6 +181,8 @@ class TensorList:
             if not t.is_contiguous():
                 raise ValueError("tensors must be contiguous")
             c.data, c.n, c.type = t.data_ptr(), t.numel(), DST_F32 if t.dtype == torch.float32 else DST_BF16
+        places = [t.data_ptr() for t in self.tensors if t.numel()]
+        self.distinct = len(set(places)) == len(places)
 
     def __len__(self) -> int:
         return len(self.tensors)
@@ -218,4 +220,6 @@ def dst_clip(tensors: TensorList, clip: torch.Tensor, outs: Optional[TensorList]
     _on(outs, index)
     if len(outs) != len(tensors):
         raise ValueError("outs must have as many tensors")
+    if not outs.distinct:
+        raise ValueError("a tensor that is listed twice would be scaled twice")
     _enqueue("dst_clip", index, stream, tensors._c, outs._c, len(tensors), pc)

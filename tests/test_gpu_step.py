@@ -463,3 +463,57 @@ def test_norm_is_the_same_twice_and_a_factor_of_one_in_place_keeps_every_bit():
     kept = [t.clone() for t in tensors]
     dst.dst_clip(lists, clips[0])
     assert all(torch.equal(a, b) for a, b in zip(tensors, kept))
+
+
+# ---- many rows at once, which share a ring in shared memory ------------------------------------------------------
+@pytest.mark.parametrize("vocab,dtype", [(33708, "bf16"), (33708, "f32"), (9000, "bf16"), (70001, "bf16"), (30011, "f32")])
+def test_many_rows_give_the_same_bits_every_time(vocab, dtype):
+    rows = 700
+    x, targets, g = make_logits(rows, vocab, dtype, 8, pad=3)
+    a = torch.randn(rows, generator=g).cuda()
+    out = [torch.empty(rows, device="cuda") for _ in range(2)]
+    d = [torch.empty(rows, vocab, dtype=TYPES[dtype], device="cuda") for _ in range(2)]
+    dst.dst_logprob_loss(x, targets, a, out[0], d[0])
+    for _ in range(20):
+        d[1].zero_()
+        dst.dst_logprob_loss(x, targets, a, out[1], d[1])
+        assert torch.equal(*out) and torch.equal(*d)
+    some = torch.randint(0, rows, (12,), generator=g)
+    w = Want(x[some.cuda()], 1.0, dtype)
+    t, b = targets[some.cuda()].cpu().numpy(), np.zeros(12)
+    near(d[0][some.cuda()], o.logits_gradient(w.x, t, 1.0, np64(a[some.cuda()]), b), w.tol_grad(t, np64(a[some.cuda()]), b), dtype)
+    near_sums(w, targets[some.cuda()], out[0][some.cuda()], torch.from_numpy(w.lse).float(), torch.from_numpy(w.entropy).float())
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("vocab", [9000, 40000])
+@pytest.mark.parametrize("pad", [0, 5])
+def test_special_and_confident_rows_among_many(dtype, out, vocab, pad):
+    inf, nan, n = float("inf"), float("nan"), 12
+    x = torch.randn(n, vocab, generator=torch.Generator().manual_seed(1))
+    x[0] = -inf
+    x[1] = -inf
+    x[1, vocab - 1] = -4.0
+    x[2, 3] = nan
+    x[3, vocab // 2] = inf
+    x[4] = nan
+    x[5] = torch.finfo(TYPES[dtype]).min
+    x[6, ::2] = torch.finfo(TYPES[dtype]).min
+    x[7, 77] = 30.0                               # nearly all on one token
+    x[8, vocab - 1] = 60.0
+    x[9, 0] = 20.0
+    x[10] *= 100
+    x, targets = x.to(TYPES[dtype]), torch.tensor([0, vocab - 1, 0, 0, 0, 1, 1, 77, vocab - 1, 5, 2, -1])
+    w = Want(x.cuda(), 1.5, dtype)
+    many, _ = strided(n * 40, vocab, dtype, pad, 0, x.repeat(40, 1))
+    for b in (0.0, 0.5):
+        a, e = torch.linspace(-1, 1, n), torch.full((n,), b)
+        a[10] = 0.0
+        logprob, lse, entropy = (torch.empty(n * 40, device="cuda") for _ in range(3))
+        d, buf = strided(n * 40, vocab, out, pad, 0)
+        dst.dst_logprob_loss(many, targets.repeat(40).cuda(), a.repeat(40).cuda(), logprob, d, scale=1.5, dentropy=e.repeat(40).cuda(), lse=lse, entropy=entropy)
+        for part in (0, 17, 39):
+            at = slice(part * n, part * n + n)
+            near_sums(w, targets, logprob[at], lse[at], entropy[at])
+            near(d[at], o.logits_gradient(w.x, targets.numpy(), 1.5, np64(a), np64(e)), w.tol_grad(targets.numpy(), np64(a), np64(e)), out)
+        assert pad == 0 or untouched(buf, d)

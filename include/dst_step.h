@@ -38,7 +38,8 @@ extern "C" {
  * targets may be NULL where logprob is.
  * Logits of -infinity have probability zero and add nothing to the entropy.  A row of nothing but -infinity has lse and
  * logprob -infinity and entropy 0.  A row with a NaN or +infinity has NaN for all three and in top_logprob.
- * A log probability near zero is accurate relative to itself, not to one: what the largest logit leaves is summed apart.
+ * A log probability near zero is accurate relative to itself, not to one: what the largest logit leaves is summed apart
+ * (probabilities below 2^-126 count as zero).
  * rows > 0 with vocab = 0 is refused.
  */
 #define DST_LOGPROB_MAX_TOP 32

@@ -325,6 +325,7 @@ __device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, 
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
         const u64 k = list[i];
         int before = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) before += list[j] > k;
         if (k != 0 && before < n) out[before] = k;           // (0: an empty place)
     }

@@ -5,7 +5,8 @@ Tolerances, with u = 2^-24 (fp32 rounding) and h = 2^-8 (half a bf16 step, relat
              by 3u |z| and by the 2^-22 = 4u that its instruction allows.  A thread adds at most 64 of them to what it had, two chains (33u a tile),
              joins (lanes 5, warps 5, CTAs 5 additions, each join an exponential and its distance) add 3 (5 + 4 + 4)u.
              rho = (33 tiles + 60 + 3 E|z|) u bounds the relative error of r and of t, E|z| <= 2 log vocab.
-               log p: rho r / (1 + r) + 4u log1p(r) + 4u |z| (+ 4u |scale max| for lse)
+               log p: rho r / (1 + r) + 4u log1p(r) + 4u |z| (+ 4u |scale max| for lse), and vocab 2^-126: exponentials below
+               2^-126 are zero, as fp32 has no normal number there
                entropy: both terms are at most the entropy:  2 rho (H + r / (1 + r)) + 8u H
                gradient: p's own error (rho + 10u + 4u |z|) times what it multiplies, and that factor's error
              (lse is rounded to fp32, which is an infinity beyond its range)
@@ -75,7 +76,7 @@ class Want:
         vocab = x.shape[1]
         tiles = 1 if vocab <= 131072 else 8
         self.rho = (33 * tiles + 60 + 6 * np.log(max(vocab, 2))) * U
-        with np.errstate(invalid="ignore"):
+        with np.errstate(invalid="ignore", divide="ignore"):
             self.share = np.where(self.r >= 0, self.r / (1 + self.r), 0)
             self.log_total = np.where(self.r >= 0, np.log1p(np.maximum(self.r, 0)), 0)
             self.z = np.nan_to_num(scale * (self.x - self.x.max(-1, keepdims=True)), nan=0.0, neginf=0.0, posinf=0.0)
@@ -84,10 +85,11 @@ class Want:
         return np.nan_to_num(t, nan=0.0)
 
     def tol_log_p(self):
-        return (self.of(self.rho * self.share + 4 * U * self.log_total))[:, None] + 4 * U * np.abs(self.z)
+        return (self.of(self.rho * self.share + 4 * U * self.log_total))[:, None] + 4 * U * np.abs(self.z) + self.x.shape[1] * 2.0 ** -126
 
     def tol_entropy(self):
-        return self.of(2 * self.rho * (self.entropy + self.share) + 8 * U * self.entropy)
+        # (a term of the entropy is at most 90 times its exponential where that is below 2^-126 and the gap is what fp32 can hold of it)
+        return self.of(2 * self.rho * (self.entropy + self.share) + 8 * U * self.entropy) + self.x.shape[1] * 200 * 2.0 ** -126
 
     def tol_grad(self, targets, a, b):
         p = np.exp(np.nan_to_num(self.log_p, nan=0.0))
@@ -95,6 +97,7 @@ class Want:
         a, b = np.abs(np.where(targets >= 0, a, 0))[:, None], np.abs(b)[:, None]
         rel = self.rho + 10 * U + 4 * U * np.abs(self.z)
         t = p * (rel * (a + b * (np.abs(lp) + h)) + b * (self.tol_log_p() + self.tol_entropy()[:, None]))
+        t = t + 2.0 ** -126 * (a + b * (200 + h))              # exponentials below 2^-126 are zero; their logarithm is above -200 where that matters
         rows = np.flatnonzero(targets >= 0)
         at = targets[rows]
         # the target's own: (1 - p) to 4u of itself and to p's error through log p

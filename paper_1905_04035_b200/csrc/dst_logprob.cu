@@ -337,10 +337,11 @@ __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thr
     constexpr int kN = Logits8<T>::kN;
     const int threads = blockDim.x, enough = n <= 8 ? 32 : 64;          // groups: some n more logits than n reach the n-th largest of that many maxima
     unsigned key = order_key(thread_max), most = key;
-    int per = 1;                                                        // threads of a group
-    for (; threads / (2 * per) >= enough; per *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, per));
+    // threads of a group, as far apart in the warp as they can be: frequent tokens often lie together, and would all be one group's
+    int per = 1;
+    for (; threads / (2 * per) >= enough; per *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 16 / per));
     const int groups = threads / per;
-    if (threadIdx.x % per == 0) s.group[threadIdx.x / per] = most;
+    if (lane_id() < 32 / per) s.group[warp_id() * (32 / per) + lane_id()] = most;
     if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
     if (threadIdx.x == 0) { s.count = 0; s.bound = kKeyLowest; }
     __syncthreads();
@@ -369,9 +370,23 @@ __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thr
 #pragma unroll
                 for (int i = 0; i < kLpVecs; ++i) collect(x[i], v0 + i * threads);
             });
-    } else {                                                            // a thread's vectors again, by its whole warp
-        for (unsigned left = __ballot_sync(0xFFFFFFFFu, key >= bound); left; left &= left - 1)
-            for (int v = mine.begin + (int)(threadIdx.x & ~31u) + __ffs(left) - 1 + lane_id() * threads; v < mine.end; v += 32 * threads) collect(mine.row.load(v), v);
+    } else {
+        // a thread's vectors again, by its whole warp, and those of four threads at a time
+        for (unsigned left = __ballot_sync(0xFFFFFFFFu, key >= bound); left;) {
+            int first[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                first[i] = left ? mine.begin + (int)(threadIdx.x & ~31u) + __ffs(left) - 1 + lane_id() * threads : mine.end;
+                left &= left - 1;
+            }
+            for (int at = 0; at < mine.end - mine.begin; at += 32 * threads) {
+                Logits8<T> x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (first[i] + at < mine.end) x[i] = mine.row.load(first[i] + at); else x[i] = Logits8<T>::nothing();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) collect(x[i], first[i] + at);
+            }
+        }
     }
     __syncthreads();
     const int count = (int)s.count;

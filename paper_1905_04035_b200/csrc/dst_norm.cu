@@ -11,6 +11,7 @@
 
 namespace dst {
 
+constexpr int kNormOnSm = 2;                 // CTAs of the forward kernel that fit an SM, up to 4096 columns
 constexpr int kNormWarps = 8;                // of a CTA, at most where a team has fewer
 
 // How a lane's elements lie in a row.  8 and 4: in vectors of so many, aligned to them; 0: a column a lane, in any place.
@@ -166,7 +167,7 @@ __device__ __forceinline__ void store_fp8(const Fp8View& q, long long row, const
 }
 
 template <typename XT, typename ST, int MODE, int PER>
-__global__ void __launch_bounds__(PER == 16 ? 256 : 512) k_rmsnorm(const __grid_constant__ NormParams p, int team, int out_type) {
+__global__ void __launch_bounds__(PER == 16 ? 256 : 512, PER == 16 ? kNormOnSm : 1) k_rmsnorm(const __grid_constant__ NormParams p, int team, int out_type) {
     __shared__ float parts[2][16];
     const int teams = blockDim.x / 32 / team;
     const Place<MODE, PER> at(warp_id() % team, p.d);
@@ -334,7 +335,7 @@ template <typename... M> static int least(int a, M... more) {
 
 template <typename XT, typename ST, int MODE>
 static cudaError_t norm_m(const NormParams& p, int out_type, cudaStream_t stream) {
-    const NormShape s = norm_shape(p.rows, p.d, 3 * kSmCount);
+    const NormShape s = norm_shape(p.rows, p.d, kNormOnSm * kSmCount);
     const dim3 grid((unsigned)s.ctas), block(s.warps * 32);
     return s.per == 16 ? launch_pdl(k_rmsnorm<XT, ST, MODE, 16>, grid, block, 0, stream, p, s.team, out_type)
                        : launch_pdl(k_rmsnorm<XT, ST, MODE, 32>, grid, block, 0, stream, p, s.team, out_type);

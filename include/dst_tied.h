@@ -141,7 +141,7 @@ int dst_quantize_fp4(const void* x, int64_t ldx, int32_t x_type, int64_t rows, i
 /*
  * out = a b^T and out = quantised(x) w^T as dst_matmul_fp8 and dst_linear_fp8 have them, their workspaces likewise.  Sums are
  * fp32 in an order fixed by the shapes and out_type; an fp32 result leaves the tensor cores every 1024 columns.  The 8-bit
- * and the 4-bit form of a matrix do not mix.  dst_linear_fp4 takes up to 20 blocks of 256 elements, of up to 2048
+ * and the 4-bit form of a matrix do not mix.  dst_linear_fp4 takes up to 12 blocks of 256 elements, of up to 2048
  * columns, in one kernel.
  */
 size_t dst_matmul_fp4_workspace_bytes(int64_t M, int64_t N, int64_t K);

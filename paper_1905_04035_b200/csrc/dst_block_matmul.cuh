@@ -22,9 +22,11 @@ namespace dst {
 // cores take 512 cycles.  One side of at most 128 rows: that side is Q, padded to 16, 32, 64 or 128 rows, and a CTA has
 // 128 rows of the other one; the time is that side's bytes.
 //
-// Measured: 8192 x 33,708 x 1024 to bf16 263 us (2150 TFLOP/s; stores and the drain of a tile's sums between its eight
-// blocks and the next tile's), 8111 x 1024 x 33,708 251 us, 33,708 x 1024 x 8111 to fp32 284 us (the last of 7.1 rounds of
-// tiles, and sums moved to registers); one row by 33,708 x 1024 7.9 us, where the weight's 34.5 MB need 5.3.
+// Measured, 8 bits: 8192 x 33,708 x 1024 to bf16 238 to 250 us (2380 to 2260 TFLOP/s; stores and the drain of a tile's sums between its
+// eight blocks and the next tile's), 8192^3 392 to 407 us, 33,708 x 1024 x 8111 to fp32 280 to 290 us (the last of 7.1 rounds of
+// tiles, and sums moved to registers); one row by 33,708 x 1024 7.5 us, where the weight's 34.5 MB need 5.3.
+// 4 bits: 8192^3 182 us (6040 TFLOP/s), 4096 x 33,708 x 1024 to bf16 79 us (52 without its stores, which alone would take 39: both go
+// through shared memory), to fp32 133 us; one row by 33,708 x 1024 4.9 us, where 18.3 MB need 2.8.
 //
 // Warps of a CTA: the epilogue warps (4, or 8 where a warp would otherwise hold more than 128 columns), one that issues
 // the copies and one that issues the matrix instructions.  Every wait has a limit; a CTA in which one ran out leaves

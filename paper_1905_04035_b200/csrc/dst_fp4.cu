@@ -74,10 +74,13 @@ cudaError_t launch_matmul_fp4(const Fp8View& a, const Fp8View& b, void* out, lon
     return launch_block_matmul<Fp4Kind>(a, b, out, ldo, out_type, workspace, sms, stream);
 }
 
-// A few rows of x are quantised by every CTA for itself while the weight's first tiles are on their way.
+// A few rows of x are quantised by every CTA for itself while the weight's first tiles are on their way: up to 12 blocks of 256, where the
+// two forms cost the same (in one kernel and in two, 33,708 x 1024: 1 row 5.8 and 6.7 us, 3 rows 6.4 and 6.8, 4 rows 7.2 and 6.7, 8 rows 9.5
+// and 7.0; x 512: 1 row 4.3 and 4.7, 6 rows 5.3 and 4.7; x 64: 1 row 4.2 and 4.7, 10 rows 5.4 and 5.7, 16 rows 6.3 and 5.7; x 2048: 1 row 8.5 and
+// 9.7; 1000 x 1024: 1 row 4.1 and 4.2, 3 rows 4.8 and 4.2).
 bool linear_fp4_fused(long long M, long long N, long long K) {
     const MatmulPlan L = plan_matmul<Fp4Kind>(M, N, K);
-    return block_linear_fits<Fp4Kind>(L) && M * L.blocks <= 20;
+    return block_linear_fits<Fp4Kind>(L) && M * L.blocks <= 12;
 }
 cudaError_t launch_linear_fp4_fused(const void* x, long long ldx, int x_type, long long M, const Fp8View& w, void* out, long long ldo, int out_type,
                                     int sms, cudaStream_t stream) {

@@ -6,12 +6,17 @@
 // difference; a thread's logits, the lanes of a warp, the warps of a CTA and the CTAs of a row join in that way, and each
 // is read once.  Then log p = z - log1p(r) and the entropy is log1p(r) - t / (1 + r): a sum of two terms of one sign.
 //
-// A row belongs to a cluster of 1, 2, 4 or 8 CTAs, joined through distributed shared memory.  Where a CTA's part fits into its
-// threads' registers (eight vectors of 16 bytes each) it stays there for the gradient and the alternatives.
+// A row belongs to a cluster of 1, 2, 4 or 8 CTAs, joined through distributed shared memory, that stream their parts or, where a part is four vectors of
+// 16 bytes a thread, keep it in registers for the gradient and the alternatives (k_logprob); for the gradient of many long rows a CTA keeps a whole
+// row in shared memory (k_logprob_ring).
 //
-// Alternatives: the n-th largest of the maxima of some hundred groups of logits is a bound that n logits reach at least and
+// Alternatives: the n-th largest of the maxima of 32 to 128 groups of logits is a bound that n logits reach at least and
 // few more than n do; those are collected and ranked by counting.  Where too many reach it (equal logits), n
 // rounds look for the next largest instead.
+//
+// Measured: forward 8111 x 33,708 fp32 158 us (6920 GB/s: the rate of reading), 4096 x 33,708 bf16 56 us (4960 GB/s; the exponential unit is 63 % busy,
+// the issue slots 64 %), 512 x 65,536 bf16 16.5 us and 24 with five alternatives, one row of 33,708 fp32 3.9 us and 8.1 with twenty; loss and gradient of
+// 4096 x 33,708 bf16 120 us (4600 GB/s; two exponentials a logit), of 8111 x 33,708 fp32 400 us (5470 GB/s); the gradient alone 99 us (5580) and 348 (6290).
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -727,8 +732,10 @@ __global__ void __launch_bounds__(N + 32, Ring<N>::kCtas) k_logprob_ring(const _
     }
 }
 
-// How a row is cut.  Many rows: a CTA of 256 threads each, four on an SM, which read them four vectors a thread at a time.  Fewer rows than fill
-// the device so: several CTAs a row, and as many threads as hold their part at four vectors each.
+// How a row is cut.  Many rows: a CTA of 256 threads each (fewer for short rows: eight vectors a thread at least, 2000 x 5000 bf16 9.4 us against 12.8 with
+// two), four on an SM, which read them four vectors a thread at a time.  Where two CTAs a row still do not pass the SMs, two to eight, each with
+// as many threads as hold its part at two to four vectors (48 x 33,708 bf16 4.9 us with two, 8.2 with eight; 150 rows 6.6 with one, 10.2 with two, 20 with four: clusters
+// of CTAs that fill the device wait for one another's places).
 struct LogprobShape { int ctas, threads, vectors, keep; };
 static LogprobShape logprob_shape(long long rows, long long vocab, int per_vector, bool grad, int sms) {
     const long long all = (vocab + 2 * per_vector - 2) / per_vector;     // whatever the row's place within 16 bytes
@@ -769,7 +776,6 @@ cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream
     return type == DST_F32 ? logprob_t<float, float, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false>(p, sms, stream);
 }
 
-// Enough rows for every SM, longer than what a few warps hold, and short enough for the ring's threads.
 template <typename T, typename OT, int N>
 static cudaError_t ring_run(const LogprobParams& p, int sms, cudaStream_t stream) {
     using S = Ring<N>;
@@ -783,7 +789,11 @@ template <typename T, typename OT>
 static cudaError_t loss_t(const LogprobParams& p, int sms, cudaStream_t stream) {
     constexpr int kTwo = 384, kOne = 480;
     const long long vectors = (p.vocab + 2 * Logits8<T>::kN - 2) / Logits8<T>::kN;
-    if (p.rows >= 2 * sms && vectors > 1024) {
+    // More than half as many rows as SMs, fewer of which are cut, and rows longer than four vectors for each of 256 threads, which keep them in
+    // registers (ring and not, bf16: 100 x 33,708 9.7 and 13.8 us, 600 x 33,708 23.5 and 31.6, 2400 x 33,708 74 and 92, 2400 x 65,536 149 and 153, 2400 x 9000 35.3 and
+    // 36.4, 1200 x 5000 16.3 and 11.0; fp32: 100 x 33,708 9.3 and 19.8, 2400 x 33,708 119 and 154, 1200 x 5000 15.7 and 17.3).  Rows that leave the ring no room for two
+    // chunks more are streamed and read again from L2.
+    if (2 * p.rows > sms && vectors > 1024) {
         if (vectors <= (Ring<kTwo>::kSlots - 2) * Ring<kTwo>::kChunk) return ring_run<T, OT, kTwo>(p, sms, stream);
         if (vectors <= (Ring<kOne>::kSlots - 2) * Ring<kOne>::kChunk) return ring_run<T, OT, kOne>(p, sms, stream);
     }

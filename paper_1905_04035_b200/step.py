@@ -163,12 +163,19 @@ def dst_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[tor
     return dx
 
 
+def _apart(spans) -> bool:
+    """Whether no two of the (first byte, byte after the last) overlap."""
+    spans = sorted(s for s in spans if s[0] < s[1])
+    return all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+
+
 class TensorList:
-    """A list of contiguous tensors of one CUDA device, fp32 or bf16, laid out for ``dst_grad_norm`` and ``dst_clip``.  It keeps the tensors
-    alive; their values are read when a call runs."""
+    """A list of contiguous tensors of one CUDA device, fp32 or bf16, laid out for ``dst_grad_norm`` and ``dst_clip``.  It keeps the memory
+    alive that the tensors have when the list is made (a tensor that is given other memory later is to be listed anew); the values are read
+    when a call runs."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
-        self.tensors = list(tensors)
+        self.tensors = [t.detach() for t in tensors]
         self.device_index: Optional[int] = None
         self._c = (_Tensor * max(1, len(self.tensors)))()
         for t, c in zip(self.tensors, self._c):
@@ -181,8 +188,7 @@ class TensorList:
             if not t.is_contiguous():
                 raise ValueError("tensors must be contiguous")
             c.data, c.n, c.type = t.data_ptr(), t.numel(), DST_F32 if t.dtype == torch.float32 else DST_BF16
-        places = [t.data_ptr() for t in self.tensors if t.numel()]
-        self.distinct = len(set(places)) == len(places)
+        self.distinct = _apart((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.tensors)
 
     def __len__(self) -> int:
         return len(self.tensors)
@@ -221,5 +227,5 @@ def dst_clip(tensors: TensorList, clip: torch.Tensor, outs: Optional[TensorList]
     if len(outs) != len(tensors):
         raise ValueError("outs must have as many tensors")
     if not outs.distinct:
-        raise ValueError("a tensor that is listed twice would be scaled twice")
+        raise ValueError("tensors that share memory would be scaled twice")
     _enqueue("dst_clip", index, stream, tensors._c, outs._c, len(tensors), pc)

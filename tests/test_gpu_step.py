@@ -520,3 +520,67 @@ def test_special_and_confident_rows_among_many(dtype, out, vocab, pad):
             near_sums(w, targets, logprob[at], lse[at], entropy[at])
             near(d[at], o.logits_gradient(w.x, targets.numpy(), 1.5, np64(a), np64(e)), w.tol_grad(targets.numpy(), np64(a), np64(e)), out)
         assert pad == 0 or untouched(buf, d)
+
+
+def test_lists_keep_their_memory_and_refuse_shared_outputs():
+    x = torch.arange(20.0, device="cuda")
+    clip = torch.tensor([1.0, 0.5], device="cuda")
+    for shared in ([x, x], [x[:11], x[10:]], [x, x[3:4]]):
+        with pytest.raises(ValueError):
+            dst.dst_clip(dst.TensorList(shared), clip)
+    dst.dst_clip(dst.TensorList([x[:10], x[10:], x[:0]]), clip)   # side by side
+    assert torch.equal(x.cpu(), torch.arange(20.0) * 0.5)
+    t = torch.ones(1000, device="cuda")
+    lists, seen = dst.TensorList([t]), t.detach()
+    t.data = torch.zeros(5, device="cuda")                        # other memory: the list has what it was made of
+    dst.dst_clip(lists, clip)
+    assert bool((seen == 0.5).all()) and bool((t == 0).all()) and lists.tensors[0].data_ptr() == seen.data_ptr()
+
+
+# ---- row counts and lengths on both sides of the rules by which a variant is chosen ------------------------------
+@pytest.mark.parametrize("rows", [74, 75, 148, 149, 297])
+@pytest.mark.parametrize("dtype,out,vocab", [("f32", "f32", 5003), ("bf16", "bf16", 9000), ("bf16", "f32", 33708), ("f32", "bf16", 27000)])
+def test_logits_gradient_by_rows(rows, dtype, out, vocab):
+    x, targets, g = make_logits(rows, vocab, dtype, rows, 5, 1, masked=True)
+    targets[3], targets[rows - 1] = -1, vocab + 7
+    a, b = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    a[5] = b[5] = 0.0
+    check_gradient(x, targets, a, b, 1.1, out, 5, 1)
+    if dtype == out:
+        check_gradient(x, targets, a, b * 0, 1.0, out, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("per_lane", [0, 1])
+def test_logits_gradient_where_the_ring_ends(dtype, per_lane):
+    """Rows as long as four vectors a thread, and as the ring holds with two CTAs an SM and with one, and one vector more."""
+    n = 4 if dtype == "f32" else 8
+    for vectors in (1024, (9 - 2) * 768, (14 - 2) * 960):
+        vocab = (vectors + per_lane) * n - n + 1                  # (whose vectors are counted for the worst place within 16 bytes)
+        x, targets, g = make_logits(80, vocab, dtype, vocab, 3, 1)
+        check_gradient(x, targets, torch.randn(80, generator=g), torch.randn(80, generator=g), 1.0, dtype, 3, 1)
+
+
+@pytest.mark.parametrize("rows,d", [(3, 4097), (5, 6002), (400, 8192), (2, 8191), (300, 8193), (310, 4096)])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,skew", [(0, 0), (4, 4), (3, 1)])
+def test_rmsnorm_of_wide_rows(rows, d, t, pad, skew):
+    check_norm(rows, d, t, t, t, True, pad, skew, seed=d)
+    check_norm_gradient(rows, d, t, t, t, pad, skew, seed=rows)
+
+
+@pytest.mark.parametrize("d", [40, 128, 300, 1000])
+def test_a_norm_in_8_bits_goes_into_the_product_whatever_its_buffers_held(d):
+    g = torch.Generator().manual_seed(d)
+    x, w = torch.randn(21, d, generator=g).cuda(), dst.Fp8Matrix(50, d, dst.DST_FP8_SQUARE)
+    dst.dst_quantize_fp8(torch.randn(50, d, generator=g).cuda(), w)
+    ws = torch.empty(max(256, dst.dst_matmul_fp8_workspace_bytes(21, 50, d)), dtype=torch.uint8, device="cuda")
+    outs = []
+    for held in (0, 255):
+        q = dst.Fp8Matrix(21, d)
+        q.q.view(torch.uint8).fill_(held)
+        q.scale.fill_(held)
+        dst.dst_rmsnorm(x, None, q=q)
+        outs.append(torch.empty(21, 50, device="cuda"))
+        dst.dst_matmul_fp8(q, w, outs[-1], ws)
+    assert torch.equal(*outs) and bool(torch.isfinite(outs[0]).all())

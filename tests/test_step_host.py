@@ -157,3 +157,10 @@ def test_binding_refuses_tensors_off_the_gpu_and_of_other_types_and_shapes():
         with pytest.raises(ValueError):
             step._stats(bad, 4, CPU)
     assert step._stats(None, 4, CPU) is None and step._stats(torch.zeros(4, 2), 4, CPU)
+
+
+def test_lists_know_whether_their_tensors_share_memory():
+    assert step._apart([]) and step._apart([(4, 8)]) and step._apart([(8, 12), (0, 4), (4, 8)])
+    assert step._apart([(4, 4), (0, 8), (2, 2)])                  # (what is empty shares nothing)
+    for bad in ([(0, 4), (0, 4)], [(8, 12), (0, 9)], [(0, 100), (8, 12), (200, 300)], [(0, 8), (7, 8)]):
+        assert not step._apart(bad), bad

@@ -11,6 +11,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdst_b200.so")
 _lib = None
+_calls = None
 
 DST_STATUS = {
     0: "DST_OK", 1: "DST_ERR_INVALID_ARG", 2: "DST_ERR_UNSUPPORTED", 3: "DST_ERR_WORKSPACE_TOO_SMALL",
@@ -178,6 +179,19 @@ def load_library():
             fn.restype, fn.argtypes = res, args
         _lib = lib
     return _lib
+
+
+def load_calls():
+    """Load the Python module of the library's entries, for calls that are short; raises if it has not been built."""
+    global _calls
+    if _calls is None:
+        load_library()
+        try:
+            from . import _calls as calls
+        except ImportError as e:
+            raise ImportError("%s: build it with `python -m paper_1905_04035_b200.build`" % e)
+        _calls = calls
+    return _calls
 
 
 def _index_type(t: torch.dtype) -> int:

@@ -4,12 +4,15 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libdst_b200.so")
+CALLS_PATH = os.path.join(HERE, "_calls.so")         # the entries as a Python module
+CALLS_SOURCE = os.path.join(CSRC, "dst_python.cpp")
 SOURCES = ["dst_api.cu", "dst_index_kernels.cu", "dst_front_cluster.cu", "dst_reduce_kernels.cu",
            "dst_accumulate_kernels.cu", "dst_dropout.cu", "dst_fp8.cu", "dst_fp4.cu", "dst_sample.cu", "dst_tied_api.cu",
            "dst_logprob.cu", "dst_norm.cu", "dst_clip.cu", "dst_step_api.cu"]
@@ -27,15 +30,27 @@ def _nvcc() -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+    if not (os.path.exists(LIB_PATH) and os.path.exists(CALLS_PATH)):
         return True
-    t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALLS_PATH))
+    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS + [CALLS_SOURCE]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def _calls_commands(obj: str, out: str):
+    """The compiler's command for the Python module, and the linker's."""
+    import torch
+
+    base = os.path.join(os.path.dirname(torch.__file__), "include")
+    include = [INCLUDE, sysconfig.get_paths()["include"], base, os.path.join(base, "torch", "csrc", "api", "include"), "/usr/local/cuda/include"]
+    flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi()]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return (["g++"] + flags + [a for i in include for a in ("-I", i)] + ["-c", CALLS_SOURCE, "-o", obj],
+            ["g++", "-shared", "-o", out, obj, "-L" + HERE, "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN", "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"])
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu file and link ``libdst_b200.so`` next to this file."""
+    """Compile every .cu file, link ``libdst_b200.so`` next to this file, and the Python module of its entries."""
     if not force and not is_stale():
         return LIB_PATH
     objdir = os.path.join(HERE, "_build")
@@ -48,15 +63,20 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, s), "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
+    tag = ".tmp.%d" % os.getpid()
+    compile_calls, link_calls = _calls_commands(os.path.join(objdir, "dst_python.o"), CALLS_PATH + tag)
+    procs.append((compile_calls, subprocess.Popen(compile_calls, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, p in procs:
         out, _ = p.communicate()
         if verbose or p.returncode != 0:
             sys.stderr.write(out)
         if p.returncode != 0:
-            raise RuntimeError("nvcc failed: %s" % " ".join(cmd))
-    tmp = LIB_PATH + ".tmp.%d" % os.getpid()
+            raise RuntimeError("compilation failed: %s" % " ".join(cmd))
+    tmp = LIB_PATH + tag
     subprocess.check_call([nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-ldl"])
     os.replace(tmp, LIB_PATH)
+    subprocess.check_call(link_calls)
+    os.replace(CALLS_PATH + tag, CALLS_PATH)
     return LIB_PATH
 
 

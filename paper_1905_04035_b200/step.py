@@ -1,4 +1,4 @@
-"""ctypes marshalling for the operators of a step around the tied weight (see ``include/dst_step.h`` for the contract):
+"""Marshalling for the operators of a step around the tied weight (see ``include/dst_step.h`` for the contract):
 log probabilities and their gradient, the root-mean-square norm, the gradient norm and clipping.
 
 The functions carry the names of the C entry points.  Matrices are 2-D CUDA tensors with contiguous rows (any distance

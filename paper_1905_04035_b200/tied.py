@@ -1,4 +1,4 @@
-"""ctypes marshalling for the operators around the tied weight (see ``include/dst_tied.h`` for the contract).
+"""Marshalling for the operators around the tied weight (see ``include/dst_tied.h`` for the contract).
 
 The functions carry the names of the C entry points; ``Fp8Matrix`` and ``TiedProjection`` own caller-side buffers.
 Matrices are 2-D CUDA tensors with contiguous rows (any distance between rows); outputs are allocated by the caller.
@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _Fp4, _Fp8, load_library
+from .binding import DST_BF16, DST_F32, DST_I32, DST_I64, DstError, _Dropout, _Fp4, _Fp8, load_calls, load_library
 
 DST_FP8_ROW, DST_FP8_SQUARE = 0, 1
 _TYPES = {torch.float32: DST_F32, torch.bfloat16: DST_BF16}
@@ -21,35 +21,17 @@ _INDEX = {torch.int32: DST_I32, torch.int64: DST_I64}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-_current_device = torch.cuda.current_device
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # (a tensor is on a device already)
 
 
 def _matrix(t: torch.Tensor, rows: int, cols: int, index: int, name: str):
     """(pointer, leading dimension, type) of a [rows, cols] matrix with contiguous rows on CUDA device `index`."""
-    kind = _TYPES.get(t.dtype)
-    if kind is None:
-        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
-    if t.shape != (rows, cols):
-        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
-    if t.get_device() != index:
-        raise ValueError("all tensors must live on the same device")
-    ld, step = t.stride()
-    if step != 1 and cols > 1 or ld < cols:                 # (the stride of a single column means nothing)
-        if rows > 1 or step != 1 and cols > 1:
-            raise ValueError("%s must have contiguous rows that do not overlap" % name)
-        ld = cols
-    return t.data_ptr(), ld, kind
+    return load_calls().matrix(t, rows, cols, index, name)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, index: int, name: str):
-    if t is None:
-        return None
-    if t.dtype != dtype:
-        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s must be contiguous [%d]" % (name, n))
-    _here(t, index)
-    return t.data_ptr()
+    """The pointer of n contiguous elements, or None."""
+    return None if t is None else load_calls().vector(t, n, dtype, index, name)
 
 
 def _device(t: torch.Tensor) -> int:
@@ -66,7 +48,7 @@ def _here(t: torch.Tensor, index: int) -> None:
 
 def _enqueue(name: str, index: int, stream, *args) -> None:
     """Call a C entry whose last argument is the stream, with device `index` current; raises on a status."""
-    fn = getattr(load_library(), name)
+    fn = getattr(load_calls(), name)
     if _current_device() == index:
         rc = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:

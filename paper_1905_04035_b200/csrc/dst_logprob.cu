@@ -10,12 +10,12 @@
 // 16 bytes a thread, keep it in registers for the gradient and the alternatives (k_logprob); for the gradient of many long rows a CTA keeps a whole
 // row in shared memory (k_logprob_ring).
 //
-// Alternatives: the n-th largest of the maxima of 32 to 128 groups of logits is a bound that n logits reach at least and
-// few more than n do; those are collected and ranked by counting.  Where too many reach it (equal logits), n
+// Alternatives: the n-th largest of the maxima of 32 or 64 groups of logits is a bound that n logits reach at least and
+// few more than n do; those are collected and ranked by counting, and the CTAs of a row place their own n among all.  Where too many reach it (equal logits), n
 // rounds look for the next largest instead.
 //
-// Measured: forward 8111 x 33,708 fp32 158 us (6920 GB/s: the rate of reading), 4096 x 33,708 bf16 56 us (4960 GB/s; the exponential unit is 63 % busy,
-// the issue slots 64 %), 512 x 65,536 bf16 16.5 us and 24 with five alternatives, one row of 33,708 fp32 3.9 us and 8.1 with twenty; loss and gradient of
+// Measured: forward 8111 x 33,708 fp32 162 us (6750 GB/s: the rate of reading), 4096 x 33,708 bf16 52 us (5270 GB/s; the exponential unit is 63 % busy,
+// the issue slots 64 %), 512 x 65,536 bf16 16 us and 19.4 with five alternatives, one row of 33,708 fp32 3.7 us and 6.6 with twenty; loss and gradient of
 // 4096 x 33,708 bf16 120 us (4600 GB/s; two exponentials a logit), of 8111 x 33,708 fp32 400 us (5470 GB/s); the gradient alone 99 us (5580) and 348 (6290).
 #include <cooperative_groups.h>
 
@@ -33,7 +33,6 @@ constexpr int kLpStream = 256;               // ... where it streams its part
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpVecs = 4;                   // vectors a thread takes at a time
 constexpr int kLpCtas = 8;                   // of a row, at most
-constexpr int kLpGroups = 128;               // whose maxima bound the alternatives, at most
 constexpr int kLpList = 512;                 // candidates that are ranked
 constexpr unsigned kKeyLowest = 0x007FFFFFu; // key of -infinity
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
@@ -162,14 +161,18 @@ __device__ __forceinline__ Part join_lanes(Part p, float scale2, int& owner) {
     return Part{top, r, t};
 }
 
-struct LpShared {
+struct LpSums {
     Part warp[kLpWarps], cta;                // `cta`: read by the other CTAs of the row
-    unsigned group[kLpGroups];
+};
+struct LpTop {                               // for the alternatives
+    uint2 group[32];
+    unsigned threads[kLpThreads];            // their maxima
     unsigned bound, count;
     u64 round[kLpWarps];
     u64 list[kLpList];
     u64 top[DST_LOGPROB_MAX_TOP];            // the CTA's alternatives: key, then the index' complement (a larger number comes first)
 };
+struct LpNoTop {};
 
 // The gradient by a row's logits: scale (dlogprob ([here the target] - p) - dentropy p (log p + H)).
 struct RowGrad {
@@ -221,6 +224,13 @@ struct RowGrad {
     }
 };
 
+// 16 bytes that are read once and that nothing writes meanwhile (volatile: it stays behind the wait for the kernel before)
+__device__ __forceinline__ uint4 read_once(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 // A CTA's part of a row.  KEEP: four vectors a thread, that stay in registers.
 template <typename T, bool KEEP, bool GRAD> struct RowPart {
     static constexpr int kN = Logits8<T>::kN;
@@ -229,11 +239,14 @@ template <typename T, bool KEEP, bool GRAD> struct RowPart {
     Logits8<T> kept[KEEP ? kLpVecs : 1];
     __device__ __forceinline__ RowPart(const T* r, int vocab, int b, int e) : row(r, vocab), begin(b), end(e) {}
     __device__ __forceinline__ void fetch(Logits8<T> (&x)[kLpVecs], int v0) const {
-        const int step = blockDim.x, last = v0 + (kLpVecs - 1) * step;
-        if (row.first(v0) >= 0 && last < end && row.first(last) + kN <= row.vocab) {
-            const T* const from = row.row + row.first(v0);
+        const int step = blockDim.x;
+        if (v0 >= (row.skew != 0) && v0 + (kLpVecs - 1) * step < min(end, (row.vocab + row.skew) / kN)) {   // all wholly in the row
+            const uint4* const from = reinterpret_cast<const uint4*>(row.row - row.skew) + v0;
 #pragma unroll
-            for (int i = 0; i < kLpVecs; ++i) x[i].v = *reinterpret_cast<const uint4*>(from + i * step * kN);
+            for (int i = 0; i < kLpVecs; ++i) {
+                if constexpr (GRAD) x[i].v = from[i * step];
+                else x[i].v = read_once(from + i * step);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kLpVecs; ++i) if (v0 + i * step < end) x[i] = row.load(v0 + i * step); else x[i] = Logits8<T>::nothing();
@@ -326,37 +339,51 @@ __device__ __forceinline__ float others_of(int n, float top, float scale2, F vec
     return s + (float)((int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)ties) - 1);
 }
 
-__device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, int n) {
-    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+__device__ __forceinline__ void rank_into(const u64* list, int count, u64* out, int n, int threads) {
+    for (int i = threadIdx.x; i < count; i += threads) {
         const u64 k = list[i];
         int before = 0;
 #pragma unroll 8
         for (int j = 0; j < count; ++j) before += list[j] > k;
-        if (k != 0 && before < n) out[before] = k;           // (0: an empty place)
+        if (before < n) out[before] = k;
     }
 }
 
-// The CTA's n largest logits into s.top (0: none left).
-template <typename T, bool KEEP, bool GRAD>
-__device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thread_max, int n, LpShared& s) {
-    constexpr int kN = Logits8<T>::kN;
-    const int threads = blockDim.x, enough = n <= 8 ? 32 : 64;          // groups: some n more logits than n reach the n-th largest of that many maxima
-    unsigned key = order_key(thread_max), most = key;
-    // threads of a group, as far apart in the warp as they can be: frequent tokens often lie together, and would all be one group's
-    int per = 1;
-    for (; threads / (2 * per) >= enough; per *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 16 / per));
-    const int groups = threads / per;
-    if (lane_id() < 32 / per) s.group[warp_id() * (32 / per) + lane_id()] = most;
+// What comes before find_top, around the barrier that the row's sums need too: a bound that n logits reach at least, and few more than n.  It
+// is the n-th largest of the maxima of 32 groups (64 for more than eight): the threads with one lane number, since frequent
+// tokens often lie together and would all be one group's otherwise.  By the second warp: the first joins the row's sums meanwhile.
+__device__ __forceinline__ void post_maximum(float thread_max, LpTop& s) {
+    s.threads[threadIdx.x] = order_key(thread_max);
     if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
-    if (threadIdx.x == 0) { s.count = 0; s.bound = kKeyLowest; }
-    __syncthreads();
-    if ((int)threadIdx.x < groups) {
-        const unsigned k = s.group[threadIdx.x];
-        int before = 0;
-#pragma unroll 8
-        for (int j = 0; j < groups; ++j) { const unsigned o = s.group[j]; before += o > k || (o == k && j < (int)threadIdx.x); }
-        if (before == n - 1) s.bound = k;
+    if (threadIdx.x == 0) s.count = 0;
+}
+__device__ __forceinline__ void find_bound(int n, LpTop& s) {
+    const int warps = blockDim.x / 32, halves = n > 8 && warps > 1 ? 2 : 1;
+    if (warp_id() != (warps > 1 ? 1 : 0)) return;
+    uint2 k = make_uint2(0u, 0u);                                       // (below every key)
+    for (int w = 0; w < warps; w += halves) {
+        k.x = max(k.x, s.threads[w * 32 + lane_id()]);
+        if (halves == 2 && w + 1 < warps) k.y = max(k.y, s.threads[w * 32 + 32 + lane_id()]);
     }
+    s.group[lane_id()] = k;
+    __syncwarp();
+    int above_x = 0, from_x = 0, above_y = 0, from_y = 0;               // groups above, and not below, this lane's two
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+        const uint2 o = s.group[j];
+        above_x += (o.x > k.x) + (o.y > k.x); from_x += (o.x >= k.x) + (o.y >= k.x);
+        above_y += (o.x > k.y) + (o.y > k.y); from_y += (o.x >= k.y) + (o.y >= k.y);
+    }
+    if (above_x < n && from_x >= n) s.bound = k.x;
+    if (halves == 2 && above_y < n && from_y >= n) s.bound = k.y;
+}
+
+// The CTA's n largest logits into s.top (0: none left), for the first warp to see.
+template <typename T, bool KEEP, bool GRAD>
+__device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thread_max, int n, LpTop& s) {
+    constexpr int kN = Logits8<T>::kN;
+    const int threads = blockDim.x;
+    const unsigned key = order_key(thread_max);
     __syncthreads();
     const unsigned bound = max(s.bound, kKeyLowest + 1);                // (-infinity is never listed)
     auto collect = [&](const Logits8<T>& x, int v) {
@@ -376,12 +403,13 @@ __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thr
                 for (int i = 0; i < kLpVecs; ++i) collect(x[i], v0 + i * threads);
             });
     } else {
-        // a thread's vectors again, by its whole warp, and those of four threads at a time
-        for (unsigned left = __ballot_sync(0xFFFFFFFFu, key >= bound); left;) {
+        // a thread's vectors again, by a whole warp, those of four threads at a time; neighbouring threads by different warps
+        const int warps = threads / 32;
+        for (unsigned left = __ballot_sync(0xFFFFFFFFu, s.threads[lane_id() * warps + warp_id()] >= bound); left;) {
             int first[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                first[i] = left ? mine.begin + (int)(threadIdx.x & ~31u) + __ffs(left) - 1 + lane_id() * threads : mine.end;
+                first[i] = left ? mine.begin + (__ffs(left) - 1) * warps + warp_id() + lane_id() * threads : mine.end;
                 left &= left - 1;
             }
             for (int at = 0; at < mine.end - mine.begin; at += 32 * threads) {
@@ -395,8 +423,15 @@ __device__ __forceinline__ void find_top(RowPart<T, KEEP, GRAD>& mine, float thr
     }
     __syncthreads();
     const int count = (int)s.count;
+    if (count <= 64) {                                                  // as nearly always: by one warp
+        if (warp_id() == 0) {
+            rank_into(s.list, count, s.top, n, 32);
+            __syncwarp();
+        }
+        return;
+    }
     if (count <= kLpList) {
-        rank_into(s.list, count, s.top, n);
+        rank_into(s.list, count, s.top, n, threads);
         __syncthreads();
         return;
     }
@@ -459,10 +494,12 @@ struct RowSums {
     }
 };
 
-template <typename T, typename OT, bool KEEP, bool GRAD>
+// GRAD: with the gradient; LIST: with the alternatives
+template <typename T, typename OT, bool KEEP, bool GRAD, bool LIST>
 __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRAD ? 2 : 1) k_logprob(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
-    __shared__ LpShared s;
+    __shared__ LpSums s;
+    __shared__ std::conditional_t<LIST, LpTop, LpNoTop> tops;   // (what no call needs would be taken from the first-level cache)
     cg::cluster_group cluster = cg::this_cluster();
     const int ctas = 1 << p.cut, rank = blockIdx.x & (ctas - 1);
     const long long row = blockIdx.x >> p.cut;
@@ -473,11 +510,10 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRA
     mine.end = min(mine.begin + p.vectors, (p.vocab + mine.row.skew + kN - 1) / kN);
     if constexpr (KEEP) mine.fetch(mine.kept, mine.begin + threadIdx.x);
 
-    // (thread 0 of the first CTA alone uses the given token's logit; it is read before anything is written)
+    const Part thread = thread_part(mine, p.scale2);
+    // (thread 0 of the first CTA alone uses the given token's logit; it is read before anything is written, and registers are few while the row is)
     const long long target = checked_target(p, row, rank == 0 && threadIdx.x == 0);
     const float given = target >= 0 && threadIdx.x == 0 ? to_float<T>(x[target]) : 0.f;
-
-    const Part thread = thread_part(mine, p.scale2);
     // (a thread with nothing but NaN and -infinity has no largest logit, but its NaN counts)
     int owner;
     Part all = join_lanes(thread.m == -INFINITY && thread.r != thread.r ? Part{0.f, thread.r, thread.r} : thread, p.scale2, owner);
@@ -487,10 +523,12 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRA
         all.r += exact - __shfl_sync(0xFFFFFFFFu, thread.r, owner);
     }
     if (lane_id() == 0) s.warp[warp_id()] = all;
+    if constexpr (LIST) post_maximum(thread.m, tops);
     __syncthreads();
-    if (GRAD || p.top_n > 0 || ctas > 1 || warp_id() == 0) all = join_lanes(lane_id() < (int)blockDim.x / 32 ? s.warp[lane_id()] : no_part(), p.scale2, owner);
-    else return;
-    if (!GRAD && p.top_n > 0) find_top(mine, thread.m, p.top_n, s);
+    if constexpr (LIST) find_bound(p.top_n, tops);
+    if (GRAD || ctas > 1 || warp_id() == 0) all = join_lanes(lane_id() < (int)blockDim.x / 32 ? s.warp[lane_id()] : no_part(), p.scale2, owner);
+    else if (!LIST) return;
+    if constexpr (LIST) find_top(mine, thread.m, p.top_n, tops);
     if (ctas > 1) {
         if (threadIdx.x == 0) s.cta = all;
         cluster.sync();
@@ -499,7 +537,7 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRA
     }
     const RowSums sums(all);
     if (rank == 0 && threadIdx.x == 0) sums.write(p, row, target, given);
-    if (GRAD) {
+    if constexpr (GRAD) {
         const RowGrad grad(p, row, target, all.m, sums.log_total, sums.entropy);
         OT* const d = static_cast<OT*>(p.dlogits) + row * p.ldd;
         const bool aligned = vec_aligned<OT, kN>(d, mine.row.skew);
@@ -513,24 +551,31 @@ __global__ void __launch_bounds__(KEEP ? kLpThreads : kLpStream, !KEEP ? 4 : GRA
                 store_vec<OT, kN>(d, at, p.vocab, g, aligned);
             }
         });
-    } else if (p.top_n > 0 && rank == 0) {
+    } else if constexpr (LIST) {
         const int n = p.top_n;
-        if (ctas > 1) {
-            for (int i = threadIdx.x; i < ctas * n; i += blockDim.x) s.list[i] = cluster.map_shared_rank(s.top, i / n)[i % n];
-            __syncthreads();
-            if (threadIdx.x < DST_LOGPROB_MAX_TOP) s.top[threadIdx.x] = 0;
-            __syncthreads();
-            rank_into(s.list, ctas * n, s.top, n);
-            __syncthreads();
-        }
-        for (int i = threadIdx.x; i < n; i += blockDim.x) {
-            const u64 k = s.top[i];
+        auto put = [&](int place, u64 k) {
             if (p.top_tokens) {
                 const int token = k == 0 ? -1 : (int)~(unsigned)k;
-                if (p.wide) static_cast<long long*>(p.top_tokens)[row * n + i] = token;
-                else static_cast<int*>(p.top_tokens)[row * n + i] = token;
+                if (p.wide) static_cast<long long*>(p.top_tokens)[row * n + place] = token;
+                else static_cast<int*>(p.top_tokens)[row * n + place] = token;
             }
-            if (p.top_logprob) p.top_logprob[row * n + i] = k == 0 ? -INFINITY : fmaf(of_order_key((unsigned)(k >> 32)) - all.m, p.scale, -sums.log_total);
+            if (p.top_logprob) p.top_logprob[row * n + place] = k == 0 ? -INFINITY : fmaf(of_order_key((unsigned)(k >> 32)) - all.m, p.scale, -sums.log_total);
+        };
+        if (ctas == 1) {
+            if ((int)threadIdx.x < n) put(threadIdx.x, tops.top[threadIdx.x]);
+        } else {
+            // every CTA finds the places of its own n among all: a lane for each of them and each CTA's n (empty places, which all come last, by their own place)
+            for (int i = threadIdx.x; i < ctas * n; i += blockDim.x) tops.list[i] = cluster.map_shared_rank(tops.top, i / n)[i % n];
+            __syncthreads();
+            for (int u0 = warp_id() * 32; u0 < ctas * n; u0 += blockDim.x) {
+                const int i = min((u0 + lane_id()) >> p.cut, n - 1), of = (lane_id() & (ctas - 1)) * n, me = rank * n + i;
+                const u64 k = tops.list[me];
+                int before = 0;
+#pragma unroll 4
+                for (int j = of; j < of + n; ++j) { const u64 o = tops.list[j]; before += o > k || (o == k && j < me); }
+                for (int d = 1; d < ctas; d *= 2) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+                if (u0 + lane_id() < ctas * n && (lane_id() & (ctas - 1)) == 0 && before < n) put(before, k);
+            }
         }
     }
     if (ctas > 1) cluster.sync();                            // (what others read of this CTA stays until then)
@@ -753,7 +798,7 @@ static LogprobShape logprob_shape(long long rows, long long vocab, int per_vecto
     return L;
 }
 
-template <typename T, typename OT, bool KEEP, bool GRAD>
+template <typename T, typename OT, bool KEEP, bool GRAD, bool LIST>
 static cudaError_t logprob_run(const LogprobParams& p, const LogprobShape& L, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * L.ctas)); cfg.blockDim = dim3(L.threads); cfg.stream = stream;
@@ -763,17 +808,18 @@ static cudaError_t logprob_run(const LogprobParams& p, const LogprobShape& L, cu
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = L.ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_logprob<T, OT, KEEP, GRAD>, p);
+    return cudaLaunchKernelEx(&cfg, k_logprob<T, OT, KEEP, GRAD, LIST>, p);
 }
-template <typename T, typename OT, bool GRAD>
+template <typename T, typename OT, bool GRAD, bool LIST>
 static cudaError_t logprob_t(LogprobParams p, int sms, cudaStream_t stream) {
     const LogprobShape L = logprob_shape(p.rows, p.vocab, Logits8<T>::kN, GRAD, sms);
     p.vectors = L.vectors;
     p.cut = L.ctas == 1 ? 0 : L.ctas == 2 ? 1 : L.ctas == 4 ? 2 : 3;
-    return L.keep ? logprob_run<T, OT, true, GRAD>(p, L, stream) : logprob_run<T, OT, false, GRAD>(p, L, stream);
+    return L.keep ? logprob_run<T, OT, true, GRAD, LIST>(p, L, stream) : logprob_run<T, OT, false, GRAD, LIST>(p, L, stream);
 }
 cudaError_t launch_logprob(const LogprobParams& p, int type, int sms, cudaStream_t stream) {
-    return type == DST_F32 ? logprob_t<float, float, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false>(p, sms, stream);
+    if (p.top_n > 0) return type == DST_F32 ? logprob_t<float, float, false, true>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false, true>(p, sms, stream);
+    return type == DST_F32 ? logprob_t<float, float, false, false>(p, sms, stream) : logprob_t<__nv_bfloat16, float, false, false>(p, sms, stream);
 }
 
 template <typename T, typename OT, int N>
@@ -797,7 +843,7 @@ static cudaError_t loss_t(const LogprobParams& p, int sms, cudaStream_t stream) 
         if (vectors <= (Ring<kTwo>::kSlots - 2) * Ring<kTwo>::kChunk) return ring_run<T, OT, kTwo>(p, sms, stream);
         if (vectors <= (Ring<kOne>::kSlots - 2) * Ring<kOne>::kChunk) return ring_run<T, OT, kOne>(p, sms, stream);
     }
-    return logprob_t<T, OT, true>(p, sms, stream);
+    return logprob_t<T, OT, true, false>(p, sms, stream);
 }
 cudaError_t launch_logprob_loss(const LogprobParams& p, int type, int d_type, int sms, cudaStream_t stream) {
     if (type == DST_F32) return d_type == DST_F32 ? loss_t<float, float>(p, sms, stream) : loss_t<float, __nv_bfloat16>(p, sms, stream);

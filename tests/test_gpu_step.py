@@ -584,3 +584,16 @@ def test_a_norm_in_8_bits_goes_into_the_product_whatever_its_buffers_held(d):
         outs.append(torch.empty(21, 50, device="cuda"))
         dst.dst_matmul_fp8(q, w, outs[-1], ws)
     assert torch.equal(*outs) and bool(torch.isfinite(outs[0]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(1, 33), (2, 300), (1, 5000), (40, 1000), (600, 3001), (1, 33708), (90, 33708), (1, 300000)])
+def test_alternatives_of_logits_that_fall_with_the_index(rows, vocab, dtype):
+    g = torch.Generator().manual_seed(vocab)
+    x = -1.2 * torch.log(torch.arange(1, vocab + 1, dtype=torch.float32)) + 0.3 * torch.randn(rows, vocab, generator=g)
+    x[0, vocab // 3:] = -float("inf")
+    x, targets = x.to(TYPES[dtype]).cuda(), torch.zeros(rows, dtype=torch.int64).cuda()
+    for n in (1, 8, 9, 32):
+        check_logprob(x, targets, 1.0, n)
+        check_logprob(x.flip(1).contiguous(), targets + vocab - 1, 1.0, n, torch.int32)
+    check_logprob(torch.zeros_like(x), targets, 1.0, 9)           # as many equal ones as there are

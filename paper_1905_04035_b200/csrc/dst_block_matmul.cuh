@@ -576,7 +576,7 @@ k_block_matmul(const __grid_constant__ CUtensorMap map_p, const __grid_constant_
 
 // out = the parts' results added in their order
 template <typename OT>
-__global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ parts, long long stride, int splits, OT* out, long long ldo, long long rows, int cols) {
+__global__ void __launch_bounds__(256) k_join_parts(const float* parts, long long stride, int splits, OT* out, long long ldo, long long rows, int cols) {
     pdl_trigger();
     pdl_wait();
     const long long total = rows * cols, step = (long long)gridDim.x * 256;

@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const __grid_constant_
 
 // dweight[c] = the CTAs' shares in their order: 32 columns a CTA, each of its warps a run of the shares
 constexpr int kShareWarps = 32;
-__global__ void __launch_bounds__(kShareWarps * 32) k_norm_dweight(const float* __restrict__ parts, int n, int d, float* __restrict__ dweight) {
+__global__ void __launch_bounds__(kShareWarps * 32) k_norm_dweight(const float* parts, int n, int d, float* dweight) {
     __shared__ float sums[kShareWarps][32];
     pdl_trigger();
     pdl_wait();

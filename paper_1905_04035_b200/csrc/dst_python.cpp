@@ -140,22 +140,45 @@ PyObject* matrix(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// a tensor of a type; a new error otherwise
+const at::Tensor* typed(PyObject* o, PyObject* dtype, PyObject* name) {
+    const at::Tensor* const t = tensor_of(o, name);
+    if (!t) return nullptr;
+    PyObject* const is = dtype_name(o);                      // (one object for each type)
+    if (!is) return nullptr;
+    Py_DECREF(is);
+    if (is == dtype) return t;
+    PyErr_Format(PyExc_TypeError, "%U must be %S, got %S", name, dtype, is);
+    return nullptr;
+}
+
 // vector(tensor or None, n, dtype, device, name): pointer of n contiguous elements, or None
 PyObject* vector(PyObject*, PyObject* const* a, Py_ssize_t n) {
     long long elements, device;
     if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments, not %zd", n);
     if (a[0] == Py_None) Py_RETURN_NONE;
     if (!number(a[1], elements) || !number(a[3], device)) return nullptr;
-    const at::Tensor* const t = tensor_of(a[0], a[4]);
-    if (!t) return nullptr;
     try {
-        PyObject* const dtype = dtype_name(a[0]);            // (one object for each type)
-        if (!dtype) return nullptr;
-        Py_DECREF(dtype);
-        if (dtype != a[2]) return PyErr_Format(PyExc_TypeError, "%U must be %S, got %S", a[4], a[2], dtype);
+        const at::Tensor* const t = typed(a[0], a[2], a[4]);
+        if (!t) return nullptr;
         if (t->dim() != 1 || t->size(0) != elements || !t->is_contiguous()) return PyErr_Format(PyExc_ValueError, "%U must be contiguous [%lld]", a[4], elements);
-        if (elsewhere(*t, device)) return nullptr;
-        return PyLong_FromVoidPtr(t->data_ptr());
+        return elsewhere(*t, device) ? nullptr : PyLong_FromVoidPtr(t->data_ptr());
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// table(tensor, rows, dtype, device, name): (pointer, columns) of a contiguous matrix
+PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    long long rows, device;
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments, not %zd", n);
+    if (!number(a[1], rows) || !number(a[3], device)) return nullptr;
+    try {
+        const at::Tensor* const t = typed(a[0], a[2], a[4]);
+        if (!t) return nullptr;
+        if (t->dim() != 2 || t->size(0) != rows || !t->is_contiguous()) return PyErr_Format(PyExc_ValueError, "%U must be contiguous [%lld, n]", a[4], rows);
+        return elsewhere(*t, device) ? nullptr : Py_BuildValue("(NL)", PyLong_FromVoidPtr(t->data_ptr()), (long long)t->size(1));
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -165,7 +188,7 @@ PyObject* vector(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define DST_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(Entry<NAME>::call)), METH_FASTCALL, nullptr}
 #define DST_CHECK(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    DST_CHECK(matrix), DST_CHECK(vector),
+    DST_CHECK(matrix), DST_CHECK(vector), DST_CHECK(table),
     DST_ENTRY(dst_dropout), DST_ENTRY(dst_embed), DST_ENTRY(dst_quantize_fp8), DST_ENTRY(dst_matmul_fp8), DST_ENTRY(dst_linear_fp8),
     DST_ENTRY(dst_quantize_fp4), DST_ENTRY(dst_matmul_fp4), DST_ENTRY(dst_linear_fp4), DST_ENTRY(dst_sample),
     DST_ENTRY(dst_logprob), DST_ENTRY(dst_logprob_loss), DST_ENTRY(dst_logprob_backward), DST_ENTRY(dst_rmsnorm), DST_ENTRY(dst_rmsnorm_backward),

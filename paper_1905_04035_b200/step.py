@@ -10,7 +10,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .binding import DST_BF16, DST_F32, _Tensor, load_library
+from .binding import DST_BF16, DST_F32, _Tensor, load_calls, load_library
 from .tied import _INDEX, Fp8Matrix, _device, _enqueue, _here, _matrix, _vector, _workspace
 
 DST_LOGPROB_MAX_TOP = 32
@@ -35,12 +35,10 @@ def _logits(logits: torch.Tensor, targets: Optional[torch.Tensor], other: Option
 def _stats(t: Optional[torch.Tensor], rows: int, index: int):
     if t is None:
         return None
-    if t.dtype != torch.float32:
-        raise TypeError("stats must be float32, got %s" % t.dtype)
-    if t.shape != (rows, 2) or not t.is_contiguous():
+    at, n = load_calls().table(t, rows, torch.float32, index, "stats")
+    if n != 2:
         raise ValueError("stats must be contiguous [%d, 2]" % rows)
-    _here(t, index)
-    return t.data_ptr()
+    return at
 
 
 def _result(t: Optional[torch.Tensor], index: int):
@@ -61,21 +59,16 @@ def dst_logprob(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, lo
     not computed.  ``result``: an int32/uint8 CUDA tensor of at least 24 bytes that receives ``dst_result_t``."""
     index, head, rows, _ = _logits(logits, targets, top_tokens)
     f32 = torch.float32
-    n, tops = 0, []
-    for t, dtype, name in ((top_tokens, None, "top_tokens"), (top_logprob, f32, "top_logprob")):
-        if t is None:
-            tops.append(None)
-            continue
-        dtype = dtype or (torch.int32 if head[6] == 0 else torch.int64)
-        if t.dtype != dtype:
-            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-        if t.dim() != 2 or t.shape[0] != rows or not t.is_contiguous() or (n and t.shape[1] != n):
-            raise ValueError("%s must be contiguous [%d, n], both alike" % (name, rows))
-        _here(t, index)
-        n = t.shape[1]
-        tops.append(t.data_ptr())
+    n, tokens, their = 0, None, None
+    if top_tokens is not None:
+        tokens, n = load_calls().table(top_tokens, rows, torch.int64 if head[6] else torch.int32, index, "top_tokens")
+    if top_logprob is not None:
+        their, k = load_calls().table(top_logprob, rows, f32, index, "top_logprob")
+        if tokens is not None and k != n:
+            raise ValueError("top_tokens and top_logprob must have as many columns")
+        n = k
     _enqueue("dst_logprob", index, stream, *head, scale, _vector(logprob, rows, f32, index, "logprob"), _vector(lse, rows, f32, index, "lse"),
-             _vector(entropy, rows, f32, index, "entropy"), _stats(stats, rows, index), n, *tops, _result(result, index))
+             _vector(entropy, rows, f32, index, "entropy"), _stats(stats, rows, index), n, tokens, their, _result(result, index))
 
 
 def dst_logprob_loss(logits: torch.Tensor, targets: Optional[torch.Tensor], dlogprob: Optional[torch.Tensor], logprob: Optional[torch.Tensor],

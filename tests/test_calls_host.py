@@ -85,6 +85,12 @@ def test_tensors_are_looked_at(calls):
             calls.vector(bad, 6, torch.int32, CPU, "v")
     with pytest.raises(ValueError, match="same device"):
         calls.vector(v, 6, torch.int32, 2, "v")
+    assert calls.table(x, 3, torch.float32, CPU, "x") == (x.data_ptr(), 8) and calls.table(x[:, :0].contiguous(), 3, torch.float32, CPU, "x")[1] == 0
+    for bad, error, said in ((x.int(), TypeError, "x must be torch.float32, got torch.int32"), (x[:2], ValueError, r"x must be contiguous \[3, n\]"), (x[:, :4], ValueError, "contiguous"), (v, TypeError, "float32"), (None, TypeError, "x must be a tensor")):
+        with pytest.raises(error, match=said):
+            calls.table(bad, 3, torch.float32, CPU, "x")
+    with pytest.raises(ValueError, match="same device"):
+        calls.table(x, 3, torch.float32, 0, "x")
     for wrong in (lambda: calls.matrix(x, 3, 8, CPU), lambda: calls.matrix(x, 3, 8, CPU, 5), lambda: calls.matrix(x, "3", 8, CPU, "x"), lambda: calls.vector(v, 6)):
         with pytest.raises(TypeError):
             wrong()

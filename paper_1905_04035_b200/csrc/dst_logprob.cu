@@ -10,13 +10,14 @@
 // 16 bytes a thread, keep it in registers for the gradient and the alternatives (k_logprob); for the gradient of many long rows a CTA keeps a whole
 // row in shared memory (k_logprob_ring).
 //
-// Alternatives: the n-th largest of the maxima of 32 or 64 groups of logits is a bound that n logits reach at least and
-// few more than n do; those are collected and ranked by counting, and the CTAs of a row place their own n among all.  Where too many reach it (equal logits), n
-// rounds look for the next largest instead.
+// Alternatives: the n-th largest of the maxima of 32 or 64 groups of logits is a bound that n logits reach at least and few more than n
+// do; those are collected and ranked by counting, and the CTAs of a row place their own n among all.  Where too many reach it (equal
+// logits), n rounds look for the next largest instead.
 //
-// Measured: forward 8111 x 33,708 fp32 162 us (6750 GB/s: the rate of reading), 4096 x 33,708 bf16 52 us (5270 GB/s; the exponential unit is 63 % busy,
-// the issue slots 64 %), 512 x 65,536 bf16 16 us and 19.4 with five alternatives, one row of 33,708 fp32 3.7 us and 6.6 with twenty; loss and gradient of
-// 4096 x 33,708 bf16 120 us (4600 GB/s; two exponentials a logit), of 8111 x 33,708 fp32 400 us (5470 GB/s); the gradient alone 99 us (5580) and 348 (6290).
+// Measured: forward 8111 x 33,708 fp32 162 us (6750 GB/s: the rate of reading), 4096 x 33,708 bf16 52 us (5270 GB/s; the exponential unit
+// and the issue slots are 67 % busy), 512 x 65,536 bf16 16 us and 19.4 with five alternatives, one row of 33,708 fp32 3.7 us and 6.6 with
+// twenty; loss and gradient of 4096 x 33,708 bf16 120 us (4600 GB/s; two exponentials a logit), of 8111 x 33,708 fp32 400 us (5470 GB/s);
+// the gradient alone 99 us (5580) and 348 (6290).
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -586,8 +587,9 @@ template <typename T, typename OT>
 __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
     const int parts = ((p.vocab + 2 * kN - 2) / kN + p.vectors - 1) / p.vectors;
-    const long long row = blockIdx.x / parts;
-    const int part = (int)(blockIdx.x - row * parts);
+    const unsigned block = gridDim.x - 1 - blockIdx.x;       // last rows first: what the forward call read last is still in L2 (both calls on 4096 x 33,708 bf16: 155 us, 156.2 from the first on)
+    const long long row = block / parts;
+    const int part = (int)(block - row * parts);
     pdl_trigger();
     pdl_wait();
     const RowView<T> x(static_cast<const T*>(p.logits) + row * p.ld, p.vocab);

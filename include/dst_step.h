@@ -119,8 +119,8 @@ int dst_grad_norm(const dst_tensor_t* tensors, int64_t count, double max_norm, f
 /*
  * outs[i] = clip[1] * tensors[i], rounded once to outs[i]'s type; the two lists have the same lengths.  A factor of 0
  * writes zeros whatever the elements are.  outs may be the same list: in place, where types agree, and a factor of 1
- * then touches nothing.  Otherwise no output may overlap a tensor, and none another output, in place either (a tensor that is
- * listed twice would be scaled twice; in the norm it counts twice).
+ * then touches nothing.  Otherwise an output that overlaps a tensor, or another output, is refused, in place too (a tensor that is
+ * listed twice would be scaled twice; in the norm it counts twice).  Tensors may overlap one another.
  */
 int dst_clip(const dst_tensor_t* tensors, const dst_tensor_t* outs, int64_t count, const float* clip, dst_stream_t stream);
 

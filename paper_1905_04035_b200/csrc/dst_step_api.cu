@@ -1,6 +1,10 @@
 // C ABI of a step's operators: argument checks and kernel sequencing.
 #include <math.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "dst_step.cuh"
 
 namespace dst {
@@ -54,6 +58,35 @@ static bool tensors_fit(const dst_tensor_t* t, int64_t count) {
     if (count > kMaxTensors) return false;
     for (int64_t i = 0; i < count; ++i) if (t[i].n > kMaxTensor) return false;
     return true;
+}
+
+
+// Whether every output has memory of its own: none lies on another, nor on a tensor other than the one that it takes the place of.
+// A CTA writes an output's chunk while others have yet to read theirs.
+struct Span { uintptr_t from, to; };
+static Span span_of(const dst_tensor_t& t) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(t.data);
+    return Span{at, t.n > kMaxTensor ? UINTPTR_MAX : at + uintptr_t(t.n) * type_size(t.type)};
+}
+static int outputs_apart(const dst_tensor_t* in, const dst_tensor_t* out, int64_t count) {
+    constexpr int64_t kFew = 128;
+    Span few[kFew];
+    std::unique_ptr<Span[]> many;
+    if (count > kFew) many.reset(new (std::nothrow) Span[size_t(count)]);
+    Span* const spans = count > kFew ? many.get() : few;
+    if (!spans) return DST_ERR_UNSUPPORTED;
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; ++i) if (out[i].n > 0) spans[n++] = span_of(out[i]);
+    std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.from < b.from; });
+    for (int64_t i = 1; i < n; ++i) if (spans[i - 1].to > spans[i].from) return DST_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < count; ++i) {
+        if (in[i].n == 0 || in[i].data == out[i].data) continue;             // (in place: where its output is)
+        const Span s = span_of(in[i]);
+        if (s.to <= spans[0].from || s.from >= spans[n - 1].to) continue;    // (as of lists that were made one after the other)
+        const Span* const after = std::lower_bound(spans, spans + n, s.to, [](const Span& a, uintptr_t to) { return a.from < to; });
+        if (after > spans && after[-1].to > s.from) return DST_ERR_INVALID_ARG;   // the last output that starts before its end
+    }
+    return DST_OK;
 }
 
 }  // namespace dst
@@ -181,11 +214,14 @@ int dst_grad_norm(const dst_tensor_t* tensors, int64_t count, double max_norm, f
 
 int dst_clip(const dst_tensor_t* tensors, const dst_tensor_t* outs, int64_t count, const float* clip, dst_stream_t stream) {
     if (!tensors_ok(tensors, count) || !tensors_ok(outs, count) || !clip || misaligned(clip, 4)) return DST_ERR_INVALID_ARG;
-    if (!tensors_fit(tensors, count)) return DST_ERR_UNSUPPORTED;
+    if (count > kMaxTensors) return DST_ERR_UNSUPPORTED;
     for (int64_t i = 0; i < count; ++i) {
         if (tensors[i].n != outs[i].n) return DST_ERR_INVALID_ARG;
         if (tensors[i].n > 0 && tensors[i].data == outs[i].data && tensors[i].type != outs[i].type) return DST_ERR_INVALID_ARG;
     }
+    const int rc = outputs_apart(tensors, outs, count);
+    if (rc != DST_OK) return rc;
+    if (!tensors_fit(tensors, count)) return DST_ERR_UNSUPPORTED;
     int launches = 0;
     const cudaError_t e = launch_clip(tensors, outs, count, clip, &launches, stream);
     return done(e, launches);

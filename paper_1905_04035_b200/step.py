@@ -211,7 +211,8 @@ def dst_grad_norm(tensors: TensorList, clip: torch.Tensor, max_norm: float, work
 
 
 def dst_clip(tensors: TensorList, clip: torch.Tensor, outs: Optional[TensorList] = None, *, stream=None) -> None:
-    """Enqueue ``dst_clip``: every tensor times ``clip[1]``, into ``outs`` or in place."""
+    """Enqueue ``dst_clip``: every tensor times ``clip[1]``, into ``outs`` or in place.  An output may be its own tensor; one that shares
+    memory with another tensor, or with another output, is refused."""
     index, pc = _clip(clip)
     _on(tensors, index)
     if outs is None:

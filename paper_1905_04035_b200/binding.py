@@ -4,6 +4,9 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import sysconfig
+from importlib.machinery import ExtensionFileLoader
+from importlib.util import module_from_spec, spec_from_file_location
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -181,13 +184,22 @@ def load_library():
     return _lib
 
 
+def calls_path() -> str:
+    """The file of the Python module of the library's entries.  It is compiled with the memory layouts of torch's tensors and of Python's
+    objects, so its name says which, and another torch or Python finds none until it is built there."""
+    return os.path.join(_HERE, "_calls-torch%s-abi%d%s" % (torch.__version__, torch.compiled_with_cxx11_abi(), sysconfig.get_config_var("EXT_SUFFIX")))
+
+
 def load_calls():
-    """Load the Python module of the library's entries, for calls that are short; raises if it has not been built."""
+    """Load the Python module of the library's entries, for calls that are short; raises if it has not been built for this torch and
+    this Python, or does not load."""
     global _calls
     if _calls is None:
         load_library()
+        loader = ExtensionFileLoader(__package__ + "._calls", calls_path())
         try:
-            from . import _calls as calls
+            calls = module_from_spec(spec_from_file_location(loader.name, loader.path, loader=loader))
+            loader.exec_module(calls)
         except ImportError as e:
             raise ImportError("%s: build it with `python -m paper_1905_04035_b200.build`" % e)
         _calls = calls

@@ -11,8 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libdst_b200.so")
-CALLS_PATH = os.path.join(HERE, "_calls.so")         # the entries as a Python module
-CALLS_SOURCE = os.path.join(CSRC, "dst_python.cpp")
+CALLS_SOURCE = os.path.join(CSRC, "dst_python.cpp")  # the entries as a Python module (binding.calls_path())
 SOURCES = ["dst_api.cu", "dst_index_kernels.cu", "dst_front_cluster.cu", "dst_reduce_kernels.cu",
            "dst_accumulate_kernels.cu", "dst_dropout.cu", "dst_fp8.cu", "dst_fp4.cu", "dst_sample.cu", "dst_tied_api.cu",
            "dst_logprob.cu", "dst_norm.cu", "dst_clip.cu", "dst_step_api.cu"]
@@ -29,12 +28,29 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def _older(path: str, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(p) > os.path.getmtime(path) for p in deps)
+
+
+def stale_parts():
+    """Whether the library, and the Python module of its entries, are to be built: missing, older than their sources, or such as do not load."""
+    from . import binding
+    library = _older(LIB_PATH, [os.path.join(CSRC, s) for s in SOURCES] + HEADERS)
+    calls = library or _older(binding.calls_path(), [CALLS_SOURCE] + HEADERS)
+    if not library:                                   # (what is to be built anew is not loaded before)
+        try:
+            binding.load_library()
+            if not calls:
+                binding.load_calls()
+        except ImportError:
+            calls = True
+        except (OSError, AttributeError):
+            library = calls = True
+    return library, calls
+
+
 def is_stale() -> bool:
-    if not (os.path.exists(LIB_PATH) and os.path.exists(CALLS_PATH)):
-        return True
-    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALLS_PATH))
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS + [CALLS_SOURCE]
-    return any(os.path.getmtime(p) > t for p in deps)
+    return any(stale_parts())
 
 
 def _calls_commands(obj: str, out: str):
@@ -50,33 +66,37 @@ def _calls_commands(obj: str, out: str):
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu file, link ``libdst_b200.so`` next to this file, and the Python module of its entries."""
-    if not force and not is_stale():
-        return LIB_PATH
+    """Compile every .cu file and link ``libdst_b200.so`` next to this file, and the Python module of its entries; of the two, what is stale."""
+    from . import binding
+    library, calls = (True, True) if force else stale_parts()
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     nvcc = _nvcc()
-    objs = []
     procs = []
-    for s in SOURCES:
-        obj = os.path.join(objdir, s.replace(".cu", ".o"))
+    objs = []
+    for s in SOURCES if library else []:
+        obj = os.path.join(objdir, s[:-3] + ".o")
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, s), "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
     tag = ".tmp.%d" % os.getpid()
-    compile_calls, link_calls = _calls_commands(os.path.join(objdir, "dst_python.o"), CALLS_PATH + tag)
-    procs.append((compile_calls, subprocess.Popen(compile_calls, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    calls_path = binding.calls_path()
+    compile_calls, link_calls = _calls_commands(os.path.join(objdir, "dst_python.o"), calls_path + tag)
+    if calls:
+        procs.append((compile_calls, subprocess.Popen(compile_calls, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, p in procs:
         out, _ = p.communicate()
         if verbose or p.returncode != 0:
             sys.stderr.write(out)
         if p.returncode != 0:
             raise RuntimeError("compilation failed: %s" % " ".join(cmd))
-    tmp = LIB_PATH + tag
-    subprocess.check_call([nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-ldl"])
-    os.replace(tmp, LIB_PATH)
-    subprocess.check_call(link_calls)
-    os.replace(CALLS_PATH + tag, CALLS_PATH)
+    if library:
+        tmp = LIB_PATH + tag
+        subprocess.check_call([nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-ldl"])
+        os.replace(tmp, LIB_PATH)
+    if calls:
+        subprocess.check_call(link_calls)
+        os.replace(calls_path + tag, calls_path)
     return LIB_PATH
 
 

@@ -58,7 +58,7 @@ def _calls_commands(obj: str, out: str):
     import torch
 
     base = os.path.join(os.path.dirname(torch.__file__), "include")
-    include = [INCLUDE, sysconfig.get_paths()["include"], base, os.path.join(base, "torch", "csrc", "api", "include"), "/usr/local/cuda/include"]
+    include = [INCLUDE, sysconfig.get_paths()["include"], base, os.path.join(base, "torch", "csrc", "api", "include")]
     flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi()]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     return (["g++"] + flags + [a for i in include for a in ("-I", i)] + ["-c", CALLS_SOURCE, "-o", obj],

@@ -57,3 +57,9 @@ def test_a_library_that_does_not_load_is_stale(fresh, monkeypatch, tmp_path):
     assert build.is_stale() and build.stale_parts() == (True, True)
     with pytest.raises(OSError):
         dst.load_library()
+
+
+def test_the_module_is_compiled_without_a_toolkit_s_headers():
+    """It includes none of CUDA's, and the compiler that the library is built with may lie anywhere."""
+    compile_calls, link_calls = build._calls_commands("a.o", "a.so")
+    assert not any("cuda" in os.path.relpath(a, os.path.dirname(torch.__file__)) for a in compile_calls + link_calls if a.startswith("/"))

@@ -75,8 +75,8 @@ int dst_logprob_backward(const void* logits, int64_t ld, int32_t type, int64_t r
  *   x [rows, d] in x_type; residual (optional) and sum_out (optional, receives h; may be residual, or x where types
  *   agree) in sum_type; weight [d] fp32 or NULL (ones); inv_rms [rows] fp32, optional, for the backward pass
  *   out [rows, d] in out_type and / or q, its 8-bit form (DST_FP8_ROW blocks, rounded once from fp32, as
- *   dst_quantize_fp8 would from an fp32 y); one of them at least.  out may be x, residual or sum_out's buffer only where
- *   that one is not needed afterwards and type and leading dimension agree.
+ *   dst_quantize_fp8 would from an fp32 y); one of them at least.  out may be x's or residual's buffer where that one is not
+ *   needed afterwards and type and leading dimension agree; sum_out's holds h, and out in its place is refused.
  */
 #define DST_RMSNORM_MAX_D 16384
 int dst_rmsnorm(const void* x, int64_t ldx, int32_t x_type, const void* residual, int64_t ldr, void* sum_out,

@@ -123,6 +123,9 @@ int dst_linear_fp8(const void* x, int64_t ldx, int32_t x_type, int64_t M, const 
  *          the lower half for even ones.  An odd last column's other half, and the rest of its 4-byte word, are written as zeros
  *   scale  as in dst_fp8_t with blocks of 32: the byte of row r and block b in tile (r / 128) * ld_scale + b / 4, so that
  *          ld_scale is at least cols / 128, rounded up.  dst_quantize_fp4 writes whole groups of four blocks
+ * The products read what dst_quantize_fp4 writes beyond the last column, up to a multiple of 128: elements that are zero and scales that
+ * are numbers.  So the first columns of a matrix that holds more are a matrix of their own where cols is a multiple of 128, and
+ * otherwise once they are quantised as such.
  */
 typedef struct {
     void* q;

@@ -179,7 +179,8 @@ class Fp4Matrix:
         self._c = _Fp4(self.q.data_ptr(), self.scale.data_ptr(), rows, cols, self.q.shape[1], self.scale.shape[1])
 
     def part(self, rows: int, cols: int) -> "Fp4Matrix":
-        """The same buffers seen as a smaller matrix (leading dimensions stay)."""
+        """The same buffers seen as a smaller matrix (leading dimensions stay), to be quantised into.  Of what they hold already it is the
+        first rows and columns where ``cols`` is a multiple of 128 or all there are: a product reads up to such a multiple."""
         if not (0 <= rows <= self.rows and 0 <= cols <= self.cols):
             raise ValueError("a part is at most [%d, %d]" % (self.rows, self.cols))
         m = object.__new__(Fp4Matrix)

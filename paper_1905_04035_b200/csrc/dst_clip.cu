@@ -3,7 +3,8 @@
 // The tensors are cut into chunks, numbered through the list; a CTA takes every gridDim.x-th and finds the tensor by bisection
 // in the table, which travels as a kernel parameter (longer lists take several launches).  Squares are summed in 64 bits:
 // exact to 2^-52, and neither a large gradient overflows nor a small one vanishes.  The CTAs' sums are added in their order by one
-// CTA, so the norm depends on the sizes and values alone.  Bound by memory: the list is read once for the norm, read and written
+// CTA, so the norm depends on the values, the sizes and types, and on which tensors are aligned to 16 bytes (the others are read an element
+// a thread, and their squares are added up in other lanes).  Bound by memory: the list is read once for the norm, read and written
 // once for the scaling.
 // Measured: 186 million gradients, 34.5 million in fp32 and 151 in bf16: norm 70 us (6280 GB/s; 74 by way of the first-level cache), scaling 144 us (6110 GB/s); 163,840 in fp32: 3.9
 // and 3.3 us, launches and one round of loads.

@@ -45,12 +45,6 @@ __device__ __forceinline__ const ClipEntry& tensor_of(const ClipTable& t, int ch
 }
 __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// 16 bytes, not kept in the first-level cache (volatile: it stays behind the wait for the kernel before)
-__device__ __forceinline__ uint4 read_once(const void* p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* x, int n) {
     double s[2] = {0., 0.};

@@ -225,13 +225,6 @@ struct RowGrad {
     }
 };
 
-// 16 bytes that are read once and that nothing writes meanwhile (volatile: it stays behind the wait for the kernel before)
-__device__ __forceinline__ uint4 read_once(const void* p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-
 // A CTA's part of a row.  KEEP: four vectors a thread, that stay in registers.
 template <typename T, bool KEEP, bool GRAD> struct RowPart {
     static constexpr int kN = Logits8<T>::kN;

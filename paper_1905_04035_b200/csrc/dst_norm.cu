@@ -31,12 +31,12 @@ template <int MODE, int PER> struct Place {
 template <typename T, int MODE, int PER> struct Elements {
     static constexpr int kBits = 8 * (int)sizeof(T);
     unsigned w[MODE == 0 ? PER : PER * kBits / 32];
-    __device__ __forceinline__ void load(const T* row, const Place<MODE, PER>& at, bool wanted) {
+    __device__ __forceinline__ void load(const T* row, const Place<MODE, PER>& at) {
         if constexpr (MODE == 0) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 w[i] = 0u;
-                if (wanted && at.here(i)) {
+                if (at.here(i)) {
                     if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(row[at.col(i)]);
                     else w[i] = (unsigned)__bfloat16_as_ushort(row[at.col(i)]) << 16;
                 }
@@ -45,7 +45,7 @@ template <typename T, int MODE, int PER> struct Elements {
             constexpr int kWords = MODE * kBits / 32;
 #pragma unroll
             for (int v = 0; v < PER / MODE; ++v) {
-                const bool in = wanted && at.here(v * MODE);
+                const bool in = at.here(v * MODE);
                 const T* const from = row + at.col(v * MODE);
 #pragma unroll
                 for (int j = 0; j < kWords; j += 4) {
@@ -112,14 +112,14 @@ __device__ __forceinline__ void store_row(void* out, long long offset, const Pla
 template <typename T, int MODE, int PER>
 __device__ __forceinline__ void load_row(const void* from, long long offset, const Place<MODE, PER>& at, float (&v)[PER]) {
     Elements<T, MODE, PER> e;
-    e.load(static_cast<const T*>(from) + offset, at, true);
+    e.load(static_cast<const T*>(from) + offset, at);
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = e.get(i);
 }
 template <int MODE, int PER>
 __device__ __forceinline__ void load_weight(const float* weight, const Place<MODE, PER>& at, float (&w)[PER]) {
     Elements<float, MODE, PER> e;
-    if (weight) e.load(weight, at, true);
+    if (weight) e.load(weight, at);
 #pragma unroll
     for (int i = 0; i < PER; ++i) w[i] = weight ? e.get(i) : 1.f;
 }
@@ -184,8 +184,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm(const __grid_constant__ NormPar
     Elements<ST, MODE, PER> r;
     constexpr bool kAhead = PER == 16;                                     // (32 elements of the next row do not fit the registers)
     auto load = [&](long long of) {
-        x.load(static_cast<const XT*>(p.x) + of * p.ldx, at, true);
-        if (p.residual) r.load(static_cast<const ST*>(p.residual) + of * p.ldr, at, true);
+        x.load(static_cast<const XT*>(p.x) + of * p.ldx, at);
+        if (p.residual) r.load(static_cast<const ST*>(p.residual) + of * p.ldr, at);
     };
     if (kAhead) load(row);
     float w[PER];
@@ -236,8 +236,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const __grid_constant_
     Elements<HT, MODE, PER> h;
     float inv = 0.f;
     auto load = [&](long long of) {
-        y.load(static_cast<const DT*>(p.dy) + of * p.ldy, at, true);
-        h.load(static_cast<const HT*>(p.h) + of * p.ldh, at, true);
+        y.load(static_cast<const DT*>(p.dy) + of * p.ldy, at);
+        h.load(static_cast<const HT*>(p.h) + of * p.ldh, at);
         inv = p.inv_rms[of];
     };
     constexpr bool kAhead = PER == 16;                                     // (32 elements of the next row do not fit the registers)

@@ -68,4 +68,15 @@ size_t grad_norm_workspace(const dst_tensor_t* tensors, long long count);
 cudaError_t launch_grad_norm(const dst_tensor_t* tensors, long long count, double max_norm, float* clip, void* workspace, int* launches, cudaStream_t stream);
 cudaError_t launch_clip(const dst_tensor_t* tensors, const dst_tensor_t* outs, long long count, const float* clip, int* launches, cudaStream_t stream);
 
+// ---- device helpers ---------------------------------------------------------------
+#ifdef __CUDACC__
+// 16 bytes that are read once and that nothing writes meanwhile, not kept in the first-level cache (volatile: it stays behind the wait for
+// the kernel before)
+__device__ __forceinline__ uint4 read_once(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+#endif
+
 }  // namespace dst

@@ -9,18 +9,6 @@
 
 namespace dst {
 
-static bool dtype_ok(int t) { return t == DST_F32 || t == DST_BF16; }
-static bool index_ok(int t) { return t == DST_I32 || t == DST_I64; }
-static size_t type_size(int t) { return t == DST_F32 ? 4 : 2; }
-static bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-static bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int type) {
-    return rows >= 0 && cols >= 0 && ld >= cols && !misaligned(p, type_size(type)) && (p || rows == 0 || cols == 0);
-}
-static int done(cudaError_t e, int launches) {
-    if (e != cudaSuccess) { cudaGetLastError(); return DST_ERR_CUDA; }
-    count_launches(launches);
-    return DST_OK;
-}
 constexpr int64_t kMaxLogits = int64_t(1) << 30, kMaxLogitRows = int64_t(1) << 27, kMaxNormRows = int64_t(1) << 31;
 constexpr int64_t kMaxTensor = int64_t(1) << 44, kMaxTensors = int64_t(1) << 24;
 

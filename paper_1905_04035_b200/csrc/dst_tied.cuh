@@ -10,6 +10,20 @@ namespace dst {
 int device_sm_count();                      // of the current device, asked of the runtime once
 void count_launches(int n);                 // what dst_kernel_launches reports
 
+// ---- what the C entries look at, and how they end ---------------------------------
+inline bool dtype_ok(int t) { return t == DST_F32 || t == DST_BF16; }
+inline bool index_ok(int t) { return t == DST_I32 || t == DST_I64; }
+inline size_t type_size(int t) { return t == DST_F32 ? 4 : 2; }
+inline bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+inline bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int type) {
+    return rows >= 0 && cols >= 0 && ld >= cols && !misaligned(p, type_size(type)) && (p || rows == 0 || cols == 0);
+}
+inline int done(cudaError_t e, int launches) {
+    if (e != cudaSuccess) { cudaGetLastError(); return DST_ERR_CUDA; }
+    count_launches(launches);
+    return DST_OK;
+}
+
 // ---- dropout and embedding (dst_dropout.cu) ---------------------------------------
 struct DropParams {                         // the generator's keys of every round and counter, and the factor of a kept element
     unsigned key0[10], key1[10];

@@ -5,16 +5,6 @@
 
 namespace dst {
 
-static bool dtype_ok(int t) { return t == DST_F32 || t == DST_BF16; }
-static bool index_ok(int t) { return t == DST_I32 || t == DST_I64; }
-static size_t type_size(int t) { return t == DST_F32 ? 4 : 2; }
-static bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-static int done(cudaError_t e, int launches) {
-    if (e != cudaSuccess) { cudaGetLastError(); return DST_ERR_CUDA; }
-    count_launches(launches);
-    return DST_OK;
-}
-
 constexpr int64_t kMaxCols = int64_t(1) << 30;   // columns of a row, and rows of a matrix in 8 bits
 
 // The generator's parameters; false: refused.
@@ -48,10 +38,6 @@ int fp8_view(const dst_fp8_t* m, Fp8View& v) {
     v = Fp8View{static_cast<uint8_t*>(m->q), static_cast<uint8_t*>(m->scale), (long long)m->rows, (long long)m->cols, (long long)m->ld,
                 (long long)m->ld_scale, m->block == DST_FP8_SQUARE};
     return DST_OK;
-}
-
-static bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int type) {
-    return rows >= 0 && cols >= 0 && ld >= cols && !misaligned(p, type_size(type)) && (p || rows == 0 || cols == 0);
 }
 
 static int fp4_view(const dst_fp4_t* m, Fp8View& v) {

@@ -32,7 +32,8 @@ extern "C" {
  *   entropy [rows]        -sum p_i log p_i
  *   top_tokens, top_logprob [rows, top_n]   the top_n <= DST_LOGPROB_MAX_TOP largest logits in descending order, equal
  *                         ones by index, and their log p; logits of -infinity and NaN are not listed, places left over
- *                         hold token -1 and -infinity
+ *                         hold token -1 and -infinity.  A row in which hundreds of logits equal the last of these (all logits
+ *                         equal; a mask of the type's lowest value that leaves fewer than top_n) is read once more for each
  * targets [rows] and top_tokens have index_type.  A negative target marks a row without one (padding); one of vocab or
  * more counts as none too, and is counted in `result` (optional, cleared by this call).  Every output may be NULL;
  * targets may be NULL where logprob is.

@@ -12,7 +12,8 @@
 //
 // Alternatives: the n-th largest of the maxima of 32 or 64 groups of logits is a bound that n logits reach at least and few more than n
 // do; those are collected and ranked by counting, and the CTAs of a row place their own n among all.  Where too many reach it (equal
-// logits), n rounds look for the next largest instead.
+// logits), n rounds look for the next largest instead, each of which reads the row again (all logits equal: 512 x 65,536 bf16 with five alternatives
+// 251 us, with twenty 787, where others take 19 and 24; 4096 x 33,708 bf16 with five 1230 and 84; one row of 33,708 fp32 with twenty 31 and 6.6).
 //
 // Measured: forward 8111 x 33,708 fp32 162 us (6750 GB/s: the rate of reading), 4096 x 33,708 bf16 52 us (5270 GB/s; the exponential unit
 // and the issue slots are 67 % busy), 512 x 65,536 bf16 16 us and 19.4 with five alternatives, one row of 33,708 fp32 3.7 us and 6.6 with
@@ -580,7 +581,7 @@ template <typename T, typename OT>
 __global__ void __launch_bounds__(256) k_logprob_backward(const __grid_constant__ LogprobParams p) {
     constexpr int kN = Logits8<T>::kN;
     const int parts = ((p.vocab + 2 * kN - 2) / kN + p.vectors - 1) / p.vectors;
-    const unsigned block = gridDim.x - 1 - blockIdx.x;       // last rows first: what the forward call read last is still in L2 (both calls on 4096 x 33,708 bf16: 155 us, 156.2 from the first on)
+    const unsigned block = gridDim.x - 1 - blockIdx.x;       // last rows first: what the forward call read last is still in L2 (both calls, in turn with the first row first, three times: 8111 x 33,708 fp32 497 us against 501, 700 x 33,708 54.0 against 55.3, 4096 x 33,708 bf16 159.9 against 161.0)
     const long long row = block / parts;
     const int part = (int)(block - row * parts);
     pdl_trigger();
@@ -828,6 +829,10 @@ static cudaError_t ring_run(const LogprobParams& p, int sms, cudaStream_t stream
 }
 template <typename T, typename OT>
 static cudaError_t loss_t(const LogprobParams& p, int sms, cudaStream_t stream) {
+    // Threads: two CTAs an SM while a row fits half of its shared memory, as many as their registers allow (4096 x 33,708 bf16 122 us with 384, 136 with 320,
+    // 128 with 288, 130 with 256; shorter rows 2400 x 9000 35.2, 34.7, 32.9, 36.6); else one CTA of 480, whose slots
+    // hold rows of up to 12 chunks of 960 vectors, where 736 threads have room for 7 of 1472 (8111 x 33,708 fp32 372 us with 480, 392 with 416, 374 with 640,
+    // 363 with 736; 4096 x 65,536 bf16 249, 249, 250, 238).
     constexpr int kTwo = 384, kOne = 480;
     const long long vectors = (p.vocab + 2 * Logits8<T>::kN - 2) / Logits8<T>::kN;
     // More than half as many rows as SMs, fewer of which are cut, and rows longer than four vectors for each of 256 threads, which keep them in

@@ -8,7 +8,12 @@
 // theirs, so the order follows from the sizes alone.
 //
 // Measured, with the residual: 8192 x 512 bf16 6.8 us forward, 11.9 backward (3 of them the joining of the weight's shares; 33.5 MB each way need 5.1); 12,801 x
-// 1021 fp32, unaligned, 35 and 38 us (209 MB need 31.9).
+// 1021 fp32, unaligned, 35 and 38 us (209 MB need 31.9).  To 8 bits, without and with a result in bf16: 8192 x 512 7.8 and 8.8 us (29.4 and 37.7 MB need 4.5 and
+// 5.8), 8192 x 1024 13.0 and 14.7 (9.0 and 11.5), 48 x 1024 1.9 and 2.0.
+//
+// Above 8192 columns a lane's 32 elements and, in the gradient, as many of the weight's leave 128 registers short: the gradient spills 390 to 520 bytes a thread, the forward
+// pass 136 at most.  2048 x 16,384 bf16 49 us forward, 114 backward (90 without the weight's gradient; 40.9 needed each way), fp32 89 and 138 (81.8); 2047 x 16,381 bf16,
+// unaligned, 166 and 184.  2048 x 8192 bf16 25 and 45 (20.5), fp32 43 and 52 (40.9).
 #include "dst_fp8.cuh"
 #include "dst_step.cuh"
 

@@ -48,7 +48,6 @@ static bool tensors_fit(const dst_tensor_t* t, int64_t count) {
     return true;
 }
 
-
 // Whether every output has memory of its own: none lies on another, nor on a tensor other than the one that it takes the place of.
 // A CTA writes an output's chunk while others have yet to read theirs.
 struct Span { uintptr_t from, to; };
